@@ -307,6 +307,86 @@ int moshpit_refresh_donors(moshpit_ctx *h, int64_t t, uint64_t seed, const uint8
 int moshpit_grouped_round(moshpit_ctx *h, const int32_t *index_host, int64_t n_index, int32_t group_size,
                           const uint8_t *alive_host);
 
+/* ---- A peer's local step when the peers are language models ----------------
+ * What lies between a row of the state (the parameters of one peer) and a row of
+ * the gradient matrix that moshpit_local_step, moshpit_sgd_round and
+ * moshpit_sgd_run take.  Every call works on all N peers at once, is queued on
+ * the bound stream and returns without waiting.  Matrices of activations are
+ * device memory, [N * n_tokens][row stride] with row i * n_tokens + t for token t
+ * of peer i, elements MOSHPIT_F32 or MOSHPIT_BF16 whatever the state's type, rows
+ * starting on any element; tokens and per-token values are device arrays
+ * [N][n_tokens].  A token outside [0, vocab) is a place without a token (padding;
+ * an absent peer has nothing else).  Arithmetic and sums are binary32 (or wider),
+ * rounded once when stored; the order of every sum follows from the sizes and the
+ * tokens alone, so a call repeats to the bit.  Workspace belongs to the handle and
+ * grows at the first call that needs more (that call waits for the stream and
+ * allocates): make one call of each size before a graph capture.  Tensors last
+ * written on another stream than the bound one must be ordered by the caller.
+ * Limits: n_tokens <= 2^30, N * n_tokens < 2^31, 2^23 elements per activation
+ * row, 2^27 entries of a vocabulary of logits; a launch beyond 2^32 - 1 threads
+ * is an error. */
+
+/* Embedding lookup: out[i][t][:] = scale * table_i[token][:], zeros where there is
+ * no token.  The table of peer i is its parameters column .. column + vocab * width
+ * - 1, read as [vocab][width].  n_tokens = 1 is a step of generation. */
+int moshpit_embed(moshpit_ctx *h, int64_t column, int64_t vocab, int64_t width, const int32_t *tokens_dev, int64_t n_tokens,
+                  float scale, void *out_dev, int32_t out_dtype, int64_t out_row_stride);
+
+/* Its gradient, into the same columns of grad_dev (laid out as for
+ * moshpit_local_step):
+ *   grad_i[v][:] = scale * sum over t with token[i][t] == v of dy[i][t][:],
+ * zeros for rows without a token; accumulate != 0 adds to what is there and leaves
+ * rows without a token alone.  Other columns are not touched. */
+int moshpit_embed_grad(moshpit_ctx *h, const void *dy_dev, int32_t dy_dtype, int64_t dy_row_stride, const int32_t *tokens_dev,
+                       int64_t n_tokens, float scale, int32_t accumulate, void *grad_dev, int64_t grad_row_stride_elems,
+                       int64_t column, int64_t vocab, int64_t width);
+
+/* Activations saved in 8 bits between the forward and the backward pass (the
+ * activations of N peers share one GPU's memory with N states and N gradients).
+ * 32 consecutive elements of a row (fewer at its end) share a power of two 2^e, e
+ * the smallest whole number >= -126 with which all codes x / 2^e, rounded to
+ * nearest, ties to even, lie within -127 .. 127; the scale byte is e + 127.  A code
+ * stands for code * 2^e, which is exact in bfloat16.  A group that holds an
+ * infinity or a NaN gets the scale byte 255 and restores as NaN throughout.
+ * codes_dev: rows * width bytes, scales_dev: rows * ceil(width / 32) bytes, both
+ * row-major without padding. */
+int moshpit_checkpoint(moshpit_ctx *h, const void *x_dev, int32_t dtype, int64_t rows, int64_t width, int64_t row_stride,
+                       int8_t *codes_dev, uint8_t *scales_dev);
+int moshpit_checkpoint_restore(moshpit_ctx *h, const int8_t *codes_dev, const uint8_t *scales_dev, int64_t rows, int64_t width,
+                               void *out_dev, int32_t dtype, int64_t row_stride);
+
+/* The gradient of a linear layer's weights from the layer's saved input x (N *
+ * n_tokens rows of `ins` in the form above) and its output's gradient dy:
+ *   grad_i[o][c] = sum over t of dy[i][t][o] * x[i][t][c],
+ * [outs][ins] from `column` of peer i's row of grad_dev on; accumulate != 0 adds to
+ * what is there. */
+int moshpit_weight_grad(moshpit_ctx *h, const void *dy_dev, int32_t dy_dtype, int64_t dy_row_stride, const int8_t *codes_dev,
+                        const uint8_t *scales_dev, int64_t n_tokens, int64_t outs, int64_t ins, int32_t accumulate, void *grad_dev,
+                        int64_t grad_row_stride_elems, int64_t column);
+
+/* Log-probabilities of given tokens: logp[i][t] = z[token] - log sum_j exp z[j], z the
+ * row of `vocab` logits; 0 where there is no token. */
+int moshpit_token_logp(moshpit_ctx *h, const void *logits_dev, int32_t dtype, int64_t logits_row_stride, const int32_t *tokens_dev,
+                       int64_t n_tokens, int64_t vocab, float *logp_dev);
+
+/* The clipped policy loss with a KL term and its gradient.  With lp as above, A the
+ * advantage, w the weight of the place, r = exp(lp - old_logp) and
+ * k = exp(ref_logp - lp) - (ref_logp - lp) - 1:
+ *   loss_i  = sum over t of w * (kl_coef * k - min(A r, A clip(r, 1 - clip_low, 1 + clip_high)))
+ *   grad[i][t][j] = d loss_i / d z[i][t][j], the unclipped branch where both are equal.
+ * The caller's weights hold the mask and the mean (1 / number of tokens, for
+ * instance).  Places with weight 0 or without a token are not read: gradient and lp
+ * are 0 there, whatever the logits hold.  Logits of -inf (excluded tokens) have
+ * probability and gradient 0; a row of nothing else gives NaN.
+ * ref_logp_dev may be NULL when kl_coef is 0.  grad_dev: laid out like the logits and
+ * of their type; it may be the logits themselves (same row stride) but must not
+ * overlap them in any other way.  logp_dev: [N][n_tokens] floats.  stats_dev: [N][3]
+ * floats: loss_i, sum of w k, sum of the weights whose ratio was clipped. */
+int moshpit_policy_loss(moshpit_ctx *h, const void *logits_dev, int32_t dtype, int64_t logits_row_stride, const int32_t *tokens_dev,
+                        int64_t n_tokens, int64_t vocab, const float *old_logp_dev, const float *ref_logp_dev,
+                        const float *advantage_dev, const float *weight_dev, float clip_low, float clip_high, float kl_coef,
+                        void *grad_dev, int64_t grad_row_stride, float *logp_dev, float *stats_dev);
+
 /* Measurement aids (no counterpart in the paper).
  *
  * moshpit_set_tuning overrides the launch shape of the averaging kernel:

@@ -24,6 +24,8 @@ EXPORTS = [
     "moshpit_create", "moshpit_destroy", "moshpit_bind_state", "moshpit_round", "moshpit_round_dev",
     "moshpit_run", "moshpit_dist_to_mean", "moshpit_dist_to_mean_static", "moshpit_dist_to_mean_subset", "moshpit_group_keys", "moshpit_schedule_mask",
     "moshpit_dynamic_reset", "moshpit_dynamic_round", "moshpit_dynamic_keys", "moshpit_local_step", "moshpit_sgd_round", "moshpit_sgd_run", "moshpit_random_groups_round", "moshpit_random_permutation", "moshpit_refresh", "moshpit_refresh_donors", "moshpit_grouped_round", "moshpit_set_tuning", "moshpit_copy_probe", "moshpit_check_bf16_rounding", "moshpit_sync", "moshpit_last_error",
+    "moshpit_embed", "moshpit_embed_grad", "moshpit_checkpoint", "moshpit_checkpoint_restore", "moshpit_weight_grad", "moshpit_token_logp",
+    "moshpit_policy_loss",
 ]
 
 
@@ -85,6 +87,14 @@ def load_library() -> ctypes.CDLL:
     lib.moshpit_set_tuning.argtypes = [vp, i32, i32, i32, i32, i32, i32]
     lib.moshpit_copy_probe.argtypes = [vp, vp, i64, vp]
     lib.moshpit_check_bf16_rounding.argtypes = [vp, vp]
+    f32 = ctypes.c_float
+    lib.moshpit_embed.argtypes = [vp, i64, i64, i64, vp, i64, f32, vp, i32, i64]
+    lib.moshpit_embed_grad.argtypes = [vp, vp, i32, i64, vp, i64, f32, i32, vp, i64, i64, i64, i64]
+    lib.moshpit_checkpoint.argtypes = [vp, vp, i32, i64, i64, i64, vp, vp]
+    lib.moshpit_checkpoint_restore.argtypes = [vp, vp, vp, i64, i64, vp, i32, i64]
+    lib.moshpit_weight_grad.argtypes = [vp, vp, i32, i64, vp, vp, i64, i64, i64, i32, vp, i64, i64]
+    lib.moshpit_token_logp.argtypes = [vp, vp, i32, i64, vp, i64, i64, vp]
+    lib.moshpit_policy_loss.argtypes = [vp, vp, i32, i64, vp, i64, i64, vp, vp, vp, vp, f32, f32, f32, vp, i64, vp, vp]
     lib.moshpit_sync.argtypes = [vp]
     lib.moshpit_last_error.argtypes = [vp]
     lib.moshpit_last_error.restype = ctypes.c_char_p
@@ -308,6 +318,131 @@ class Moshpit:
                    waves_per_cu: int = 0, order: int = -1) -> None:
         self._check(self._lib.moshpit_set_tuning(self._h, cols, unroll, nontemporal, block, waves_per_cu, order),
                     "set_tuning")
+
+    # -- the local step of language-model peers --------------------------------
+    def _type_code(self, dtype) -> int:
+        import torch
+        if dtype == torch.float32:
+            return F32
+        if dtype == torch.bfloat16:
+            return BF16
+        raise ValueError("activations must be float32 or bfloat16")
+
+    def _rows(self, x, name: str, T: int | None = None):
+        """x: [N, T, width] on the GPU, unit column stride, row i * T + t at a constant stride.
+        Returns (pointer, type code, T, width, row stride)."""
+        if x.dim() != 3 or x.shape[0] != self.N or not x.is_cuda or (T is not None and x.shape[1] != T):
+            raise ValueError(f"{name} must be a GPU tensor [N, {'T' if T is None else T}, width]")
+        _, n, width = x.shape
+        peer, row, col = x.stride()
+        if width > 1 and col != 1:
+            raise ValueError(f"{name} must have unit column stride")
+        stride = row if n > 1 else (peer if peer >= width else width)
+        if n > 1 and peer != n * row or stride < width:
+            raise ValueError(f"rows of {name} must lie at one constant distance over all peers and tokens")
+        return x.data_ptr(), self._type_code(x.dtype), n, width, stride
+
+    def _tokens(self, tokens):
+        """tokens: int32 [N, T] on the GPU, contiguous."""
+        import torch
+        if tokens.dtype != torch.int32 or tokens.dim() != 2 or tokens.shape[0] != self.N or not tokens.is_cuda or not tokens.is_contiguous():
+            raise ValueError("tokens must be a contiguous int32 GPU tensor [N, T]")
+        return tokens.data_ptr(), tokens.shape[1]
+
+    def _per_token(self, x, T: int, name: str):
+        import torch
+        if x.dtype != torch.float32 or tuple(x.shape) != (self.N, T) or not x.is_cuda or not x.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous float32 GPU tensor [N, {T}]")
+        return x.data_ptr()
+
+    def embed(self, tokens, column: int, vocab: int, width: int, scale: float = 1.0, out=None, dtype=None):
+        """Token embeddings [N, T, width] from the tables [vocab, width] that start at parameter `column` of
+        every peer.  out: tensor to write; without it a new one of `dtype` (the state's if not given)."""
+        import torch
+        tp, T = self._tokens(tokens)
+        if out is None:
+            dtype = dtype or (torch.float32 if self.dtype == F32 else torch.bfloat16)
+            out = torch.empty((self.N, T, width), dtype=dtype, device=tokens.device)
+        op, code, _, w, stride = self._rows(out, "out", T)
+        if w != width:
+            raise ValueError("out must be [N, T, width]")
+        self._check(self._lib.moshpit_embed(self._h, column, vocab, width, tp, T, scale, op, code, stride), "embed")
+        return out
+
+    def embed_grad(self, dY, tokens, G, column: int, vocab: int, scale: float = 1.0, accumulate: bool = False) -> None:
+        """Gradient of the tables for dY [N, T, width], into columns column.. of the gradient matrix G."""
+        tp, T = self._tokens(tokens)
+        yp, code, _, width, stride = self._rows(dY, "dY", T)
+        gp, gs = self._grad(G)
+        self._check(self._lib.moshpit_embed_grad(self._h, yp, code, stride, tp, T, scale, int(accumulate), gp, gs, column, vocab, width),
+                    "embed_grad")
+
+    def checkpoint(self, x):
+        """x [N, T, width] in 8 bits: (codes int8 [N, T, width], scales uint8 [N, T, ceil(width / 32)])."""
+        import torch
+        xp, code, T, width, stride = self._rows(x, "x")
+        codes = torch.empty((self.N, T, width), dtype=torch.int8, device=x.device)
+        scales = torch.empty((self.N, T, -(-width // 32)), dtype=torch.uint8, device=x.device)
+        self._check(self._lib.moshpit_checkpoint(self._h, xp, code, self.N * T, width, stride, codes.data_ptr(), scales.data_ptr()),
+                    "checkpoint")
+        return codes, scales
+
+    def _saved(self, codes, scales):
+        import torch
+        if codes.dtype != torch.int8 or scales.dtype != torch.uint8 or codes.dim() != 3 or codes.shape[0] != self.N or \
+                tuple(scales.shape) != (*codes.shape[:2], -(-codes.shape[2] // 32)) or not codes.is_cuda or not scales.is_cuda or \
+                not codes.is_contiguous() or not scales.is_contiguous():
+            raise ValueError("codes and scales must be what checkpoint() returned")
+        return codes.data_ptr(), scales.data_ptr()
+
+    def checkpoint_restore(self, codes, scales, dtype=None, out=None):
+        """The activations that codes and scales stand for, in `dtype` (float32 if not given) or into `out`."""
+        import torch
+        cp, sp = self._saved(codes, scales)
+        if out is None:
+            out = torch.empty(codes.shape, dtype=dtype or torch.float32, device=codes.device)
+        op, code, T, width, stride = self._rows(out, "out", codes.shape[1])
+        if width != codes.shape[2]:
+            raise ValueError("out must have the shape of codes")
+        self._check(self._lib.moshpit_checkpoint_restore(self._h, cp, sp, self.N * T, width, op, code, stride), "checkpoint_restore")
+        return out
+
+    def weight_grad(self, dY, codes, scales, G, column: int, accumulate: bool = False) -> None:
+        """Gradient [outs, ins] of a linear layer's weights for dY [N, T, outs] and the saved input [N, T, ins], into
+        columns column.. of the gradient matrix G."""
+        cp, sp = self._saved(codes, scales)
+        yp, code, T, outs, stride = self._rows(dY, "dY", codes.shape[1])
+        gp, gs = self._grad(G)
+        self._check(self._lib.moshpit_weight_grad(self._h, yp, code, stride, cp, sp, T, outs, codes.shape[2], int(accumulate), gp, gs, column),
+                    "weight_grad")
+
+    def token_logp(self, logits, tokens):
+        """Log-probabilities [N, T] (float32) of `tokens` under logits [N, T, vocab]."""
+        import torch
+        tp, T = self._tokens(tokens)
+        zp, code, _, vocab, stride = self._rows(logits, "logits", T)
+        logp = torch.empty((self.N, T), dtype=torch.float32, device=logits.device)
+        self._check(self._lib.moshpit_token_logp(self._h, zp, code, stride, tp, T, vocab, logp.data_ptr()), "token_logp")
+        return logp
+
+    def policy_loss(self, logits, tokens, old_logp, advantage, weight, ref_logp=None, clip_low: float = 0.2, clip_high: float = 0.2,
+                    kl_coef: float = 0.0, grad=None):
+        """Clipped policy loss with a KL term: (stats [N, 3] = loss, KL, clipped weight of every peer; logp [N, T]).  The
+        logits' gradient goes into `grad` (like logits; None: into the logits themselves)."""
+        import torch
+        tp, T = self._tokens(tokens)
+        zp, code, _, vocab, stride = self._rows(logits, "logits", T)
+        grad = logits if grad is None else grad
+        dp, dcode, _, dvocab, dstride = self._rows(grad, "grad", T)
+        if dcode != code or dvocab != vocab:
+            raise ValueError("grad must have the type and shape of logits")
+        old, adv, w = self._per_token(old_logp, T, "old_logp"), self._per_token(advantage, T, "advantage"), self._per_token(weight, T, "weight")
+        ref = None if ref_logp is None else self._per_token(ref_logp, T, "ref_logp")
+        logp = torch.empty((self.N, T), dtype=torch.float32, device=logits.device)
+        stats = torch.empty((self.N, 3), dtype=torch.float32, device=logits.device)
+        self._check(self._lib.moshpit_policy_loss(self._h, zp, code, stride, tp, T, vocab, old, ref, adv, w, clip_low, clip_high, kl_coef, dp,
+                                                  dstride, logp.data_ptr(), stats.data_ptr()), "policy_loss")
+        return stats, logp
 
     def sync(self) -> None:
         self._check(self._lib.moshpit_sync(self._h), "sync")

@@ -8,6 +8,7 @@
 #include <vector>
 
 #include "../../include/moshpit.h"
+#include "local_ops.h"
 #include "moshpit_internal.h"
 #include "pass_rules.h"
 
@@ -42,6 +43,8 @@ struct moshpit_ctx {
     int64_t partials_cap = 0;
     double *d_dist = nullptr;          // dist_cap doubles
     int64_t dist_cap = 0;
+    void *d_work = nullptr;            // workspace of the local step's operators: work_cap bytes
+    int64_t work_cap = 0;
     std::vector<hipEvent_t> events;    // 2 per timed round
 
     // Host bytes on their way to the device (masks, peer lists): copied out of the caller's
@@ -521,6 +524,7 @@ int moshpit_destroy(moshpit_ctx *h)
     if (h->d_grid) (void)hipFree(h->d_grid);
     if (h->d_grid_partials) (void)hipFree(h->d_grid_partials);
     if (h->d_dist) (void)hipFree(h->d_dist);
+    if (h->d_work) (void)hipFree(h->d_work);
     delete h;
     return MOSHPIT_OK;
 }
@@ -1281,6 +1285,217 @@ int moshpit_schedule_mask(moshpit_ctx *h, const moshpit_schedule *s, int64_t t0,
     HIP_TRY(h, hipMemcpyAsync(masks_host, h->d_masks, static_cast<size_t>(rounds) * h->N, hipMemcpyDeviceToHost,
                               h->stream));
     HIP_TRY(h, hipStreamSynchronize(h->stream));
+    return MOSHPIT_OK;
+}
+
+namespace {
+
+// Largest token, row and column counts the operators of the local step take: places, rows of a grid and
+// column slices are 32-bit numbers in their kernels.
+constexpr int64_t kMostTokens = int64_t(1) << 30, kMostRows = int64_t(1) << 31, kMostWidth = int64_t(1) << 23;
+
+int reserve_work(moshpit_ctx *h, int64_t bytes)
+{
+    if (bytes <= h->work_cap) return MOSHPIT_OK;
+    if (h->d_work) {
+        HIP_TRY(h, hipStreamSynchronize(h->stream));
+        HIP_TRY(h, hipFree(h->d_work));
+        h->d_work = nullptr;
+        h->work_cap = 0;
+    }
+    HIP_TRY(h, hipMalloc(&h->d_work, static_cast<size_t>(bytes)));
+    h->work_cap = bytes;
+    return MOSHPIT_OK;
+}
+
+int check_dtype(moshpit_ctx *h, const char *what, int32_t dtype)
+{
+    if (dtype == MOSHPIT_F32 || dtype == MOSHPIT_BF16) return MOSHPIT_OK;
+    return fail(h, MOSHPIT_EINVAL, "%s: unknown dtype %d", what, dtype);
+}
+
+// A matrix of activations or logits: `rows` rows of `width` elements.
+int check_matrix(moshpit_ctx *h, const char *what, const void *dev, int32_t dtype, int64_t rows, int64_t width, int64_t row_stride)
+{
+    int rc = check_dtype(h, what, dtype);
+    if (rc != MOSHPIT_OK) return rc;
+    if (rows > 0 && !dev) return fail(h, MOSHPIT_EINVAL, "%s: pointer is NULL", what);
+    if (reinterpret_cast<uintptr_t>(dev) % (dtype == MOSHPIT_F32 ? 4 : 2) != 0)
+        return fail(h, MOSHPIT_EINVAL, "%s: pointer is not aligned to the element size", what);
+    if (row_stride < width || row_stride > (int64_t(1) << 40))
+        return fail(h, MOSHPIT_EINVAL, "%s: row stride %lld for rows of %lld", what, (long long)row_stride, (long long)width);
+    return MOSHPIT_OK;
+}
+
+// An array of 4-byte values.
+int check_words(moshpit_ctx *h, const char *what, const void *dev, int64_t count)
+{
+    if (count > 0 && !dev) return fail(h, MOSHPIT_EINVAL, "%s: pointer is NULL", what);
+    if (reinterpret_cast<uintptr_t>(dev) % 4 != 0) return fail(h, MOSHPIT_EINVAL, "%s: pointer is not aligned to 4 bytes", what);
+    return MOSHPIT_OK;
+}
+
+int check_tokens(moshpit_ctx *h, int64_t n_tokens)
+{
+    if (n_tokens < 0 || n_tokens > kMostTokens || h->N * n_tokens > kMostRows - 1)
+        return fail(h, MOSHPIT_EINVAL, "%lld tokens a peer: at least 0, at most 2^30 and 2^31 - 1 of all peers", (long long)n_tokens);
+    return MOSHPIT_OK;
+}
+
+// Parameters column .. column + rows * width - 1 of a peer.
+int check_params(moshpit_ctx *h, int64_t column, int64_t rows, int64_t width)
+{
+    if (rows < 1 || width < 1 || rows > 0x7ffffffe || width > kMostWidth)
+        return fail(h, MOSHPIT_EINVAL, "%lld rows of %lld parameters: at least 1, at most 2^31 - 2 rows of 2^23", (long long)rows, (long long)width);
+    if (column < 0 || column > h->P || rows > (h->P - column) / width)
+        return fail(h, MOSHPIT_EINVAL, "%lld x %lld parameters from %lld on do not fit into P = %lld", (long long)rows, (long long)width,
+                    (long long)column, (long long)h->P);
+    return MOSHPIT_OK;
+}
+
+int64_t elem_bytes(int32_t dtype) { return dtype == MOSHPIT_F32 ? 4 : 2; }
+
+#define CHECK(call)                              \
+    do {                                         \
+        const int rc_ = (call);                  \
+        if (rc_ != MOSHPIT_OK) return rc_;       \
+    } while (0)
+
+}  // namespace
+
+int moshpit_embed(moshpit_ctx *h, int64_t column, int64_t vocab, int64_t width, const int32_t *tokens_dev, int64_t n_tokens,
+                  float scale, void *out_dev, int32_t out_dtype, int64_t out_row_stride)
+{
+    CHECK(check_ready(h));
+    CHECK(check_params(h, column, vocab, width));
+    CHECK(check_tokens(h, n_tokens));
+    CHECK(check_words(h, "tokens", tokens_dev, n_tokens));
+    CHECK(check_matrix(h, "output", out_dev, out_dtype, n_tokens, width, out_row_stride));
+    const TableGeom g{h->N, h->row_stride, vocab, width, n_tokens};
+    HIP_TRY(h, launch_embed(static_cast<const char *>(h->X) + column * elem_bytes(h->dtype), h->dtype, g, tokens_dev, scale, out_dev,
+                            out_dtype, out_row_stride, h->stream));
+    return MOSHPIT_OK;
+}
+
+int moshpit_embed_grad(moshpit_ctx *h, const void *dy_dev, int32_t dy_dtype, int64_t dy_row_stride, const int32_t *tokens_dev,
+                       int64_t n_tokens, float scale, int32_t accumulate, void *grad_dev, int64_t grad_row_stride_elems,
+                       int64_t column, int64_t vocab, int64_t width)
+{
+    CHECK(check_ready(h));
+    CHECK(check_params(h, column, vocab, width));
+    CHECK(check_tokens(h, n_tokens));
+    CHECK(check_words(h, "tokens", tokens_dev, n_tokens));
+    CHECK(check_matrix(h, "output's gradient", dy_dev, dy_dtype, n_tokens, width, dy_row_stride));
+    CHECK(check_grad(h, grad_dev, grad_row_stride_elems));
+    const TableGeom g{h->N, grad_row_stride_elems, vocab, width, n_tokens};
+    if (!embed_grad_fits(g)) return fail(h, MOSHPIT_EINVAL, "%lld tables of %lld rows are too many for one call", (long long)h->N, (long long)vocab);
+    CHECK(reserve_work(h, embed_grad_work_bytes(g)));
+    HIP_TRY(h, launch_embed_grad(static_cast<char *>(grad_dev) + column * elem_bytes(h->dtype), h->dtype, g, tokens_dev, scale, dy_dev,
+                                 dy_dtype, dy_row_stride, accumulate != 0, h->d_work, h->stream));
+    return MOSHPIT_OK;
+}
+
+namespace {
+int check_codes(moshpit_ctx *h, const int8_t *codes_dev, const uint8_t *scales_dev, int64_t rows, int64_t width)
+{
+    if (rows < 0 || rows >= kMostRows || width < 1 || width > kMostWidth || rows * ((width + 31) / 32) > (int64_t(1) << 38))
+        return fail(h, MOSHPIT_EINVAL, "%lld rows of %lld: at most 2^31 - 1 rows of 1 .. 2^23, 2^38 groups of 32", (long long)rows, (long long)width);
+    if (rows > 0 && (!codes_dev || !scales_dev)) return fail(h, MOSHPIT_EINVAL, "codes or scales: pointer is NULL");
+    return MOSHPIT_OK;
+}
+}  // namespace
+
+int moshpit_checkpoint(moshpit_ctx *h, const void *x_dev, int32_t dtype, int64_t rows, int64_t width, int64_t row_stride,
+                       int8_t *codes_dev, uint8_t *scales_dev)
+{
+    CHECK(check_ready(h));
+    CHECK(check_codes(h, codes_dev, scales_dev, rows, width));
+    CHECK(check_matrix(h, "activations", x_dev, dtype, rows, width, row_stride));
+    HIP_TRY(h, launch_checkpoint(x_dev, dtype, rows, width, row_stride, codes_dev, scales_dev, h->stream));
+    return MOSHPIT_OK;
+}
+
+int moshpit_checkpoint_restore(moshpit_ctx *h, const int8_t *codes_dev, const uint8_t *scales_dev, int64_t rows, int64_t width,
+                               void *out_dev, int32_t dtype, int64_t row_stride)
+{
+    CHECK(check_ready(h));
+    CHECK(check_codes(h, codes_dev, scales_dev, rows, width));
+    CHECK(check_matrix(h, "output", out_dev, dtype, rows, width, row_stride));
+    HIP_TRY(h, launch_checkpoint_restore(codes_dev, scales_dev, rows, width, out_dev, dtype, row_stride, h->stream));
+    return MOSHPIT_OK;
+}
+
+int moshpit_weight_grad(moshpit_ctx *h, const void *dy_dev, int32_t dy_dtype, int64_t dy_row_stride, const int8_t *codes_dev,
+                        const uint8_t *scales_dev, int64_t n_tokens, int64_t outs, int64_t ins, int32_t accumulate, void *grad_dev,
+                        int64_t grad_row_stride_elems, int64_t column)
+{
+    CHECK(check_ready(h));
+    CHECK(check_params(h, column, outs, ins));
+    if (outs > kMostWidth) return fail(h, MOSHPIT_EINVAL, "%lld outputs: at most 2^23", (long long)outs);
+    CHECK(check_tokens(h, n_tokens));
+    CHECK(check_codes(h, codes_dev, scales_dev, h->N * n_tokens, ins));
+    CHECK(check_matrix(h, "output's gradient", dy_dev, dy_dtype, n_tokens, outs, dy_row_stride));
+    CHECK(check_grad(h, grad_dev, grad_row_stride_elems));
+    int compute_units = 0;
+    HIP_TRY(h, current_compute_units(&compute_units));
+    const WeightGradGeom g{h->N, n_tokens, outs, ins, dy_row_stride, grad_row_stride_elems};
+    if (!weight_grad_fits(g)) return fail(h, MOSHPIT_EINVAL, "%lld matrices of %lld x %lld are too many for one call", (long long)h->N, (long long)outs, (long long)ins);
+    CHECK(reserve_work(h, weight_grad_work_bytes(g, dy_dtype, compute_units)));
+    HIP_TRY(h, launch_weight_grad(dy_dev, dy_dtype, codes_dev, scales_dev, g, static_cast<char *>(grad_dev) + column * elem_bytes(h->dtype),
+                                  h->dtype, accumulate != 0, h->d_work, compute_units, h->stream));
+    return MOSHPIT_OK;
+}
+
+namespace {
+int check_logits(moshpit_ctx *h, const void *logits_dev, int32_t dtype, int64_t row_stride, const int32_t *tokens_dev, int64_t n_tokens,
+                 int64_t vocab)
+{
+    if (vocab < 1 || vocab > (int64_t(1) << 27)) return fail(h, MOSHPIT_EINVAL, "a vocabulary of %lld: 1 .. 2^27", (long long)vocab);
+    CHECK(check_tokens(h, n_tokens));
+    CHECK(check_words(h, "tokens", tokens_dev, n_tokens));
+    return check_matrix(h, "logits", logits_dev, dtype, n_tokens, vocab, row_stride);
+}
+}  // namespace
+
+int moshpit_token_logp(moshpit_ctx *h, const void *logits_dev, int32_t dtype, int64_t logits_row_stride, const int32_t *tokens_dev,
+                       int64_t n_tokens, int64_t vocab, float *logp_dev)
+{
+    CHECK(check_ready(h));
+    CHECK(check_logits(h, logits_dev, dtype, logits_row_stride, tokens_dev, n_tokens, vocab));
+    CHECK(check_words(h, "log-probabilities", logp_dev, n_tokens));
+    int compute_units = 0;
+    HIP_TRY(h, current_compute_units(&compute_units));
+    CHECK(reserve_work(h, policy_work_bytes(h->N, n_tokens, vocab, dtype, compute_units)));
+    HIP_TRY(h, launch_token_logp(logits_dev, dtype, h->N * n_tokens, vocab, logits_row_stride, tokens_dev, logp_dev, h->d_work, compute_units,
+                                 h->stream));
+    return MOSHPIT_OK;
+}
+
+int moshpit_policy_loss(moshpit_ctx *h, const void *logits_dev, int32_t dtype, int64_t logits_row_stride, const int32_t *tokens_dev,
+                        int64_t n_tokens, int64_t vocab, const float *old_logp_dev, const float *ref_logp_dev,
+                        const float *advantage_dev, const float *weight_dev, float clip_low, float clip_high, float kl_coef,
+                        void *grad_dev, int64_t grad_row_stride, float *logp_dev, float *stats_dev)
+{
+    CHECK(check_ready(h));
+    CHECK(check_logits(h, logits_dev, dtype, logits_row_stride, tokens_dev, n_tokens, vocab));
+    CHECK(check_words(h, "old log-probabilities", old_logp_dev, n_tokens));
+    CHECK(check_words(h, "reference log-probabilities", ref_logp_dev, 0));
+    CHECK(check_words(h, "advantages", advantage_dev, n_tokens));
+    CHECK(check_words(h, "weights", weight_dev, n_tokens));
+    CHECK(check_words(h, "log-probabilities", logp_dev, n_tokens));
+    CHECK(check_words(h, "statistics", stats_dev, 1));
+    CHECK(check_matrix(h, "logits' gradient", grad_dev, dtype, n_tokens, vocab, grad_row_stride));
+    if (!(clip_low >= 0.f) || !(clip_high >= 0.f)) return fail(h, MOSHPIT_EINVAL, "the clip range must be >= 0 on both sides");
+    if (!std::isfinite(kl_coef)) return fail(h, MOSHPIT_EINVAL, "the KL coefficient must be finite");
+    if (kl_coef != 0.f && !ref_logp_dev && n_tokens > 0) return fail(h, MOSHPIT_EINVAL, "a KL term needs the reference log-probabilities");
+    if (grad_dev == logits_dev && grad_row_stride != logits_row_stride)
+        return fail(h, MOSHPIT_EINVAL, "the gradient can take the logits' place only with the logits' row stride");
+    int compute_units = 0;
+    HIP_TRY(h, current_compute_units(&compute_units));
+    CHECK(reserve_work(h, policy_work_bytes(h->N, n_tokens, vocab, dtype, compute_units)));
+    const PolicyTerms p{old_logp_dev, ref_logp_dev, advantage_dev, weight_dev, clip_low, clip_high, kl_coef};
+    HIP_TRY(h, launch_policy_loss(logits_dev, dtype, h->N, n_tokens, vocab, logits_row_stride, tokens_dev, p, grad_dev, grad_row_stride, logp_dev,
+                                  stats_dev, h->d_work, compute_units, h->stream));
     return MOSHPIT_OK;
 }
 

@@ -1,0 +1,453 @@
+// The clipped policy loss with a KL term, from logits, and the logits' gradient, for gfx950.  For a row z of
+// logits, its token a and weight w:
+//   lp = z_a - log sum_j exp z_j,  r = exp(lp - old),  k = exp(ref - lp) - (ref - lp) - 1
+//   loss = w * (kl_coef * k - min(A r, A clip(r, 1 - clip_low, 1 + clip_high)))
+//   d loss / d lp = s = w * (kl_coef * (1 - exp(ref - lp)) - [A r <= A clip(r)] A r)
+//   d loss / d z_j = s * ([j = a] - exp(z_j - m) / sum exp(z - m)),   m = max z
+// in binary32 throughout, the gradient rounded once.  A row without weight or token is not read: its gradient
+// and log-probability are zeros.
+//
+// Bound by HBM: a row is read once and its gradient written once, so a block holds a whole row in registers
+// (kVecs vectors of 16 bytes a thread) from the first pass (largest element and sum of exponentials, by thread,
+// wave and block) to the second (gradient).  Rows that do not fit, and few rows, are cut into slices: a first
+// kernel leaves (largest, sum) of every slice, a second joins them and writes the gradient, its second
+// read of the logits coming from the caches where they are small.
+#include <hip/hip_runtime.h>
+
+#include "local_ops.h"
+#include "row_elems.h"
+
+namespace moshpit {
+namespace {
+
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+// exp(x - m), m finite or x = m = -inf excluded by the caller
+__device__ __forceinline__ float exp_above(float x, float m) { return __builtin_amdgcn_exp2f((x - m) * kLog2e); }
+
+// The largest element of a set and the sum of exp(x - largest) over it; {-inf, 0} of nothing.
+struct TopSum {
+    float top, sum;
+};
+__device__ __forceinline__ TopSum join(const TopSum &a, const TopSum &b)
+{
+    const float top = fmaxf(a.top, b.top);
+    // a set whose largest element is -inf has the sum 0 (nothing) or its number of elements (all -inf): exp(-inf - top) = 0
+    // counts neither where the other one is finite, and where both are -inf the sums add as they are
+    const float fa = a.top == top ? 1.f : exp_above(a.top, top), fb = b.top == top ? 1.f : exp_above(b.top, top);
+    // (a NaN anywhere stays in the sum: fmaxf drops it from the tops)
+    return {top, a.sum * fa + b.sum * fb};
+}
+
+template <int THREADS>
+__device__ __forceinline__ TopSum block_join(TopSum t)
+{
+    constexpr int WAVES = THREADS / 64;
+    __shared__ TopSum of_wave[WAVES];
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) t = join(t, TopSum{__shfl_xor(t.top, off, 64), __shfl_xor(t.sum, off, 64)});
+    if constexpr (WAVES > 1) {
+        if ((threadIdx.x & 63) == 0) of_wave[threadIdx.x >> 6] = t;
+        __syncthreads();
+        t = of_wave[0];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) t = join(t, of_wave[w]);
+    }
+    return t;
+}
+
+// Elements [begin, end) of a row as whole vectors at 16-byte boundaries and up to 2 (VE - 1) single elements
+// around them.
+template <int DT> struct Slice {
+    static constexpr int ES = DT == 0 ? 4 : 2, VE = 16 / ES;
+    const char *vectors;                 // the first whole vector
+    int32_t count;                       // whole vectors
+    int32_t head, tail;                  // single elements before and after them
+    __device__ __forceinline__ Slice(const char *from, int64_t n)
+    {
+        const uint32_t phase = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(from)) % 16 / ES;
+        head = phase ? VE - static_cast<int32_t>(phase) : 0;
+        if (head > n) head = static_cast<int32_t>(n);
+        vectors = from + head * ES;
+        count = static_cast<int32_t>((n - head) / VE);
+        tail = static_cast<int32_t>(n - head - int64_t(count) * VE);
+    }
+    // element of single number k, 0 <= k < head + tail, from the slice's first one on
+    __device__ __forceinline__ int64_t single(int k) const { return k < head ? k : int64_t(count) * VE + k; }
+};
+
+template <int DT> __device__ __forceinline__ void widen_vec(const u32x4 &m, float (&f)[16 / (DT == 0 ? 4 : 2)])
+{
+    if constexpr (DT == 0) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) f[k] = __uint_as_float(m[k]);
+    } else Vec<1, 8>::widen(m, f);
+}
+
+template <int VE> __device__ __forceinline__ void add_values(TopSum &t, const float (&f)[VE])
+{
+    float top = f[0];
+#pragma unroll
+    for (int k = 1; k < VE; ++k) top = fmaxf(top, f[k]);
+    if (top > t.top) {
+        t.sum *= t.top == -INFINITY ? 0.f : exp_above(t.top, top);
+        t.top = top;
+    }
+    const float m = t.top == -INFINITY ? 0.f : t.top;      // (-inf alone: exp(-inf) = 0)
+    float sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < VE; ++k) sum += exp_above(f[k], m);
+    t.sum += sum;
+}
+
+struct RowPlace {
+    int64_t vocab, stride;
+};
+
+// What a row adds to its peer's sums: loss, w k, w [clipped].
+struct RowTerms {
+    float loss, kl, clipped;
+};
+
+// From a row's log-probability: its terms and d loss / d lp.
+__device__ __forceinline__ float row_terms(const PolicyTerms &p, int64_t row, float w, float lp, RowTerms &terms)
+{
+    const float A = p.advantage[row], r = expf(lp - p.old_logp[row]);
+    const float low = 1.f - p.clip_low, high = 1.f + p.clip_high;
+    const float plain = A * r, cut = A * (r < low ? low : r > high ? high : r);
+    const bool clipped = plain > cut;
+    float k = 0.f, dk = 0.f;
+    if (p.ref_logp) {
+        const float off = p.ref_logp[row] - lp, e = expf(off);
+        k = e - off - 1.f;
+        dk = 1.f - e;
+    }
+    terms.loss = w * (p.kl_coef * k - (clipped ? cut : plain));
+    terms.kl = w * k;
+    terms.clipped = clipped ? w : 0.f;
+    return w * (p.kl_coef * dk - (clipped ? 0.f : plain));
+}
+
+template <int DT, int THREADS>
+__device__ __forceinline__ void store_zeros(char *grad, int64_t n)
+{
+    constexpr int ES = DT == 0 ? 4 : 2;
+    const Slice<DT> s(grad, n);
+    for (int v = threadIdx.x; v < s.count; v += THREADS)
+        store_vec<true, u32x4>(const_cast<char *>(s.vectors) + int64_t(v) * 16, u32x4{0, 0, 0, 0});
+    for (int k = threadIdx.x; k < s.head + s.tail; k += THREADS) store_one<DT>(grad + s.single(k) * ES, 0.f);
+}
+
+// One row a block, in registers.  The gradient may take the logits' place (here and below): every element is read
+// before it is written, by the same thread.
+template <int DT, int THREADS, int VECS>
+__global__ __launch_bounds__(THREADS) void policy_row_kernel(const char *logits, RowPlace at, const int32_t *__restrict__ tokens,
+                                                             PolicyTerms p, char *grad, int64_t grad_stride,
+                                                             float *__restrict__ logp, RowTerms *__restrict__ terms)
+{
+    constexpr int ES = DT == 0 ? 4 : 2, VE = 16 / ES;
+    const int64_t row = blockIdx.x;
+    const float w = p.weight[row];
+    const int64_t token = tokens[row];
+    char *to = grad + row * grad_stride * ES;
+    if (w == 0.f || token < 0 || token >= at.vocab) {
+        store_zeros<DT, THREADS>(to, at.vocab);
+        if (threadIdx.x == 0) {
+            logp[row] = 0.f;
+            terms[row] = RowTerms{0.f, 0.f, 0.f};
+        }
+        return;
+    }
+    const char *from = logits + row * at.stride * ES;
+    const Slice<DT> s(from, at.vocab);
+    const float z_token = load_one<DT>(from + token * ES);
+    u32x4 held[VECS];
+    float single = -INFINITY;
+#pragma unroll
+    for (int v = 0; v < VECS; ++v) {
+        const int32_t i = v * THREADS + threadIdx.x;
+        if (i < s.count) held[v] = load_vec<true, u32x4>(s.vectors + int64_t(i) * 16);
+    }
+    if (static_cast<int32_t>(threadIdx.x) < s.head + s.tail) single = load_one<DT>(from + s.single(threadIdx.x) * ES);
+    TopSum t{single, single == -INFINITY ? 0.f : 1.f};
+#pragma unroll
+    for (int v = 0; v < VECS; ++v) {
+        if (v * THREADS + static_cast<int32_t>(threadIdx.x) >= s.count) continue;
+        float f[VE];
+        widen_vec<DT>(held[v], f);
+        add_values(t, f);
+    }
+    t = block_join<THREADS>(t);
+    const float lp = z_token - t.top - logf(t.sum);
+    RowTerms mine;
+    const float slope = row_terms(p, row, w, lp, mine);
+    if (threadIdx.x == 0) {
+        logp[row] = lp;
+        terms[row] = mine;
+    }
+    const float factor = -slope / t.sum;
+#pragma unroll
+    for (int v = 0; v < VECS; ++v) {
+        const int32_t i = v * THREADS + threadIdx.x;
+        if (i >= s.count) continue;
+        float f[VE];
+        widen_vec<DT>(held[v], f);
+#pragma unroll
+        for (int k = 0; k < VE; ++k) f[k] = factor * exp_above(f[k], t.top);
+        const int64_t e = s.head + int64_t(i) * VE;
+        if (token >= e && token < e + VE) {
+#pragma unroll
+            for (int k = 0; k < VE; ++k)
+                if (token == e + k) f[k] += slope;
+        }
+        store_elems<DT, VE, true>(to + e * ES, f);
+    }
+    if (static_cast<int32_t>(threadIdx.x) < s.head + s.tail) {
+        const int64_t e = s.single(threadIdx.x);
+        store_one<DT>(to + e * ES, factor * exp_above(single, t.top) + (token == e ? slope : 0.f));
+    }
+}
+
+// Rows cut into slices: block b works on slice b % slices of row b / slices.
+struct Cut {
+    int32_t slices;
+    int64_t length;                      // elements of a slice
+};
+
+template <int DT, int THREADS>
+__global__ __launch_bounds__(THREADS) void slice_sum_kernel(const char *__restrict__ logits, RowPlace at, Cut cut, const int32_t *__restrict__ tokens,
+                                                            const float *__restrict__ weight, TopSum *__restrict__ sums, float *__restrict__ z_token,
+                                                            float *__restrict__ logp)
+{
+    constexpr int ES = DT == 0 ? 4 : 2, VE = 16 / ES, kBatch = 8;
+    const int64_t row = blockIdx.x / static_cast<uint32_t>(cut.slices);
+    const int32_t slice = blockIdx.x % static_cast<uint32_t>(cut.slices);
+    const int64_t token = tokens[row];
+    const bool live = (!weight || weight[row] != 0.f) && token >= 0 && token < at.vocab;
+    if (!live) {
+        if (logp && slice == 0 && threadIdx.x == 0) logp[row] = 0.f;
+        return;
+    }
+    const int64_t begin = slice * cut.length, end = begin + cut.length < at.vocab ? begin + cut.length : at.vocab;
+    const char *from = logits + (row * at.stride + begin) * ES;
+    const Slice<DT> s(from, end - begin);
+    TopSum t{-INFINITY, 0.f};
+    for (int k = threadIdx.x; k < s.head + s.tail; k += THREADS) t = join(t, TopSum{load_one<DT>(from + s.single(k) * ES), 1.f});
+    for (int32_t i0 = threadIdx.x; i0 < s.count; i0 += THREADS * kBatch) {
+        u32x4 m[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u)
+            if (i0 + u * THREADS < s.count) m[u] = load_vec<false, u32x4>(s.vectors + int64_t(i0 + u * THREADS) * 16);
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            if (i0 + u * THREADS >= s.count) continue;
+            float f[VE];
+            widen_vec<DT>(m[u], f);
+            add_values(t, f);
+        }
+    }
+    t = block_join<THREADS>(t);
+    if (threadIdx.x != 0) return;
+    if (!z_token) {
+        logp[row] = load_one<DT>(logits + (row * at.stride + token) * ES) - t.top - logf(t.sum);
+        return;
+    }
+    sums[blockIdx.x] = t;
+    if (slice == 0) z_token[row] = load_one<DT>(logits + (row * at.stride + token) * ES);
+}
+
+// The slices of a row joined, by a wave.
+__device__ __forceinline__ TopSum joined(const TopSum *__restrict__ sums, int32_t slices)
+{
+    TopSum t{-INFINITY, 0.f};
+    for (int32_t k = threadIdx.x & 63; k < slices; k += 64) t = join(t, sums[k]);
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) t = join(t, TopSum{__shfl_xor(t.top, off, 64), __shfl_xor(t.sum, off, 64)});
+    return t;
+}
+
+template <int DT, int THREADS>
+__global__ __launch_bounds__(THREADS) void policy_slice_kernel(const char *logits, RowPlace at, Cut cut, const int32_t *__restrict__ tokens,
+                                                               PolicyTerms p, const TopSum *__restrict__ sums, const float *__restrict__ z_token, char *grad, int64_t grad_stride,
+                                                               float *__restrict__ logp, RowTerms *__restrict__ terms)
+{
+    constexpr int ES = DT == 0 ? 4 : 2, VE = 16 / ES, kBatch = 4;
+    const int64_t row = blockIdx.x / static_cast<uint32_t>(cut.slices);
+    const int32_t slice = blockIdx.x % static_cast<uint32_t>(cut.slices);
+    const float w = p.weight[row];
+    const int64_t token = tokens[row];
+    const int64_t begin = slice * cut.length, end = begin + cut.length < at.vocab ? begin + cut.length : at.vocab;
+    char *to = grad + (row * grad_stride + begin) * ES;
+    if (w == 0.f || token < 0 || token >= at.vocab) {
+        store_zeros<DT, THREADS>(to, end - begin);
+        if (slice == 0 && threadIdx.x == 0) {
+            logp[row] = 0.f;
+            terms[row] = RowTerms{0.f, 0.f, 0.f};
+        }
+        return;
+    }
+    const TopSum t = joined(sums + row * cut.slices, cut.slices);
+    const float lp = z_token[row] - t.top - logf(t.sum);             // (kept aside: another block's gradient may be in the logit's place by now)
+    RowTerms mine;
+    const float slope = row_terms(p, row, w, lp, mine);
+    if (slice == 0 && threadIdx.x == 0) {
+        logp[row] = lp;
+        terms[row] = mine;
+    }
+    const float factor = -slope / t.sum;
+    const char *from = logits + (row * at.stride + begin) * ES;
+    const Slice<DT> s(from, end - begin);
+    for (int32_t i0 = threadIdx.x; i0 < s.count; i0 += THREADS * kBatch) {
+        u32x4 m[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u)
+            if (i0 + u * THREADS < s.count) m[u] = load_vec<false, u32x4>(s.vectors + int64_t(i0 + u * THREADS) * 16);
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const int32_t i = i0 + u * THREADS;
+            if (i >= s.count) continue;
+            float f[VE];
+            widen_vec<DT>(m[u], f);
+            const int64_t e = s.head + int64_t(i) * VE;
+#pragma unroll
+            for (int k = 0; k < VE; ++k) f[k] = factor * exp_above(f[k], t.top) + (token == begin + e + k ? slope : 0.f);
+            store_elems<DT, VE, true>(to + e * ES, f);
+        }
+    }
+    for (int k = threadIdx.x; k < s.head + s.tail; k += THREADS) {
+        const int64_t e = s.single(k);
+        store_one<DT>(to + e * ES, factor * exp_above(load_one<DT>(from + e * ES), t.top) + (token == begin + e ? slope : 0.f));
+    }
+}
+
+__global__ __launch_bounds__(64) void logp_join_kernel(const TopSum *__restrict__ sums, const float *__restrict__ z_token, int32_t slices,
+                                                       const int32_t *__restrict__ tokens, int64_t vocab, float *__restrict__ logp)
+{
+    const int64_t row = blockIdx.x, token = tokens[row];
+    if (token < 0 || token >= vocab) return;                         // (written by the kernel before)
+    const TopSum t = joined(sums + row * slices, slices);
+    if (threadIdx.x == 0) logp[row] = z_token[row] - t.top - logf(t.sum);
+}
+
+// The terms of a peer's rows, summed in binary64 in an order that depends on T alone.
+__global__ __launch_bounds__(256) void policy_stats_kernel(const RowTerms *__restrict__ terms, int64_t T, float *__restrict__ stats)
+{
+    __shared__ double of_wave[4][3];
+    const RowTerms *mine = terms + int64_t(blockIdx.x) * T;
+    double sum[3] = {0.0, 0.0, 0.0};
+    for (int64_t t = threadIdx.x; t < T; t += 256) {
+        const RowTerms v = mine[t];
+        sum[0] += v.loss;
+        sum[1] += v.kl;
+        sum[2] += v.clipped;
+    }
+#pragma unroll
+    for (int q = 0; q < 3; ++q) {
+#pragma unroll
+        for (int off = 32; off > 0; off >>= 1) sum[q] += __shfl_down(sum[q], off, 64);
+        if ((threadIdx.x & 63) == 0) of_wave[threadIdx.x >> 6][q] = sum[q];
+    }
+    __syncthreads();
+    if (threadIdx.x < 3) {
+        const int q = threadIdx.x;
+        stats[int64_t(blockIdx.x) * 3 + q] = static_cast<float>((of_wave[0][q] + of_wave[1][q]) + (of_wave[2][q] + of_wave[3][q]));
+    }
+}
+
+// ---- launches ----------------------------------------------------------------
+
+constexpr int kSliceThreads = 256;
+constexpr int64_t kRowBytes = 1024 * 16 * 16;         // what a block of 1024 threads holds
+
+int64_t elem_size(int dtype) { return dtype == 0 ? 4 : 2; }
+
+// Slices of a row: enough blocks for the chip, at least 16 KiB each.
+Cut cut_of(int64_t rows, int64_t vocab, int dtype, int compute_units)
+{
+    const int64_t want = (4 * compute_units + rows - 1) / rows, most = (vocab * elem_size(dtype) + 16383) / 16384;
+    int64_t slices = want < most ? want : most;
+    if (slices < 1) slices = 1;
+    Cut cut;
+    cut.length = ((vocab + slices - 1) / slices + 7) / 8 * 8;
+    cut.slices = static_cast<int32_t>((vocab + cut.length - 1) / cut.length);
+    return cut;
+}
+
+struct Work {
+    int64_t terms, z_token, sums, bytes;
+};
+Work layout(int64_t rows, const Cut &cut)
+{
+    Work w;
+    w.terms = 0;
+    w.z_token = w.terms + static_cast<int64_t>(sizeof(RowTerms)) * rows;
+    w.sums = (w.z_token + 4 * rows + 15) / 16 * 16;
+    w.bytes = w.sums + static_cast<int64_t>(sizeof(TopSum)) * rows * cut.slices;
+    return w;
+}
+
+template <int DT>
+void launch_policy(const void *logits, int64_t rows, int64_t vocab, int64_t stride, const int32_t *tokens, const PolicyTerms &p, void *grad,
+                   int64_t grad_stride, float *logp, char *work, int compute_units, hipStream_t stream)
+{
+    const Cut cut = cut_of(rows, vocab, DT, compute_units);
+    const Work w = layout(rows, cut);
+    const RowPlace at{vocab, stride};
+    const char *from = static_cast<const char *>(logits);
+    char *to = static_cast<char *>(grad);
+    RowTerms *terms = reinterpret_cast<RowTerms *>(work + w.terms);
+    const int64_t bytes = vocab * elem_size(DT);
+    if (bytes <= kRowBytes) {
+        const uint32_t blocks = static_cast<uint32_t>(rows);
+        auto go = [&](auto kernel, int threads) { kernel<<<blocks, threads, 0, stream>>>(from, at, tokens, p, to, grad_stride, logp, terms); };
+        if (bytes <= 64 * 8 * 16) go(policy_row_kernel<DT, 64, 8>, 64);
+        else if (bytes <= 128 * 8 * 16) go(policy_row_kernel<DT, 128, 8>, 128);
+        else if (bytes <= 256 * 8 * 16) go(policy_row_kernel<DT, 256, 8>, 256);
+        else if (bytes <= 512 * 8 * 16) go(policy_row_kernel<DT, 512, 8>, 512);
+        else if (bytes <= 1024 * 8 * 16) go(policy_row_kernel<DT, 1024, 8>, 1024);
+        else go(policy_row_kernel<DT, 1024, 16>, 1024);
+        return;
+    }
+    TopSum *sums = reinterpret_cast<TopSum *>(work + w.sums);
+    float *z = reinterpret_cast<float *>(work + w.z_token);
+    const uint32_t blocks = static_cast<uint32_t>(rows * cut.slices);
+    slice_sum_kernel<DT, kSliceThreads><<<blocks, kSliceThreads, 0, stream>>>(from, at, cut, tokens, p.weight, sums, z, nullptr);
+    policy_slice_kernel<DT, kSliceThreads><<<blocks, kSliceThreads, 0, stream>>>(from, at, cut, tokens, p, sums, z, to, grad_stride, logp, terms);
+}
+
+}  // namespace
+
+int64_t policy_work_bytes(int64_t N, int64_t T, int64_t vocab, int dtype, int compute_units)
+{
+    return N * T == 0 ? 0 : layout(N * T, cut_of(N * T, vocab, dtype, compute_units)).bytes;
+}
+
+hipError_t launch_policy_loss(const void *logits, int dtype, int64_t N, int64_t T, int64_t vocab, int64_t stride, const int32_t *tokens,
+                              const PolicyTerms &p, void *grad, int64_t grad_stride, float *logp, float *stats, void *work,
+                              int compute_units, hipStream_t stream)
+{
+    char *at = static_cast<char *>(work);
+    if (!launchable(N * T, 1024) && !launchable(N * T, (vocab * elem_size(dtype) + 127) / 128 + 63)) return hipErrorInvalidConfiguration;
+    if (T > 0)
+        (dtype == 0 ? launch_policy<0> : launch_policy<1>)(logits, N * T, vocab, stride, tokens, p, grad, grad_stride, logp, at, compute_units, stream);
+    policy_stats_kernel<<<static_cast<uint32_t>(N), 256, 0, stream>>>(reinterpret_cast<const RowTerms *>(at), T, stats);
+    return hipGetLastError();
+}
+
+hipError_t launch_token_logp(const void *logits, int dtype, int64_t rows, int64_t vocab, int64_t stride, const int32_t *tokens, float *logp,
+                             void *work, int compute_units, hipStream_t stream)
+{
+    if (rows == 0) return hipSuccess;
+    if (!launchable(rows, kSliceThreads)) return hipErrorInvalidConfiguration;
+    const Cut cut = cut_of(rows, vocab, dtype, compute_units);
+    const Work w = layout(rows, cut);
+    TopSum *sums = reinterpret_cast<TopSum *>(static_cast<char *>(work) + w.sums);
+    float *z = cut.slices > 1 ? reinterpret_cast<float *>(static_cast<char *>(work) + w.z_token) : nullptr;
+    const uint32_t blocks = static_cast<uint32_t>(rows * cut.slices);
+    (dtype == 0 ? slice_sum_kernel<0, kSliceThreads> : slice_sum_kernel<1, kSliceThreads>)<<<blocks, kSliceThreads, 0, stream>>>(
+        static_cast<const char *>(logits), RowPlace{vocab, stride}, cut, tokens, nullptr, sums, z, logp);
+    if (cut.slices > 1) logp_join_kernel<<<static_cast<uint32_t>(rows), 64, 0, stream>>>(sums, z, cut.slices, tokens, vocab, logp);
+    return hipGetLastError();
+}
+
+}  // namespace moshpit
