@@ -3,15 +3,15 @@
 // for every row v of every table (rows without a token: zeros, or untouched where the gradient is added).
 //
 // Tokens first: each peer's places are sorted by token, stably (a radix sort, 8 bits a pass), so that the
-// places of a row lie side by side in ascending order.  Then the sums, in one pass over dy and the tables.
-// The sorted places and the ends of the table's rows are merged into one list of T + vocab items
-// (a row's end comes after its places) and cut into shares of `share` items, one to a group of lanes: a
-// frequent token is as many shares as its places take, a stretch of rows without tokens is shares of zeros,
-// and every share moves about as many bytes.  A cut moves to the start of its row where the row has at
-// most 63 places.  A row that is still cut leaves a partial sum per share, and a last kernel adds those in
-// ascending order.  Which sums are formed and in which order follows from the sizes and tokens alone.
+// places of a row lie side by side in ascending order.  Meanwhile other blocks of the same launch clear the tables:
+// most rows of a vocabulary have no token, and a plain fill writes them at 6.8 TB/s, while waves that each
+// write the empty rows between their own reached 4.7 (64 tables of 30000 x 128 binary32).
+// Then the sums.  The sorted places are cut into shares of kShare, one to a wave and column slice; a cut moves to the
+// start of its row where the row has at most 63 places.  A row that is still cut leaves a partial sum per share, and
+// a last kernel adds those in ascending order.  Which sums are formed and in which order follows from the
+// sizes and tokens alone.
 //
-// Bound by HBM: dy is read once, the tables' gradient is written once.
+// Bound by HBM: dy is read once, the tables' gradient is written once (rows with tokens twice).
 #include <hip/hip_runtime.h>
 
 #include "local_ops.h"
@@ -28,6 +28,7 @@ struct SortPlan {
     int32_t T, passes;
     uint32_t vocab;
     uint32_t tiles;                      // of a peer; block b works on tile b % tiles of peer b / tiles
+    uint32_t sort_blocks;                // blocks beyond these clear the tables
 };
 
 __device__ __forceinline__ uint32_t sort_key(const int32_t *__restrict__ tokens, int64_t at, uint32_t vocab)
@@ -108,11 +109,36 @@ __device__ __forceinline__ void block_rank(const uint32_t (&key)[ITEMS], int shi
     }
 }
 
+// What the blocks beyond the sort's do: zeros to the tables, 16 bytes a thread (more of them write in a wider window of
+// memory at a time: 983 MB in 160 us, with 4 or 16 vectors a thread in 165 to 168).
+struct Fill {
+    char *base;
+    int64_t peer_bytes, table_bytes;     // from table to table; of a table
+    uint32_t blocks;                     // of a table
+    uint32_t first;                      // block of all tables that this launch begins with
+};
+
+template <int THREADS> __device__ __forceinline__ void fill_zeros(const Fill &f, uint32_t block)
+{
+    block += f.first;
+    const int64_t begin = int64_t(block % f.blocks) * (16 * THREADS);
+    char *table = f.base + int64_t(block / f.blocks) * f.peer_bytes;
+    // whole vectors at 16-byte boundaries; the few bytes at the table's ends by elements
+    const uint32_t phase = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(table)) % 16;
+    const int64_t head = phase ? 16 - phase : 0;
+    const int64_t at = begin + head + int64_t(threadIdx.x) * 16;
+    if (at + 16 <= f.table_bytes) store_vec<true, u32x4>(table + at, u32x4{0, 0, 0, 0});
+    else
+        for (int64_t e = at; e < f.table_bytes; e += 2) *reinterpret_cast<uint16_t *>(table + e) = 0;
+    if (begin == 0 && threadIdx.x < head / 2 && threadIdx.x * 2 < f.table_bytes) *reinterpret_cast<uint16_t *>(table + 2 * threadIdx.x) = 0;
+}
+
 // All passes of a peer's sort by one block, T <= THREADS * ITEMS.
 template <int THREADS, int ITEMS>
 __global__ __launch_bounds__(THREADS) void sort_block_kernel(const int32_t *__restrict__ tokens, SortPlan p, uint32_t *__restrict__ keys,
-                                                             int32_t *__restrict__ places)
+                                                             int32_t *__restrict__ places, Fill fill)
 {
+    if (blockIdx.x >= p.sort_blocks) return fill_zeros<THREADS>(fill, blockIdx.x - p.sort_blocks);
     __shared__ uint32_t count[(THREADS / 64 + 1) * kBins];
     __shared__ uint32_t swap_key[THREADS * ITEMS];
     __shared__ uint16_t swap_place[THREADS * ITEMS];
@@ -160,8 +186,9 @@ __device__ __forceinline__ uint32_t pass_key(const int32_t *__restrict__ tokens,
 }
 
 __global__ __launch_bounds__(kTileThreads) void sort_count_kernel(const int32_t *__restrict__ tokens, const uint32_t *__restrict__ keys,
-                                                                   SortPlan p, int shift, uint32_t *__restrict__ bins)
+                                                                   SortPlan p, int shift, uint32_t *__restrict__ bins, Fill fill)
 {
+    if (blockIdx.x >= p.sort_blocks) return fill_zeros<kTileThreads>(fill, blockIdx.x - p.sort_blocks);
     __shared__ uint32_t count[kBins];
     const uint32_t peer = blockIdx.x / p.tiles, tile = blockIdx.x % p.tiles;
     const int64_t row = int64_t(peer) * p.T;
@@ -219,8 +246,9 @@ __global__ __launch_bounds__(1024) void sort_scan_kernel(uint32_t *__restrict__ 
 __global__ __launch_bounds__(kTileThreads) void sort_move_kernel(const int32_t *__restrict__ tokens, const uint32_t *__restrict__ keys,
                                                                   const int32_t *__restrict__ places, SortPlan p, int shift,
                                                                   const uint32_t *__restrict__ bins, uint32_t *__restrict__ keys_out,
-                                                                  int32_t *__restrict__ places_out)
+                                                                  int32_t *__restrict__ places_out, Fill fill)
 {
+    if (blockIdx.x >= p.sort_blocks) return fill_zeros<kTileThreads>(fill, blockIdx.x - p.sort_blocks);
     __shared__ uint32_t count[(kTileThreads / 64 + 1) * kBins];
     __shared__ uint32_t goes_to[kBins];
     const uint32_t peer = blockIdx.x / p.tiles, tile = blockIdx.x % p.tiles;
@@ -250,180 +278,243 @@ __global__ __launch_bounds__(kTileThreads) void sort_move_kernel(const int32_t *
 // ---- sums --------------------------------------------------------------------
 
 constexpr int kSnap = 63;                // a row of at most this many places is not cut
-constexpr int kWave = 64, kBlock = 256, kBatch = 8, kJoinShares = 16;
+constexpr int kShare = 32;               // places of a share
+constexpr int kWave = 64, kBlock = 256, kWaves = kBlock / kWave, kBatch = 8, kJoinShares = 16;
 
-// What a share left behind: its first row, whether that row began in a share before, and its last row + 1
-// among those that end in it (row .. end - 1 end here).
-struct ShareRecord {
-    uint32_t row, end;
-    int32_t carried_in;
+// The cut before a share: its first place (in the window of the wave that made it); inside (bit 31): the row of that place has places before it too.
+struct Cut {
+    uint32_t row, place_inside;
+    __device__ __forceinline__ uint32_t place() const { return place_inside & 0x7fffffffu; }
+    __device__ __forceinline__ bool inside() const { return place_inside >> 31; }
 };
 
 struct ShareGeom {
-    int64_t shares;                      // of a peer
-    uint32_t blocks;                     // of a peer, in each of the two kernels
-    int32_t share, lanes_log2, slices;   // items of a share; lanes of its group; column slices
+    int64_t shares;                      // of a peer; it has shares + 1 cuts
+    uint32_t slices;                     // column slices of a share
+    uint32_t blocks;                     // of a peer, in the kernel at hand
 };
 
-// The cut before item d of the merged list: rows 0..v-1 have ended and j places have been taken.  The merged list
-// has key[j] + j ascending, and j is the first place with key[j] + j >= d.  Lanes of a group search together.
-__device__ __forceinline__ void find_cut(const uint32_t *__restrict__ key, int64_t T, int64_t vocab, int64_t d, int lane, int lanes, int lanes_log2,
-                                         uint64_t group_mask, int64_t &v, int64_t &j, bool &inside)
+// VE elements of a row as they lie in memory, so that loads in flight take few registers.
+template <int DT, int VE> struct Raw {
+    static constexpr int WORDS = DT == 0 ? VE : (VE + 1) / 2;
+    uint32_t w[WORDS];
+    __device__ __forceinline__ void load(const char *p)
+    {
+        if constexpr (DT == 1 && VE == 1) w[0] = *reinterpret_cast<const uint16_t *>(p);
+        else if constexpr (WORDS == 1) w[0] = load_vec<true, uint32_t>(p);
+        else if constexpr (WORDS == 2) put(load_vec<true, u32x2>(p));
+        else put(load_vec<true, u32x4>(p));
+        if constexpr (WORDS == 8) {
+            const u32x4 v = load_vec<true, u32x4>(p + 16);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) w[4 + k] = v[k];
+        }
+    }
+    template <typename V> __device__ __forceinline__ void put(const V &v)
+    {
+#pragma unroll
+        for (int k = 0; k < static_cast<int>(sizeof(V) / 4); ++k) w[k] = v[k];
+    }
+    __device__ __forceinline__ float operator[](int k) const
+    {
+        if constexpr (DT == 0) return __uint_as_float(w[k]);
+        else return __uint_as_float(k & 1 ? w[k / 2] & 0xffff0000u : w[k / 2] << 16);
+    }
+};
+template <int DT, int VE> __device__ __forceinline__ void load_run(const char *p, float (&f)[VE])
 {
-    int64_t lo = d > vocab ? d - vocab : 0, hi = d < T ? d : T;       // (lo <= hi where d <= T + vocab)
-    while (lo < hi) {
-        const int64_t step = ((hi - lo) >> lanes_log2) + 1;           // probes lo, lo + step, ...
-        const int64_t at = lo + lane * step;
-        const bool below = at < hi && int64_t(key[at]) + at < d;
-        const int n = __popcll(__ballot(below) & group_mask);         // the first n probes are below
-        if (n == 0) { hi = lo; break; }
-        const int64_t last = lo + (n - 1) * step;
-        const int64_t next = lo + n * step;
-        lo = last + 1;
-        hi = n < lanes && next < hi ? next : hi;
-    }
-    j = lo;
-    v = d - j;
-    inside = false;
-    if (j == 0 || v >= vocab || key[j - 1] != v) return;
-    // places of row v lie on both sides of the cut: count those before it and, if they are few, those after it
-    int64_t before = 0, after = 0;
-    for (int64_t k = 0; k <= kSnap && before == k; k += lanes) {
-        const int64_t at = j - 1 - k - lane;
-        before += __popcll(__ballot(at >= 0 && key[at] == v) & group_mask);
-    }
-    for (int64_t k = 0; k <= kSnap && after == k; k += lanes) {
-        const int64_t at = j + k + lane;
-        after += __popcll(__ballot(at < T && key[at] == v) & group_mask);
-    }
-    if (before + after <= kSnap) j -= before;
-    else inside = true;
+    Raw<DT, VE> raw;
+    raw.load(p);
+#pragma unroll
+    for (int k = 0; k < VE; ++k) f[k] = raw[k];
+}
+template <int DT, int VE> __device__ __forceinline__ void store_run(char *p, const float (&f)[VE])
+{
+    if constexpr (VE >= 4) store_elems<DT, VE, true>(p, f);
+    else if constexpr (VE == 2 && DT == 0) store_vec<true, u32x2>(p, u32x2{__float_as_uint(f[0]), __float_as_uint(f[1])});
+    else if constexpr (VE == 2) store_vec<false, uint32_t>(p, bf16_pair(f[0], f[1]));
+    else store_one<DT>(p, f[0]);
 }
 
-template <int ST, int YT, int VE, bool WIDE, bool ADD>
-__global__ __launch_bounds__(kBlock) void embed_grad_kernel(const uint32_t *__restrict__ keys, const int32_t *__restrict__ places,
-                                                            const char *__restrict__ dy, int64_t dy_stride, char *__restrict__ base, TableGeom g,
-                                                            ShareGeom s, float scale, ShareRecord *__restrict__ records,
-                                                            float *__restrict__ partials)
-{
-    constexpr int ES = ST == 0 ? 4 : 2, EY = YT == 0 ? 4 : 2;
-    const int lanes = 1 << s.lanes_log2, lane = threadIdx.x & (lanes - 1);
-    const uint32_t peer = blockIdx.x / s.blocks;
-    const int64_t share = int64_t(blockIdx.x % s.blocks) * (kBlock >> s.lanes_log2) + (threadIdx.x >> s.lanes_log2);
-    if (share >= s.shares) return;                                    // (whole groups; the ballots below look at a group's own lanes)
-    const uint64_t group_mask = lanes == 64 ? ~uint64_t(0) : ((uint64_t(1) << lanes) - 1) << (threadIdx.x & 63 & ~(lanes - 1));
-    const uint32_t *key = keys + peer * g.T;
-    const int32_t *place = places + peer * g.T;
-    const int64_t items = g.T + g.vocab;
-    int64_t row, j, end, j_end;
-    bool carried, cut;
-    const int64_t d0 = share * s.share, d1 = d0 + s.share < items ? d0 + s.share : items;
-    find_cut(key, g.T, g.vocab, d0, lane, lanes, s.lanes_log2, group_mask, row, j, carried);
-    find_cut(key, g.T, g.vocab, d1, lane, lanes, s.lanes_log2, group_mask, end, j_end, cut);
-
-    const int64_t c = (int64_t(blockIdx.y) * lanes + lane) * VE;
-    const int64_t at_c = WIDE && c + VE > g.width ? g.width - VE : c;  // the last vector of a row ends with the row
-    char *table = base + peer * g.peer_stride * ES;
-    const char *rows = dy + peer * g.T * dy_stride * EY;
-    float *slot = partials + (peer * s.shares + share) * 2 * g.width;
-    const uint32_t vocab = static_cast<uint32_t>(g.vocab);
-    if (lane == 0 && blockIdx.y == 0) records[peer * s.shares + share] = ShareRecord{static_cast<uint32_t>(row), static_cast<uint32_t>(end), carried};
-
-    float acc[VE] = {};
-    auto store_row = [&](int64_t r, const float (&f)[VE]) {
-        if (c >= g.width) return;
-        char *to = table + r * g.width * ES;
-        if (c + VE <= g.width) {
+// The columns of a table that a wave works on: lane l has VE of them, those of the last lane that has any ending with
+// the row (it repeats columns of the lane before).
+template <int ST, int YT, int VE, bool ADD> struct Columns {
+    static constexpr int ES = ST == 0 ? 4 : 2, EY = YT == 0 ? 4 : 2;
+    int32_t width, c, at_c;              // this lane's columns c .. c + VE - 1, read from at_c on
+    bool any, whole;                     // it has columns; VE of them
+    __device__ __forceinline__ Columns(int64_t w, uint32_t slice)
+    {
+        width = static_cast<int32_t>(w);
+        c = static_cast<int32_t>((slice * kWave + (threadIdx.x & 63)) * VE);
+        any = c < width;
+        whole = c + VE <= width;
+        at_c = whole ? c : width - VE;                                // (width >= VE; a lane without columns reads the last ones, too)
+    }
+    __device__ __forceinline__ void load(const char *row, Raw<YT, VE> &r) const { r.load(row + at_c * EY); }
+    __device__ __forceinline__ void store(char *row, const float (&f)[VE]) const
+    {
+        if (!any) return;
+        if (whole) {
             float v[VE];
             if constexpr (ADD) {
-                load_elems<ST, VE>(to + c * ES, v);
+                load_run<ST, VE>(row + c * ES, v);
 #pragma unroll
                 for (int k = 0; k < VE; ++k) v[k] += f[k];
-                store_elems<ST, VE>(to + c * ES, v);
-            } else store_elems<ST, VE>(to + c * ES, f);
+                store_run<ST, VE>(row + c * ES, v);
+            } else store_run<ST, VE>(row + c * ES, f);
         } else {
 #pragma unroll
             for (int k = 0; k < VE; ++k) {
-                const int64_t e = at_c + k;
-                if (e < c || e >= g.width) continue;
-                store_one<ST>(to + e * ES, ADD ? load_one<ST>(to + e * ES) + f[k] : f[k]);
+                const int32_t e = at_c + k;
+                if (e >= c && e < width) store_one<ST>(row + e * ES, ADD ? load_one<ST>(row + e * ES) + f[k] : f[k]);
             }
         }
-    };
-    auto store_partial = [&](float *to) {
-        if (c >= g.width) return;
+    }
+    __device__ __forceinline__ void store_partial(float *to, const float (&f)[VE]) const
+    {
+        if (!any) return;
 #pragma unroll
         for (int k = 0; k < VE; ++k) {
-            const int64_t e = at_c + k;
-            if (e >= c && e < g.width) to[e] = acc[k];
+            const int32_t e = at_c + k;
+            if (e >= c && e < width) to[e] = f[k];
+        }
+    }
+};
+
+// A share a wave and column slice.  Rows, places and all branches are the same for the whole wave.
+template <int ST, int YT, int VE, bool ADD>
+__global__ __launch_bounds__(kBlock) void embed_grad_kernel(const uint32_t *__restrict__ keys, const int32_t *__restrict__ places,
+                                                            const char *__restrict__ dy, int64_t dy_stride, char *__restrict__ base, TableGeom g,
+                                                            ShareGeom s, float scale, Cut *__restrict__ cuts, float *__restrict__ partials)
+{
+    constexpr int ES = ST == 0 ? 4 : 2, EY = YT == 0 ? 4 : 2;
+    const uint32_t peer = blockIdx.x / s.blocks;
+    const uint32_t part = blockIdx.x % s.blocks * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t share = part / s.slices, slice = part % s.slices;  // the slices of a share side by side: whole rows are read and written at a time
+    if (share >= s.shares) return;
+    const int lane = threadIdx.x & 63;
+    const uint32_t vocab = static_cast<uint32_t>(g.vocab);
+    const uint32_t *key = keys + peer * g.T;
+    // the sorted places from 64 before the share to 128 after its start, a place a lane: all that the cuts and the
+    // sums look at, requested at once
+    const int64_t first = int64_t(share) * kShare;
+    uint32_t k_of[3];
+    int32_t p_of[2];
+#pragma unroll
+    for (int q = 0; q < 3; ++q) {
+        const int64_t at = first + (q - 1) * kWave + lane;
+        const bool there = at >= 0 && at < g.T;
+        k_of[q] = there ? key[at] : vocab;
+        if (q < 2) p_of[q] = there ? places[peer * g.T + at] : 0;
+    }
+    // A cut lies before place kShare * share; where the row there has at most kSnap places on both sides it moves to the row's
+    // first.  `at`: place of the cut in the window.
+    auto cut_at = [&](int at, uint32_t row) {
+        const uint64_t same[3] = {__ballot(k_of[0] == row), __ballot(k_of[1] == row), __ballot(k_of[2] == row)};
+        // places of the row among the 64 before the cut and the 64 from it on
+        const int shift = at - kWave;                                 // 0 or kShare
+        const uint64_t before = shift == 0 ? same[0] : same[0] >> shift | same[1] << (kWave - shift);
+        const uint64_t after = shift == 0 ? same[1] : same[1] >> shift | same[2] << (kWave - shift);
+        const int b = __popcll(before), a = __popcll(after);
+        if (row >= vocab || a == 0 || b == 0) return Cut{row, static_cast<uint32_t>(at)};
+        if (a + b <= kSnap) return Cut{row, static_cast<uint32_t>(at - b)};
+        return Cut{row, static_cast<uint32_t>(at) | 0x80000000u};
+    };
+    const uint32_t row0 = __builtin_amdgcn_readfirstlane(k_of[1]);
+    const Cut from = cut_at(kWave, row0), to = cut_at(kWave + kShare, __builtin_amdgcn_readlane(k_of[1], kShare));
+    if (slice == 0 && lane == 0) {
+        Cut *mine = cuts + peer * (s.shares + 1) + share;
+        mine[0] = from;
+        if (share + 1 == s.shares) mine[1] = Cut{vocab, 0};
+    }
+    const Columns<ST, YT, VE, ADD> columns(g.width, slice);
+    char *table = base + peer * g.peer_stride * ES;
+    const char *rows = dy + peer * g.T * dy_stride * EY;
+    float *slot = partials + (peer * s.shares + share) * 2 * g.width;
+
+    // its places lie at begin .. end - 1 of the window; those without a token come last and do not count
+    const uint32_t begin = from.place();
+    const uint32_t tokens_end = __popcll(__ballot(k_of[1] < vocab)) + kWave;
+    const uint32_t end = to.place() < tokens_end ? to.place() : tokens_end;
+    if (begin >= end) return;
+    auto key_at = [&](uint32_t at) -> uint32_t {
+        return at < kWave ? __builtin_amdgcn_readlane(k_of[0], at) : __builtin_amdgcn_readlane(k_of[1], at - kWave);
+    };
+    auto request = [&](uint32_t at, Raw<YT, VE> (&v)[kBatch]) {       // the rows of up to kBatch places; beyond the last one that one again
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const uint32_t e = at + u < end ? at + u : end - 1;
+            const int32_t p = e < kWave ? __builtin_amdgcn_readlane(p_of[0], e) : __builtin_amdgcn_readlane(p_of[1], e - kWave);
+            columns.load(rows + int64_t(p) * dy_stride * EY, v[u]);
         }
     };
-    bool head = carried, any = carried;                               // any: the row has places in this share or before
-    auto finish = [&]() {                                             // the end of `row`
-        if (head) store_partial(slot);
-        else if (any || !ADD) {
-            float f[VE];
+
+    float acc[VE] = {};
+    uint32_t row = from.row;
+    bool head = from.inside();                                        // the row began in a share before
+    auto finish = [&]() {                                             // all places of `row` are in
+        if (head) columns.store_partial(slot, acc);
+        else {
 #pragma unroll
-            for (int k = 0; k < VE; ++k) f[k] = scale * acc[k];
-            store_row(row, f);
+            for (int k = 0; k < VE; ++k) acc[k] *= scale;
+            columns.store(table + int64_t(row) * g.width * ES, acc);
         }
-        head = any = false;
+        head = false;
 #pragma unroll
         for (int k = 0; k < VE; ++k) acc[k] = 0.f;
-        ++row;
     };
-    while (j < j_end) {
-        const int64_t left = j_end - j;
-        const int n = left < kBatch ? static_cast<int>(left) : kBatch;
-        uint32_t k_of[kBatch];
-        float v[kBatch][VE];
+    auto add = [&](uint32_t at, const Raw<YT, VE> (&v)[kBatch]) {
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
-            k_of[u] = u < n ? key[j + u] : vocab;
-            if (k_of[u] >= vocab) continue;                           // (no token: after every row's end)
-            const char *from = rows + int64_t(place[j + u]) * dy_stride * EY;
-            if constexpr (WIDE) {
-                if (c < g.width) load_elems<YT, VE>(from + at_c * EY, v[u]);
-            } else {
-#pragma unroll
-                for (int k = 0; k < VE; ++k) v[u][k] = c + k < g.width ? load_one<YT>(from + (c + k) * EY) : 0.f;
+            if (at + u >= end) break;
+            const uint32_t k = key_at(at + u);
+            if (row != k) {
+                finish();
+                row = k;
             }
-        }
 #pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-            if (k_of[u] >= vocab) continue;
-            while (row < k_of[u]) finish();
-            any = true;
-#pragma unroll
-            for (int k = 0; k < VE; ++k) acc[k] += v[u][k];
+            for (int e = 0; e < VE; ++e) acc[e] += v[u][e];
         }
-        if (k_of[kBatch - 1] >= vocab) break;
-        j += n;
+    };
+    // the rows of the next places are requested before those of these are added
+    Raw<YT, VE> even[kBatch], odd[kBatch];
+    request(begin, even);
+    for (uint32_t at = begin; at < end; at += 2 * kBatch) {
+        if (at + kBatch < end) request(at + kBatch, odd);
+        add(at, even);
+        if (at + kBatch >= end) break;
+        if (at + 2 * kBatch < end) request(at + 2 * kBatch, even);
+        add(at + kBatch, odd);
     }
-    while (row < end) finish();
-    if (cut) store_partial(head ? slot : slot + g.width);             // the row goes on in the next share
+    if (!to.inside()) finish();
+    else columns.store_partial(head ? slot : slot + g.width, acc);         // the row goes on in the next share
 }
 
 // Rows cut by shares: the share in which such a row ends adds its partial sums, in the order of the shares.
 template <int ST, bool ADD>
 __global__ __launch_bounds__(kBlock) void embed_grad_join_kernel(char *__restrict__ base, TableGeom g, ShareGeom s, float scale,
-                                                                 const ShareRecord *__restrict__ records, const float *__restrict__ partials)
+                                                                 const Cut *__restrict__ cuts, const float *__restrict__ partials)
 {
-    constexpr int ES = ST == 0 ? 4 : 2, kWaves = kBlock / kWave;
+    constexpr int ES = ST == 0 ? 4 : 2;
     __shared__ float wave_sum[kWaves][kWave];
     const uint32_t peer = blockIdx.x / s.blocks;
-    const ShareRecord *record = records + peer * s.shares;
+    const Cut *cut = cuts + peer * (s.shares + 1);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t share0 = int64_t(blockIdx.x % s.blocks) * kJoinShares;
-    const ShareRecord candidate = lane < kJoinShares && share0 + lane < s.shares ? record[share0 + lane] : ShareRecord{0, 0, 0};
-    uint64_t ending = __ballot(candidate.carried_in && candidate.end != candidate.row);      // the same in every wave
+    bool ends = false;                                                // a row that began before this lane's share ends in it
+    if (lane < kJoinShares && share0 + lane < s.shares) {
+        const Cut in = cut[share0 + lane];
+        const Cut out = cut[share0 + lane + 1];
+        ends = in.inside() && !(out.inside() && out.row == in.row);
+    }
+    uint64_t ending = __ballot(ends);                                 // the same in every wave
     for (; ending; ending &= ending - 1) {
         const int64_t last = share0 + __builtin_ctzll(ending);
-        const ShareRecord here = record[last];
+        const uint32_t row = cut[last].row;
         int64_t first = last - 1;                                         // the share in which the row begins
         while (true) {
             const int64_t at = first - lane;
-            const bool middle = at >= 0 && record[at].carried_in && record[at].row == here.row;
+            const bool middle = at >= 0 && cut[at].inside() && cut[at].row == row;
             const uint64_t stop = ~__ballot(middle);
             if (stop) {
                 first -= __builtin_ctzll(stop);
@@ -453,7 +544,7 @@ __global__ __launch_bounds__(kBlock) void embed_grad_join_kernel(char *__restric
                 float sum = 0.f;
     #pragma unroll
                 for (int w = 0; w < kWaves; ++w) sum += wave_sum[w][lane];
-                char *to = base + (peer * g.peer_stride + int64_t(here.row) * g.width + c) * ES;
+                char *to = base + (peer * g.peer_stride + int64_t(row) * g.width + c) * ES;
                 const float f = scale * sum;
                 store_one<ST>(to, ADD ? load_one<ST>(to) + f : f);
             }
@@ -468,19 +559,18 @@ constexpr int64_t kOneBlock = 8192;      // places that one block sorts
 
 int64_t padded(int64_t bytes) { return (bytes + 255) / 256 * 256; }
 
-ShareGeom shares_of(const TableGeom &g)
+// Elements of a lane: as few as let a wave have all columns, at most 16 bytes of the table.
+int lane_elems(const TableGeom &g, int state_dtype)
 {
-    ShareGeom s;
-    s.share = 32;
-    s.shares = (g.T + g.vocab + s.share - 1) / s.share;
-    s.blocks = 0;
-    s.lanes_log2 = 3;
-    s.slices = 0;
-    return s;
+    int ve = 1;
+    while (ve < (state_dtype == 0 ? 4 : 8) && kWave * ve < g.width) ve *= 2;
+    return ve;
 }
 
+ShareGeom shares_of(const TableGeom &g) { return ShareGeom{(g.T + kShare - 1) / kShare, 1, 0}; }
+
 struct Work {
-    int64_t keys[2], places[2], bins, records, partials, bytes;
+    int64_t keys[2], places[2], bins, cuts, partials, bytes;
 };
 
 Work layout(const TableGeom &g)
@@ -500,39 +590,49 @@ Work layout(const TableGeom &g)
     }
     if (tiled) w.bins = take(4 * g.N * kBins * ((g.T + kTile - 1) / kTile));
     const ShareGeom s = shares_of(g);
-    w.records = take(static_cast<int64_t>(sizeof(ShareRecord)) * g.N * s.shares);
+    w.cuts = take(static_cast<int64_t>(sizeof(Cut)) * g.N * (s.shares + 1));
     w.partials = take(g.T > kSnap ? 4 * g.N * s.shares * 2 * g.width : 0);
     w.bytes = at;
     return w;
 }
 
-template <int ST, int YT, bool ADD>
-void launch(void *base, const TableGeom &g, float scale, const void *dy, int64_t dy_stride, const uint32_t *keys, const int32_t *places,
-            ShareRecord *records, float *partials, hipStream_t stream)
+template <int ST, int YT, int VE, bool ADD>
+void launch_sums(void *base, const TableGeom &g, float scale, const void *dy, int64_t dy_stride, const uint32_t *keys, const int32_t *places,
+                 Cut *cuts, float *partials, hipStream_t stream)
 {
-    constexpr int VE = ST == 0 ? 4 : 8;                               // 16 bytes of the table a lane
+    if (g.T == 0) return;
     ShareGeom s = shares_of(g);
-    while (s.lanes_log2 < 6 && (int64_t(VE) << s.lanes_log2) < g.width) ++s.lanes_log2;
-    s.slices = static_cast<int32_t>((g.width + (int64_t(VE) << s.lanes_log2) - 1) / (int64_t(VE) << s.lanes_log2));
-    const int64_t per_block = kBlock >> s.lanes_log2;
-    s.blocks = static_cast<uint32_t>((s.shares + per_block - 1) / per_block);
-    const dim3 grid(static_cast<uint32_t>(s.blocks * g.N), static_cast<uint32_t>(s.slices));
-    auto kernel = g.width >= VE ? embed_grad_kernel<ST, YT, VE, true, ADD> : embed_grad_kernel<ST, YT, VE, false, ADD>;
-    kernel<<<grid, kBlock, 0, stream>>>(keys, places, static_cast<const char *>(dy), dy_stride, static_cast<char *>(base), g, s, scale, records,
-                                        partials);
+    s.slices = static_cast<uint32_t>((g.width + kWave * VE - 1) / (kWave * VE));
+    s.blocks = static_cast<uint32_t>((s.shares * s.slices + kWaves - 1) / kWaves);
+    embed_grad_kernel<ST, YT, VE, ADD><<<static_cast<uint32_t>(s.blocks * g.N), kBlock, 0, stream>>>(keys, places, static_cast<const char *>(dy), dy_stride, static_cast<char *>(base), g, s,
+                                                                    scale, cuts, partials);
     if (g.T <= kSnap) return;                                         // no row is cut
     const int64_t column_blocks = (g.width + kWave - 1) / kWave;
     s.blocks = static_cast<uint32_t>((s.shares + kJoinShares - 1) / kJoinShares);
     const dim3 joins(static_cast<uint32_t>(s.blocks * g.N), static_cast<uint32_t>(column_blocks < 16 ? column_blocks : 16));
-    embed_grad_join_kernel<ST, ADD><<<joins, kBlock, 0, stream>>>(static_cast<char *>(base), g, s, scale, records, partials);
+    embed_grad_join_kernel<ST, ADD><<<joins, kBlock, 0, stream>>>(static_cast<char *>(base), g, s, scale, cuts, partials);
+}
+
+template <int ST, int YT, bool ADD>
+void launch(void *base, const TableGeom &g, float scale, const void *dy, int64_t dy_stride, const uint32_t *keys, const int32_t *places,
+            Cut *cuts, float *partials, hipStream_t stream)
+{
+    auto go = [&](auto f) { f(base, g, scale, dy, dy_stride, keys, places, cuts, partials, stream); };
+    switch (lane_elems(g, ST)) {
+    case 1: return go(launch_sums<ST, YT, 1, ADD>);
+    case 2: return go(launch_sums<ST, YT, 2, ADD>);
+    case 4: return go(launch_sums<ST, YT, 4, ADD>);
+    default: return go(launch_sums<ST, YT, ST == 0 ? 4 : 8, ADD>);
+    }
 }
 
 }  // namespace
 
 bool embed_grad_fits(const TableGeom &g)
 {
-    // the sums' kernel: 4 shares a block at least; the sort: a tile a block at least
-    return shares_of(g).shares / 4 + 1 <= 0xffffffffLL / kBlock / g.N && (g.T / 1024 + 1) <= 0xffffffffLL / 1024 / g.N;
+    // blocks of the sums' kernel (4 shares and slices of 64 columns or more each), threads of the sort and the clearing
+    const int64_t sums = shares_of(g).shares * ((g.width + kWave - 1) / kWave) / 4 + 1, clear = g.vocab * g.width / 4 + g.T + 1024;
+    return sums <= 0xffffffffLL / kBlock / g.N && clear <= 0xffffffffLL / g.N;
 }
 
 int64_t embed_grad_work_bytes(const TableGeom &g) { return layout(g).bytes; }
@@ -544,37 +644,48 @@ hipError_t launch_embed_grad(void *base, int state_dtype, const TableGeom &g, co
     char *at = static_cast<char *>(work);
     uint32_t *keys[2] = {reinterpret_cast<uint32_t *>(at + w.keys[0]), reinterpret_cast<uint32_t *>(at + w.keys[1])};
     int32_t *places[2] = {reinterpret_cast<int32_t *>(at + w.places[0]), reinterpret_cast<int32_t *>(at + w.places[1])};
-    SortPlan p{static_cast<int32_t>(g.T), 0, static_cast<uint32_t>(g.vocab), 0};
-    while ((uint64_t(g.vocab) >> (8 * p.passes)) != 0) ++p.passes;    // keys 0 .. vocab
-    int sorted = 0;
     const uint32_t N = static_cast<uint32_t>(g.N);
+    SortPlan p{static_cast<int32_t>(g.T), 0, static_cast<uint32_t>(g.vocab), 0, g.T > 0 ? N : 0};
+    while ((uint64_t(g.vocab) >> (8 * p.passes)) != 0) ++p.passes;    // keys 0 .. vocab
+    const int32_t es = state_dtype == 0 ? 4 : 2;
+    Fill fill{static_cast<char *>(base), g.peer_stride * es, g.vocab * g.width * es, 0, 0};
+    // threads of the sort's blocks, and so of those that clear: many only where one block sorts many places
+    const int threads = g.T > kOneBlock ? kTileThreads : g.T > 1024 ? 1024 : g.T > 256 || fill.table_bytes > (1 << 20) ? 256 : 64;
+    fill.blocks = accumulate ? 0 : static_cast<uint32_t>((fill.table_bytes + 16 * threads - 1) / (16 * threads));
+    const uint32_t fill_blocks = fill.blocks * N;
+    int sorted = 0;
     if (g.T > kOneBlock) {
-        const int64_t tiles = (g.T + kTile - 1) / kTile;
-        p.tiles = static_cast<uint32_t>(tiles);
-        const uint32_t grid = p.tiles * N;
+        p.tiles = static_cast<uint32_t>((g.T + kTile - 1) / kTile);
+        p.sort_blocks = p.tiles * N;
         uint32_t *bins = reinterpret_cast<uint32_t *>(at + w.bins);
+        const uint32_t launches = 2 * p.passes, each = (fill_blocks + launches - 1) / launches;
+        auto some = [&]() {                                           // how much of the clearing goes with the next launch
+            return fill_blocks - fill.first < each ? fill_blocks - fill.first : each;
+        };
         for (int pass = 0; pass < p.passes; ++pass) {
             const uint32_t *from = pass ? keys[1 - sorted] : nullptr;
             const int32_t *from_places = pass ? places[1 - sorted] : nullptr;
-            sort_count_kernel<<<grid, kTileThreads, 0, stream>>>(tokens, from, p, 8 * pass, bins);
-            sort_scan_kernel<<<N, 1024, 0, stream>>>(bins, kBins * tiles);
-            sort_move_kernel<<<grid, kTileThreads, 0, stream>>>(tokens, from, from_places, p, 8 * pass, bins, keys[sorted], places[sorted]);
+            sort_count_kernel<<<p.sort_blocks + some(), kTileThreads, 0, stream>>>(tokens, from, p, 8 * pass, bins, fill);
+            fill.first += some();
+            sort_scan_kernel<<<N, 1024, 0, stream>>>(bins, int64_t(kBins) * p.tiles);
+            sort_move_kernel<<<p.sort_blocks + some(), kTileThreads, 0, stream>>>(tokens, from, from_places, p, 8 * pass, bins, keys[sorted],
+                                                                                  places[sorted], fill);
+            fill.first += some();
             sorted = 1 - sorted;
         }
         sorted = 1 - sorted;
-    } else if (g.T > 1024) {
-        sort_block_kernel<1024, 8><<<N, 1024, 0, stream>>>(tokens, p, keys[0], places[0]);
-    } else if (g.T > 256) {
-        sort_block_kernel<256, 4><<<N, 256, 0, stream>>>(tokens, p, keys[0], places[0]);
-    } else if (g.T > 0) {
-        sort_block_kernel<64, 4><<<N, 64, 0, stream>>>(tokens, p, keys[0], places[0]);
+    } else if (p.sort_blocks + fill_blocks > 0) {
+        auto go = [&](auto kernel) { kernel<<<p.sort_blocks + fill_blocks, threads, 0, stream>>>(tokens, p, keys[0], places[0], fill); };
+        if (threads == 1024) go(sort_block_kernel<1024, 8>);
+        else if (threads == 256) go(sort_block_kernel<256, 4>);
+        else go(sort_block_kernel<64, 4>);
     }
-    ShareRecord *records = reinterpret_cast<ShareRecord *>(at + w.records);
+    Cut *cuts = reinterpret_cast<Cut *>(at + w.cuts);
     float *partials = reinterpret_cast<float *>(at + w.partials);
     auto go = [&](auto add) {
         constexpr bool ADD = decltype(add)::value;
         auto f = state_dtype == 0 ? (dy_dtype == 0 ? launch<0, 0, ADD> : launch<0, 1, ADD>) : (dy_dtype == 0 ? launch<1, 0, ADD> : launch<1, 1, ADD>);
-        f(base, g, scale, dy, dy_stride, keys[sorted], places[sorted], records, partials, stream);
+        f(base, g, scale, dy, dy_stride, keys[sorted], places[sorted], cuts, partials, stream);
     };
     if (accumulate) go(std::true_type{});
     else go(std::false_type{});
