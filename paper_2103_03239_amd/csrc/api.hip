@@ -1432,6 +1432,7 @@ int moshpit_weight_grad(moshpit_ctx *h, const void *dy_dev, int32_t dy_dtype, in
     CHECK(check_ready(h));
     CHECK(check_params(h, column, outs, ins));
     if (outs > kMostWidth) return fail(h, MOSHPIT_EINVAL, "%lld outputs: at most 2^23", (long long)outs);
+    if (dy_row_stride > (int64_t(1) << 24)) return fail(h, MOSHPIT_EINVAL, "output's gradient: row stride %lld: at most 2^24", (long long)dy_row_stride);
     CHECK(check_tokens(h, n_tokens));
     CHECK(check_codes(h, codes_dev, scales_dev, h->N * n_tokens, ins));
     CHECK(check_matrix(h, "output's gradient", dy_dev, dy_dtype, n_tokens, outs, dy_row_stride));

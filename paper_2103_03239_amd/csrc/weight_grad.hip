@@ -11,6 +11,7 @@
 
 #include "checkpoint_codes.h"
 #include "local_ops.h"
+#include "moshpit_internal.h"
 
 namespace moshpit {
 namespace {
@@ -19,24 +20,36 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-constexpr int kBlock = 256, kTileO = 128, kTileI = 128, kTokens = 32;
-// LDS row of a tile: 64 bytes more than 256, so that the 4 token rows a transposing read takes at a time lie in
-// different banks (they would all lie in the same ones otherwise)
-constexpr int kRowElems = 128 + 32;
+constexpr int kBlock = 256;              // of the join
+
+// How the sums of a matrix are tiled: WO x WI waves a block, MO x MI blocks of 32 x 32 sums a wave, K tokens a step.
+template <int WO_, int WI_, int MO_, int MI_, int K_> struct Tile {
+    static constexpr int WO = WO_, WI = WI_, MO = MO_, MI = MI_, K = K_;
+    static constexpr int O = 32 * WO * MO, I = 32 * WI * MI, THREADS = 64 * WO * WI;
+};
 
 struct Split {
     int32_t tiles_o, tiles_i, parts;     // tiles of a peer's matrix; parts of its tokens
-    int64_t tokens;                      // tokens of a part, a multiple of kTokens
+    int64_t tokens;                      // tokens of a part, a multiple of the tokens of a step
 };
 
-// 8 tokens of a column for each lane: lane l gets column l % 32 and tokens 8 * (l / 32) .. + 7 of the 16 from `tile` on.
-__device__ __forceinline__ bf16x8 operand(const uint16_t *tile)
+// A tile in LDS: rows of tokens, C columns in bfloat16.  A transposing read takes 64 bytes of 4 token rows at a time; a row is a
+// whole number of times as long as all banks together, so the 64-byte chunks of row t are stored with their number xor
+// t % 4, and the four rows' lie in different banks.
+template <int C> __device__ __forceinline__ uint32_t lds_at(int row, int col)
+{
+    return static_cast<uint32_t>(row * C + ((col >> 5 ^ (row & 3)) << 5) + (col & 31));
+}
+
+// 8 tokens of a column for each lane: lane l gets column l % 32 of the 32 from `col` on and tokens 8 * (l / 32) .. + 7 of the 16
+// from `row` on (both multiples of 32 and 16).
+template <int C> __device__ __forceinline__ bf16x8 operand(const uint16_t *tile, int row, int col)
 {
     typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
     const int lane = threadIdx.x & 63, j = lane & 15;
-    const uint16_t *at = tile + (8 * (lane >> 5) + (j >> 2)) * kRowElems + 16 * ((lane >> 4) & 1) + 4 * (j & 3);
+    const uint16_t *at = tile + lds_at<C>(8 * (lane >> 5) + (j >> 2), col + 16 * ((lane >> 4) & 1) + 4 * (j & 3)) + row * C;
     const s16x4 low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)at);
-    const s16x4 high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 4 * kRowElems));
+    const s16x4 high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(at + 4 * C));
     typedef short s16x8 __attribute__((ext_vector_type(8)));
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7));
 }
@@ -56,124 +69,294 @@ template <int PARTS> __device__ __forceinline__ void split_parts(float f, float 
     }
 }
 
-template <int YT, int ST, bool ADD, bool PARTIAL>
-__global__ __launch_bounds__(kBlock) void weight_grad_kernel(const char *__restrict__ dy, const int8_t *__restrict__ codes,
-                                                             const uint8_t *__restrict__ scales, WeightGradGeom g, Split s, char *__restrict__ base,
-                                                             float *__restrict__ partials)
+// A 128-bit value moved down by `bytes` (0 .. 16 and more), zeros from above.
+__device__ __forceinline__ u32x4 moved_down(const u32x4 &v, int bytes)
 {
-    constexpr int EY = YT == 0 ? 4 : 2, PARTS = YT == 0 ? 3 : 1;
-    __shared__ __attribute__((aligned(16))) uint16_t lds_y[PARTS][kTokens * kRowElems];
-    __shared__ __attribute__((aligned(16))) uint16_t lds_x[kTokens * kRowElems];
-    uint32_t b = blockIdx.x;
+    uint64_t low = uint64_t(v[1]) << 32 | v[0], high = uint64_t(v[3]) << 32 | v[2];
+    if (bytes >= 8) {
+        low = high;
+        high = 0;
+        bytes -= 8;
+    }
+    if (bytes >= 8) low = bytes = 0;
+    if (bytes > 0) {
+        low = low >> (8 * bytes) | high << (64 - 8 * bytes);
+        high >>= 8 * bytes;
+    }
+    return u32x4{static_cast<uint32_t>(low), static_cast<uint32_t>(low >> 32), static_cast<uint32_t>(high), static_cast<uint32_t>(high >> 32)};
+}
+
+// What a thread has in flight of a step's tiles: 8 outputs of YN tokens as they lie in memory, 16 codes of XN tokens and their scale
+// bytes.  Columns beyond a row's end: the thread reads the row's last ones instead and moves them to their place on the way into LDS;
+// tokens beyond the last: it reads the last one and puts zeros into LDS.
+template <int YT, typename T> struct Staged {
+    static constexpr int PARTS = YT == 0 ? 3 : 1, EY = YT == 0 ? 4 : 2;
+    static constexpr int TO = T::O, TI = T::I, K = T::K;
+    static constexpr int Y_THREADS = TO / 8, YR = T::THREADS / Y_THREADS, YN = K / YR;        // threads of a token, tokens at a time, times
+    static constexpr int X_THREADS = TI / 16, XR = T::THREADS / X_THREADS, XN = K / XR;
+    u32x4 y[YN][EY / 2], x[XN];
+    uint32_t byte[XN];
+
+    struct Place {
+        const char *y;                   // the part's first token: the tile's outputs, codes and scales
+        const int8_t *x;
+        const uint8_t *scale;
+        int64_t y_step, x_step, scale_step;     // bytes from a token to the next
+        uint32_t y_at, x_at, scale_at;   // this thread's, from there on
+        uint32_t y_from, x_from, scale_from;    // the same without the token
+        int32_t y_over, x_over;          // columns this thread's were moved back
+        bool whole;                      // no thread's were
+    };
+    __device__ __forceinline__ static int y_row() { return threadIdx.x / Y_THREADS; }
+    __device__ __forceinline__ static int y_col() { return threadIdx.x % Y_THREADS * 8; }
+    __device__ __forceinline__ static int x_row() { return threadIdx.x / X_THREADS; }
+    __device__ __forceinline__ static int x_col() { return threadIdx.x % X_THREADS * 16; }
+
+    // y_left, x_left: columns of the matrix from the tile's first on (the matrix has at least 8 and 16).
+    __device__ __forceinline__ static void place_thread(Place &p, int64_t y_left, int64_t x_left, int64_t c0)
+    {
+        p.whole = y_left >= TO && x_left >= TI;
+        const int32_t yl = y_left < TO ? static_cast<int32_t>(y_left) : TO, xl = x_left < TI ? static_cast<int32_t>(x_left) : TI;
+        p.y_over = y_col() + 8 > yl ? y_col() + 8 - yl : 0;
+        p.x_over = x_col() + 16 > xl ? x_col() + 16 - xl : 0;
+        const int32_t yc = y_col() - p.y_over, xc = x_col() - p.x_over;         // (may be before the tile, not before the row)
+        const int64_t group = (c0 + (x_col() < xl ? x_col() : xl - 1)) / kCheckpointGroup - c0 / kCheckpointGroup;
+        p.y_from = static_cast<uint32_t>(yc * EY);
+        p.x_from = static_cast<uint32_t>(xc);
+        p.scale_from = static_cast<uint32_t>(group);
+        p.y_at = p.y_from + static_cast<uint32_t>(y_row() * p.y_step);
+        p.x_at = p.x_from + static_cast<uint32_t>(x_row() * p.x_step);
+        p.scale_at = p.scale_from + static_cast<uint32_t>(x_row() * p.scale_step);
+    }
+
+    // The step whose first token is number t of the part's `count`.
+    __device__ __forceinline__ void load(const Place &p, int64_t t, int64_t count)
+    {
+        typedef u32x4 any_t __attribute__((aligned(1)));
+        if (t + K <= count) {
+#pragma unroll
+            for (int n = 0; n < YN; ++n) {
+                const char *from = p.y + (t + YR * n) * p.y_step + static_cast<int32_t>(p.y_at);
+#pragma unroll
+                for (int q = 0; q < EY / 2; ++q) y[n][q] = *reinterpret_cast<const any_t *>(from + 16 * q);
+            }
+#pragma unroll
+            for (int n = 0; n < XN; ++n) {
+                x[n] = *reinterpret_cast<const any_t *>(p.x + (t + XR * n) * p.x_step + static_cast<int32_t>(p.x_at));
+                byte[n] = (p.scale + (t + XR * n) * p.scale_step)[p.scale_at];
+            }
+            return;
+        }
+        const int32_t left = static_cast<int32_t>(count - t);                   // 1 .. K - 1
+#pragma unroll
+        for (int n = 0; n < YN; ++n) {
+            const int32_t row = y_row() + YR * n < left ? y_row() + YR * n : left - 1;
+            const char *from = p.y + t * p.y_step + (int64_t(row) * p.y_step + static_cast<int32_t>(p.y_from));
+#pragma unroll
+            for (int q = 0; q < EY / 2; ++q) y[n][q] = *reinterpret_cast<const any_t *>(from + 16 * q);
+        }
+#pragma unroll
+        for (int n = 0; n < XN; ++n) {
+            const int32_t row = x_row() + XR * n < left ? x_row() + XR * n : left - 1;
+            x[n] = *reinterpret_cast<const any_t *>(p.x + t * p.x_step + (int64_t(row) * p.x_step + static_cast<int32_t>(p.x_from)));
+            byte[n] = (p.scale + t * p.scale_step)[row * p.scale_step + p.scale_from];
+        }
+    }
+    // Before the step goes into LDS, where its tile or tokens are not whole.  left: tokens from the step's first on.
+    __device__ __forceinline__ void trim(const Place &p, int64_t left)
+    {
+        if (!p.whole) {
+#pragma unroll
+            for (int n = 0; n < YN; ++n) {
+                if constexpr (YT == 1) y[n][0] = moved_down(y[n][0], 2 * p.y_over);
+                else {
+                    const int over = p.y_over < 8 ? p.y_over : 8;               // 8 values of 4 bytes: 4 and more move a vector down
+                    const u32x4 none = {0, 0, 0, 0}, low = over >= 4 ? (over >= 8 ? none : y[n][1]) : y[n][0], high = over >= 4 ? none : y[n][1];
+                    const int by = over & 3;
+                    u32x4 a, b;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        a[k] = by == 0 ? low[k] : by == 1 ? (k < 3 ? low[(k + 1) & 3] : high[0]) : by == 2 ? (k < 2 ? low[(k + 2) & 3] : high[(k + 2) & 3])
+                                                                                                 : (k < 1 ? low[3] : high[(k + 3) & 3]);
+                        b[k] = by == 0 ? high[k] : k + by < 4 ? high[by == 1 ? (k + 1) & 3 : by == 2 ? (k + 2) & 3 : (k + 3) & 3] : 0u;
+                    }
+                    y[n][0] = a;
+                    y[n][1] = b;
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < XN; ++n) x[n] = moved_down(x[n], p.x_over);
+        }
+        if (left < K) {
+#pragma unroll
+            for (int n = 0; n < YN; ++n)
+                if (y_row() + YR * n >= left)
+#pragma unroll
+                    for (int q = 0; q < EY / 2; ++q) y[n][q] = u32x4{0, 0, 0, 0};
+#pragma unroll
+            for (int n = 0; n < XN; ++n)
+                if (x_row() + XR * n >= left) {
+                    x[n] = u32x4{0, 0, 0, 0};
+                    byte[n] = 1;
+                }
+        }
+    }
+
+    // Outputs of times n: into LDS, in parts.
+    __device__ __forceinline__ void store_y(int n, uint16_t *lds_y) const
+    {
+        const uint32_t at = lds_at<TO>(y_row() + YR * n, y_col());
+        if constexpr (YT == 1) *reinterpret_cast<u32x4 *>(lds_y + at) = y[n][0];
+        else {
+            float part[PARTS][8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                float f[PARTS];
+                split_parts<PARTS>(__uint_as_float(y[n][k / 4][k & 3]), f);
+#pragma unroll
+                for (int q = 0; q < PARTS; ++q) part[q][k] = f[q];
+            }
+#pragma unroll
+            for (int q = 0; q < PARTS; ++q) *reinterpret_cast<u32x4 *>(lds_y + q * K * TO + at) = Vec<1, 8>::narrow(part[q]);
+        }
+    }
+    // Codes of times n as bfloat16 values: with u = code + 128 as an unsigned byte, value = u * 2^e - 128 * 2^e, exactly.
+    __device__ __forceinline__ void store_x(int n, uint16_t *lds_x) const
+    {
+        const float factor = to_value_factor(byte[n]), less = -128.f * factor;
+        u32x4 half[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float f[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const uint32_t w = x[n][2 * h + k / 4] ^ 0x80808080u;
+                f[k] = fmaf(static_cast<float>((w >> (8 * (k & 3))) & 0xffu), factor, less);
+            }
+            half[h] = Vec<1, 8>::narrow(f);
+        }
+        // of the 16 lanes that write at a time the first 8 write the lower half first, the others the upper one: different banks
+        const int row = x_row() + XR * n, col = x_col(), first = threadIdx.x >> 3 & 1;
+        *reinterpret_cast<u32x4 *>(lds_x + lds_at<TI>(row, col) + 8 * first) = first ? half[1] : half[0];
+        *reinterpret_cast<u32x4 *>(lds_x + lds_at<TI>(row, col) + 8 - 8 * first) = first ? half[0] : half[1];
+    }
+};
+
+template <int YT, int ST, bool ADD, bool PARTIAL, typename T>
+__global__ __launch_bounds__(T::THREADS, 2)
+void weight_grad_kernel(const char *__restrict__ dy, const int8_t *__restrict__ codes, const uint8_t *__restrict__ scales, WeightGradGeom g,
+                        Split s, char *__restrict__ base, float *__restrict__ partials)
+{
+    using St = Staged<YT, T>;
+    constexpr int PARTS = St::PARTS, TO = T::O, TI = T::I, K = T::K, MO = T::MO, MI = T::MI, STEPS = K / 16;
+    constexpr int Y_ELEMS = PARTS * K * TO, ELEMS = Y_ELEMS + K * TI;
+    extern __shared__ __attribute__((aligned(16))) uint16_t lds[];       // two buffers of ELEMS
+
+    // Block b runs on die b % 8: a die takes a run of tiles, so that the tiles of a peer share its operands in the die's cache.
+    const uint32_t die = blockIdx.x % 8, each = gridDim.x / 8, more = gridDim.x % 8;
+    uint32_t b = die * each + (die < more ? die : more) + blockIdx.x / 8;
     const int32_t ti = b % s.tiles_i;
     b /= s.tiles_i;
     const int32_t to = b % s.tiles_o;
     b /= s.tiles_o;
     const int32_t part = b % s.parts;
     const int64_t peer = b / s.parts;
-    const int64_t o0 = int64_t(to) * kTileO, c0 = int64_t(ti) * kTileI;
-    const int64_t t_begin = part * s.tokens, t_end = t_begin + s.tokens < g.T ? t_begin + s.tokens : g.T;
-    const int64_t groups = checkpoint_groups(g.ins);
+    const int64_t o0 = int64_t(to) * TO, c0 = int64_t(ti) * TI;
+    const int64_t t_begin = part * s.tokens, count = t_begin + s.tokens < g.T ? s.tokens : g.T - t_begin;
+    const int64_t groups = checkpoint_groups(g.ins), row0 = peer * g.T + t_begin;
 
-    // this thread's share of a tile: 8 outputs of tokens y_row and y_row + 16, 16 codes of token x_row
-    const int y_row = threadIdx.x >> 4, y_col = (threadIdx.x & 15) * 8;
-    const int x_row = threadIdx.x >> 3, x_col = (threadIdx.x & 7) * 16;
-    const bool y_whole = o0 + y_col + 8 <= g.outs, x_whole = c0 + x_col + 16 <= g.ins;
-    float y[2][8];
-    u32x4 x;
-    uint32_t byte;
-    auto load = [&](int64_t t0) {
-#pragma unroll
-        for (int n = 0; n < 2; ++n) {
-            const int64_t t = t0 + y_row + 16 * n;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) y[n][k] = 0.f;
-            if (t >= t_end) continue;
-            const char *from = dy + ((peer * g.T + t) * g.dy_stride + o0 + y_col) * EY;
-            if (y_whole) load_elems<YT, 8>(from, y[n]);
-            else
-                for (int k = 0; k < 8; ++k)
-                    if (o0 + y_col + k < g.outs) y[n][k] = load_one<YT>(from + k * EY);
-        }
-        const int64_t t = t0 + x_row;
-        x = u32x4{0, 0, 0, 0};
-        byte = 1;
-        if (t >= t_end || c0 + x_col >= g.ins) return;
-        const int64_t row = peer * g.T + t;
-        const int8_t *from = codes + row * g.ins + c0 + x_col;
-        byte = scales[row * groups + (c0 + x_col) / kCheckpointGroup];
-        if (x_whole) {
-            typedef u32x4 any_t __attribute__((aligned(1)));
-            x = *reinterpret_cast<const any_t *>(from);
-        } else {
-            for (int k = 0; k < 16; ++k)
-                if (c0 + x_col + k < g.ins) x[k >> 2] |= (static_cast<uint32_t>(from[k]) & 0xffu) << (8 * (k & 3));
-        }
-    };
-    auto to_lds = [&]() {
-#pragma unroll
-        for (int n = 0; n < 2; ++n) {
-            float parts[PARTS][8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                float p[PARTS];
-                split_parts<PARTS>(y[n][k], p);
-#pragma unroll
-                for (int q = 0; q < PARTS; ++q) parts[q][k] = p[q];
-            }
-#pragma unroll
-            for (int q = 0; q < PARTS; ++q)
-                *reinterpret_cast<u32x4 *>(lds_y[q] + (y_row + 16 * n) * kRowElems + y_col) = Vec<1, 8>::narrow(parts[q]);
-        }
-        const float factor = to_value_factor(byte);
-#pragma unroll
-        for (int n = 0; n < 2; ++n) {
-            float f[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) f[k] = factor * code_of(x[2 * n + (k >> 2)], k & 3);
-            *reinterpret_cast<u32x4 *>(lds_x + x_row * kRowElems + x_col + 8 * n) = Vec<1, 8>::narrow(f);
-        }
-    };
+    typename St::Place place;
+    place.y_step = g.dy_stride * St::EY;
+    place.x_step = g.ins;
+    place.scale_step = groups;
+    place.y = dy + row0 * place.y_step + o0 * St::EY;
+    place.x = codes + row0 * place.x_step + c0;
+    place.scale = scales + row0 * groups + c0 / kCheckpointGroup;
+    St::place_thread(place, g.outs - o0, g.ins - c0, c0);
 
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int wo = (wave >> 1) * 64, wi = (wave & 1) * 64;
-    f32x16 acc[2][2] = {};
-    if (t_begin < t_end) load(t_begin);
-    for (int64_t t0 = t_begin; t0 < t_end; t0 += kTokens) {
-        to_lds();
+    const int wo = wave / T::WI * 32 * MO, wi = wave % T::WI * 32 * MI;
+    f32x16 acc[MO][MI] = {};
+    // Step k's tiles are requested when the products of step k - 1 begin and go into the other buffer during their second half.
+    constexpr int LATE = STEPS / 2;
+    St st;
+    auto to_lds = [&](uint32_t buffer, int part, int parts) {
+#pragma unroll
+        for (int n = part * St::YN / parts; n < (part + 1) * St::YN / parts; ++n) st.store_y(n, lds + buffer);
+#pragma unroll
+        for (int n = part * St::XN / parts; n < (part + 1) * St::XN / parts; ++n) st.store_x(n, lds + buffer + Y_ELEMS);
+    };
+    if (count > 0) {
+        st.load(place, 0, count);
+        st.trim(place, count);
+        to_lds(0, 0, 1);
         __syncthreads();
-        if (t0 + kTokens < t_end) load(t0 + kTokens);
+    }
+    uint32_t buffer = 0;
+    for (int64_t t = 0; t < count; t += K, buffer = ELEMS - buffer) {
+        const bool next = t + K < count;
+        if (next) st.load(place, t + K, count);
+        const uint16_t *tile_y = lds + buffer, *tile_x = tile_y + Y_ELEMS;
 #pragma unroll
-        for (int k0 = 0; k0 < kTokens; k0 += 16) {
-            bf16x8 xi[2];
+        for (int k = 0; k < STEPS; ++k) {
+            if (k == LATE && next && (!place.whole || t + 2 * K > count)) st.trim(place, count - t - K);
+            bf16x8 xi[MI];
 #pragma unroll
-            for (int n = 0; n < 2; ++n) xi[n] = operand(lds_x + k0 * kRowElems + wi + 32 * n);
+            for (int n = 0; n < MI; ++n) xi[n] = operand<TI>(tile_x, 16 * k, wi + 32 * n);
 #pragma unroll
-            for (int q = PARTS - 1; q >= 0; --q)
+            for (int q = PARTS - 1; q >= 0; --q) {
+                bf16x8 yo[MO];
 #pragma unroll
-                for (int m = 0; m < 2; ++m) {
-                    const bf16x8 yo = operand(lds_y[q] + k0 * kRowElems + wo + 32 * m);
+                for (int m = 0; m < MO; ++m) yo[m] = operand<TO>(tile_y + q * K * TO, 16 * k, wo + 32 * m);
 #pragma unroll
-                    for (int n = 0; n < 2; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(yo, xi[n], acc[m][n], 0, 0, 0);
-                }
+                for (int m = 0; m < MO; ++m)
+#pragma unroll
+                    for (int n = 0; n < MI; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(yo[m], xi[n], acc[m][n], 0, 0, 0);
+            }
+            if (k >= LATE && next) to_lds(ELEMS - buffer, k - LATE, STEPS - LATE);
         }
         __syncthreads();
     }
-    constexpr int ES = ST == 0 ? 4 : 2;
+    // lane l holds column l % 32 of a 32 x 32 block, rows 8 * (k / 4) + 4 * (l / 32) + k % 4
+    constexpr int ES = PARTIAL || ST == 0 ? 4 : 2;
+    char *out = PARTIAL ? reinterpret_cast<char *>(partials + (part * g.N + peer) * g.outs * g.ins) : base + peer * g.peer_stride * ES;
+    const int32_t o_left = static_cast<int32_t>(g.outs - o0 < TO ? g.outs - o0 : TO) - wo - 4 * (lane >> 5);
+    const int32_t c_left = static_cast<int32_t>(g.ins - c0 < TI ? g.ins - c0 : TI) - wi - (lane & 31);
+    const uint32_t lane_at = static_cast<uint32_t>((4 * (lane >> 5) * g.ins + (lane & 31)) * ES);
+    out += ((o0 + wo) * g.ins + c0 + wi) * ES;
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
+    for (int m = 0; m < MO; ++m)
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+        for (int n = 0; n < MI; ++n) {
+            if (32 * n >= c_left) continue;
 #pragma unroll
             for (int k = 0; k < 16; ++k) {
-                const int64_t o = o0 + wo + 32 * m + 8 * (k >> 2) + 4 * (lane >> 5) + (k & 3), c = c0 + wi + 32 * n + (lane & 31);
-                if (o >= g.outs || c >= g.ins) continue;
-                if constexpr (PARTIAL) partials[((part * g.N + peer) * g.outs + o) * g.ins + c] = acc[m][n][k];
-                else {
-                    char *at = base + (peer * g.peer_stride + o * g.ins + c) * ES;
-                    store_one<ST>(at, ADD ? load_one<ST>(at) + acc[m][n][k] : acc[m][n][k]);
-                }
+                const int row = 32 * m + 8 * (k >> 2) + (k & 3);
+                if (row >= o_left) continue;
+                char *at = out + (row * g.ins + 32 * n) * ES + lane_at;
+                if constexpr (PARTIAL) *reinterpret_cast<float *>(at) = acc[m][n][k];
+                else store_one<ST>(at, ADD ? load_one<ST>(at) + acc[m][n][k] : acc[m][n][k]);
             }
+            __builtin_amdgcn_sched_barrier(0);                       // (sums of other blocks not requested yet)
+        }
+}
+
+// Matrices of fewer than 8 outputs or 16 inputs, by one thread a sum: less than a tile's vectors.
+template <int YT, int ST, bool ADD>
+__global__ __launch_bounds__(kBlock) void thin_weight_grad_kernel(const char *__restrict__ dy, const int8_t *__restrict__ codes,
+                                                                  const uint8_t *__restrict__ scales, WeightGradGeom g, char *__restrict__ base)
+{
+    constexpr int EY = YT == 0 ? 4 : 2, ES = ST == 0 ? 4 : 2;
+    const int64_t k = int64_t(blockIdx.x) * kBlock + threadIdx.x, sums = g.outs * g.ins;
+    if (k >= g.N * sums) return;
+    const int64_t peer = k / sums, o = k % sums / g.ins, c = k % g.ins, groups = checkpoint_groups(g.ins);
+    float sum = 0.f;
+#pragma unroll 4
+    for (int64_t t = peer * g.T; t < (peer + 1) * g.T; ++t)
+        sum = fmaf(load_one<YT>(dy + (t * g.dy_stride + o) * EY),
+                   to_value_factor(scales[t * groups + c / kCheckpointGroup]) * static_cast<float>(codes[t * g.ins + c]), sum);
+    char *at = base + (peer * g.peer_stride + k % sums) * ES;
+    store_one<ST>(at, ADD ? load_one<ST>(at) + sum : sum);
 }
 
 // The parts of every sum, added in the order of their tokens.
@@ -191,65 +374,92 @@ __global__ __launch_bounds__(kBlock) void weight_grad_join_kernel(const float *_
     }
 }
 
-Split split_of(const WeightGradGeom &g, int compute_units)
+// Which tile: 256 x 256 sums read half as much LDS for a product as 128 x 128, where enough of them are there to fill the chip.
+bool wide_tiles(const WeightGradGeom &g, int compute_units)
 {
+    return g.N * ((g.outs + 255) / 256) * ((g.ins + 255) / 256) >= compute_units;
+}
+
+Split split_of(const WeightGradGeom &g, int dy_dtype, int compute_units)
+{
+    const bool wide = wide_tiles(g, compute_units);
+    const int64_t tile = wide ? 256 : 128, step = wide && dy_dtype != 0 ? 64 : 32;
     Split s;
-    s.tiles_o = static_cast<int32_t>((g.outs + kTileO - 1) / kTileO);
-    s.tiles_i = static_cast<int32_t>((g.ins + kTileI - 1) / kTileI);
-    const int64_t tiles = g.N * s.tiles_o * s.tiles_i, steps = (g.T + kTokens - 1) / kTokens;
+    s.tiles_o = static_cast<int32_t>((g.outs + tile - 1) / tile);
+    s.tiles_i = static_cast<int32_t>((g.ins + tile - 1) / tile);
+    const int64_t tiles = g.N * s.tiles_o * s.tiles_i, steps = (g.T + step - 1) / step;
     // parts of at least 8 steps until every compute unit has two blocks
-    int64_t parts = 2 * compute_units / tiles;
+    int64_t parts = wide ? 1 : 2 * compute_units / tiles;
     if (parts > steps / 8) parts = steps / 8;
     if (parts < 1) parts = 1;
     const int64_t each = (steps + parts - 1) / parts;
-    s.tokens = (each > 0 ? each : 1) * kTokens;
+    s.tokens = (each > 0 ? each : 1) * step;
     s.parts = static_cast<int32_t>(steps > 0 ? (steps + each - 1) / each : 1);
     return s;
 }
 
-template <int YT, int ST, bool ADD>
-void launch(const void *dy, const int8_t *codes, const uint8_t *scales, const WeightGradGeom &g, void *base, float *work, const Split &s,
-            hipStream_t stream)
+template <int YT, int ST, bool ADD, bool PARTIAL>
+hipError_t launch_products(const char *dy, const int8_t *codes, const uint8_t *scales, const WeightGradGeom &g, char *base, float *work, const Split &s,
+                           bool wide, hipStream_t stream)
 {
+    constexpr int WIDE_K = YT == 0 ? 32 : 64, NARROW_K = 32;
     const uint32_t blocks = static_cast<uint32_t>(g.N * s.parts * s.tiles_o * s.tiles_i);
+    auto go = [&](auto kernel, int threads, int lds) {
+        const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void *>(kernel), lds);
+        if (e != hipSuccess) return e;
+        kernel<<<blocks, threads, lds, stream>>>(dy, codes, scales, g, s, base, work);
+        return hipGetLastError();
+    };
+    constexpr int PARTS = YT == 0 ? 3 : 1;
+    if constexpr (!PARTIAL)
+        if (wide) return go(weight_grad_kernel<YT, ST, ADD, false, Tile<2, 4, 4, 2, WIDE_K>>, 512, 2 * 2 * WIDE_K * 256 * (PARTS + 1));
+    return go(weight_grad_kernel<YT, ST, ADD, PARTIAL, Tile<2, 2, 2, 2, NARROW_K>>, 256, 2 * 2 * NARROW_K * 128 * (PARTS + 1));
+}
+
+template <int YT, int ST, bool ADD>
+hipError_t launch(const void *dy, const int8_t *codes, const uint8_t *scales, const WeightGradGeom &g, void *base, float *work, const Split &s,
+                  bool wide, hipStream_t stream)
+{
     const char *from = static_cast<const char *>(dy);
     char *to = static_cast<char *>(base);
-    if (s.parts == 1) {
-        weight_grad_kernel<YT, ST, ADD, false><<<blocks, kBlock, 0, stream>>>(from, codes, scales, g, s, to, nullptr);
-        return;
+    if (g.outs < 8 || g.ins < 16) {
+        thin_weight_grad_kernel<YT, ST, ADD><<<static_cast<uint32_t>((g.N * g.outs * g.ins + kBlock - 1) / kBlock), kBlock, 0, stream>>>(
+            from, codes, scales, g, to);
+        return hipGetLastError();
     }
-    weight_grad_kernel<YT, 0, false, true><<<blocks, kBlock, 0, stream>>>(from, codes, scales, g, s, nullptr, work);
+    if (s.parts == 1) return launch_products<YT, ST, ADD, false>(from, codes, scales, g, to, nullptr, s, wide, stream);
+    const hipError_t e = launch_products<YT, 0, false, true>(from, codes, scales, g, nullptr, work, s, wide, stream);
+    if (e != hipSuccess) return e;
     const int64_t count = g.outs * g.ins, join_blocks = (g.N * count + kBlock - 1) / kBlock;
     weight_grad_join_kernel<ST, ADD><<<static_cast<uint32_t>(join_blocks < 8192 ? join_blocks : 8192), kBlock, 0, stream>>>(work, s.parts, g.N, count,
                                                                                                                             g.peer_stride, to);
+    return hipGetLastError();
 }
 
 }  // namespace
 
 bool weight_grad_fits(const WeightGradGeom &g)
 {
-    const int64_t tiles_o = (g.outs + kTileO - 1) / kTileO, tiles_i = (g.ins + kTileI - 1) / kTileI;
-    return tiles_o * tiles_i <= 0xffffffffLL / kBlock / g.N;                     // (more than one part only where that is few)
+    return (g.outs < 8 || g.ins < 16 ? (g.outs * g.ins + kBlock) / kBlock : ((g.outs + 127) / 128) * ((g.ins + 127) / 128)) <= 0xffffffffLL / kBlock / g.N;       // (more than one part only where that is few)
 }
 
 int64_t weight_grad_work_bytes(const WeightGradGeom &g, int dy_dtype, int compute_units)
 {
-    const Split s = split_of(g, compute_units);
-    return s.parts == 1 ? 0 : 4 * s.parts * g.N * g.outs * g.ins;
+    const Split s = split_of(g, dy_dtype, compute_units);
+    return s.parts == 1 || g.outs < 8 || g.ins < 16 ? 0 : 4 * s.parts * g.N * g.outs * g.ins;
 }
 
 hipError_t launch_weight_grad(const void *dy, int dy_dtype, const int8_t *codes, const uint8_t *scales, const WeightGradGeom &g, void *base,
                               int state_dtype, bool accumulate, void *work, int compute_units, hipStream_t stream)
 {
-    const Split s = split_of(g, compute_units);
+    const Split s = split_of(g, dy_dtype, compute_units);
+    const bool wide = wide_tiles(g, compute_units);
     auto go = [&](auto add) {
         constexpr bool ADD = decltype(add)::value;
         auto f = dy_dtype == 0 ? (state_dtype == 0 ? launch<0, 0, ADD> : launch<0, 1, ADD>) : (state_dtype == 0 ? launch<1, 0, ADD> : launch<1, 1, ADD>);
-        f(dy, codes, scales, g, base, static_cast<float *>(work), s, stream);
+        return f(dy, codes, scales, g, base, static_cast<float *>(work), s, wide, stream);
     };
-    if (accumulate) go(std::true_type{});
-    else go(std::false_type{});
-    return hipGetLastError();
+    return accumulate ? go(std::true_type{}) : go(std::false_type{});
 }
 
 }  // namespace moshpit
