@@ -98,7 +98,7 @@ template <int YT, typename T> struct Staged {
     uint32_t byte[XN];
 
     struct Place {
-        const char *y;                   // the part's first token: the tile's outputs, codes and scales
+        const char *y;                   // the part's first token: its outputs, codes and scales
         const int8_t *x;
         const uint8_t *scale;
         int64_t y_step, x_step, scale_step;     // bytes from a token to the next
@@ -113,17 +113,16 @@ template <int YT, typename T> struct Staged {
     __device__ __forceinline__ static int x_col() { return threadIdx.x % X_THREADS * 16; }
 
     // y_left, x_left: columns of the matrix from the tile's first on (the matrix has at least 8 and 16).
-    __device__ __forceinline__ static void place_thread(Place &p, int64_t y_left, int64_t x_left, int64_t c0)
+    __device__ __forceinline__ static void place_thread(Place &p, int64_t y_left, int64_t x_left, int64_t o0, int64_t c0)
     {
         p.whole = y_left >= TO && x_left >= TI;
         const int32_t yl = y_left < TO ? static_cast<int32_t>(y_left) : TO, xl = x_left < TI ? static_cast<int32_t>(x_left) : TI;
         p.y_over = y_col() + 8 > yl ? y_col() + 8 - yl : 0;
         p.x_over = x_col() + 16 > xl ? x_col() + 16 - xl : 0;
         const int32_t yc = y_col() - p.y_over, xc = x_col() - p.x_over;         // (may be before the tile, not before the row)
-        const int64_t group = (c0 + (x_col() < xl ? x_col() : xl - 1)) / kCheckpointGroup - c0 / kCheckpointGroup;
-        p.y_from = static_cast<uint32_t>(yc * EY);
-        p.x_from = static_cast<uint32_t>(xc);
-        p.scale_from = static_cast<uint32_t>(group);
+        p.y_from = static_cast<uint32_t>((o0 + yc) * EY);
+        p.x_from = static_cast<uint32_t>(c0 + xc);
+        p.scale_from = static_cast<uint32_t>((c0 + (x_col() < xl ? x_col() : xl - 1)) / kCheckpointGroup);
         p.y_at = p.y_from + static_cast<uint32_t>(y_row() * p.y_step);
         p.x_at = p.x_from + static_cast<uint32_t>(x_row() * p.x_step);
         p.scale_at = p.scale_from + static_cast<uint32_t>(x_row() * p.scale_step);
@@ -136,14 +135,14 @@ template <int YT, typename T> struct Staged {
         if (t + K <= count) {
 #pragma unroll
             for (int n = 0; n < YN; ++n) {
-                const char *from = p.y + (t + YR * n) * p.y_step + static_cast<int32_t>(p.y_at);
+                const char *from = p.y + (t + YR * n) * p.y_step + p.y_at;
 #pragma unroll
                 for (int q = 0; q < EY / 2; ++q) y[n][q] = *reinterpret_cast<const any_t *>(from + 16 * q);
             }
 #pragma unroll
             for (int n = 0; n < XN; ++n) {
-                x[n] = *reinterpret_cast<const any_t *>(p.x + (t + XR * n) * p.x_step + static_cast<int32_t>(p.x_at));
-                byte[n] = (p.scale + (t + XR * n) * p.scale_step)[p.scale_at];
+                x[n] = *reinterpret_cast<const any_t *>(p.x + (t + XR * n) * p.x_step + p.x_at);
+                byte[n] = *(p.scale + (t + XR * n) * p.scale_step + p.scale_at);
             }
             return;
         }
@@ -151,14 +150,14 @@ template <int YT, typename T> struct Staged {
 #pragma unroll
         for (int n = 0; n < YN; ++n) {
             const int32_t row = y_row() + YR * n < left ? y_row() + YR * n : left - 1;
-            const char *from = p.y + t * p.y_step + (int64_t(row) * p.y_step + static_cast<int32_t>(p.y_from));
+            const char *from = p.y + t * p.y_step + (int64_t(row) * p.y_step + p.y_from);
 #pragma unroll
             for (int q = 0; q < EY / 2; ++q) y[n][q] = *reinterpret_cast<const any_t *>(from + 16 * q);
         }
 #pragma unroll
         for (int n = 0; n < XN; ++n) {
             const int32_t row = x_row() + XR * n < left ? x_row() + XR * n : left - 1;
-            x[n] = *reinterpret_cast<const any_t *>(p.x + t * p.x_step + (int64_t(row) * p.x_step + static_cast<int32_t>(p.x_from)));
+            x[n] = *reinterpret_cast<const any_t *>(p.x + t * p.x_step + (int64_t(row) * p.x_step + p.x_from));
             byte[n] = (p.scale + t * p.scale_step)[row * p.scale_step + p.scale_from];
         }
     }
@@ -269,53 +268,71 @@ void weight_grad_kernel(const char *__restrict__ dy, const int8_t *__restrict__ 
     place.y_step = g.dy_stride * St::EY;
     place.x_step = g.ins;
     place.scale_step = groups;
-    place.y = dy + row0 * place.y_step + o0 * St::EY;
-    place.x = codes + row0 * place.x_step + c0;
-    place.scale = scales + row0 * groups + c0 / kCheckpointGroup;
-    St::place_thread(place, g.outs - o0, g.ins - c0, c0);
+    place.y = dy + row0 * place.y_step;
+    place.x = codes + row0 * place.x_step;
+    place.scale = scales + row0 * groups;
+    St::place_thread(place, g.outs - o0, g.ins - c0, o0, c0);
 
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int wo = wave / T::WI * 32 * MO, wi = wave % T::WI * 32 * MI;
     f32x16 acc[MO][MI] = {};
-    // Step k's tiles are requested when the products of step k - 1 begin and go into the other buffer during their second half.
-    constexpr int LATE = STEPS / 2;
+    // The products of a step are taken in UNITS of MO * MI matrix instructions: 16 tokens and one part of dy.  A unit's operands
+    // are read from LDS before the products of the unit before it.  Step k + 1's tiles go into the other buffer between the
+    // products of the second half of step k, and step k + 2's are requested right after.
+    constexpr int UNITS = STEPS * PARTS, LATE = UNITS / 2;
     St st;
+    bf16x8 xi[2][MI], yo[2][MO];
+    auto read = [&](uint32_t buffer, int u) {
+        const uint16_t *tile_y = lds + buffer + (PARTS - 1 - u % PARTS) * K * TO, *tile_x = lds + buffer + Y_ELEMS;
+        const int k = u / PARTS;
+        if (u % PARTS == 0)
+#pragma unroll
+            for (int n = 0; n < MI; ++n) xi[k & 1][n] = operand<TI>(tile_x, 16 * k, wi + 32 * n);
+#pragma unroll
+        for (int m = 0; m < MO; ++m) yo[u & 1][m] = operand<TO>(tile_y, 16 * k, wo + 32 * m);
+    };
+    auto multiply = [&](int u) {
+#pragma unroll
+        for (int m = 0; m < MO; ++m)
+#pragma unroll
+            for (int n = 0; n < MI; ++n)
+                acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(yo[u & 1][m], xi[u / PARTS & 1][n], acc[m][n], 0, 0, 0);
+    };
     auto to_lds = [&](uint32_t buffer, int part, int parts) {
 #pragma unroll
         for (int n = part * St::YN / parts; n < (part + 1) * St::YN / parts; ++n) st.store_y(n, lds + buffer);
 #pragma unroll
         for (int n = part * St::XN / parts; n < (part + 1) * St::XN / parts; ++n) st.store_x(n, lds + buffer + Y_ELEMS);
     };
+    uint32_t buffer = 0;
+    int64_t t = 0;
     if (count > 0) {
         st.load(place, 0, count);
         st.trim(place, count);
         to_lds(0, 0, 1);
+        if (K < count) st.load(place, K, count);
         __syncthreads();
     }
-    uint32_t buffer = 0;
-    for (int64_t t = 0; t < count; t += K, buffer = ELEMS - buffer) {
-        const bool next = t + K < count;
-        if (next) st.load(place, t + K, count);
-        const uint16_t *tile_y = lds + buffer, *tile_x = tile_y + Y_ELEMS;
+    for (; t + K < count; t += K, buffer = ELEMS - buffer) {
+        read(buffer, 0);
 #pragma unroll
-        for (int k = 0; k < STEPS; ++k) {
-            if (k == LATE && next && (!place.whole || t + 2 * K > count)) st.trim(place, count - t - K);
-            bf16x8 xi[MI];
-#pragma unroll
-            for (int n = 0; n < MI; ++n) xi[n] = operand<TI>(tile_x, 16 * k, wi + 32 * n);
-#pragma unroll
-            for (int q = PARTS - 1; q >= 0; --q) {
-                bf16x8 yo[MO];
-#pragma unroll
-                for (int m = 0; m < MO; ++m) yo[m] = operand<TO>(tile_y + q * K * TO, 16 * k, wo + 32 * m);
-#pragma unroll
-                for (int m = 0; m < MO; ++m)
-#pragma unroll
-                    for (int n = 0; n < MI; ++n) acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(yo[m], xi[n], acc[m][n], 0, 0, 0);
-            }
-            if (k >= LATE && next) to_lds(ELEMS - buffer, k - LATE, STEPS - LATE);
+        for (int u = 0; u < UNITS; ++u) {
+            if (u == LATE && (!place.whole || t + 2 * K > count)) st.trim(place, count - t - K);
+            if (u + 1 < UNITS) read(buffer, u + 1);
+            multiply(u);
+            if (u >= LATE) to_lds(ELEMS - buffer, u - LATE, UNITS - LATE);
         }
+        if (t + 2 * K < count) st.load(place, t + 2 * K, count);
         __syncthreads();
+    }
+    if (count > 0) {
+        read(buffer, 0);
+#pragma unroll
+        for (int u = 0; u < UNITS; ++u) {
+            if (u + 1 < UNITS) read(buffer, u + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(u);
+        }
     }
     // lane l holds column l % 32 of a 32 x 32 block, rows 8 * (k / 4) + 4 * (l / 32) + k % 4
     constexpr int ES = PARTIAL || ST == 0 ? 4 : 2;
