@@ -1322,8 +1322,8 @@ int check_matrix(moshpit_ctx *h, const char *what, const void *dev, int32_t dtyp
     if (rows > 0 && !dev) return fail(h, MOSHPIT_EINVAL, "%s: pointer is NULL", what);
     if (reinterpret_cast<uintptr_t>(dev) % (dtype == MOSHPIT_F32 ? 4 : 2) != 0)
         return fail(h, MOSHPIT_EINVAL, "%s: pointer is not aligned to the element size", what);
-    if (row_stride < width || row_stride > (int64_t(1) << 40))
-        return fail(h, MOSHPIT_EINVAL, "%s: row stride %lld for rows of %lld", what, (long long)row_stride, (long long)width);
+    if (row_stride < width || row_stride > (int64_t(1) << 29))
+        return fail(h, MOSHPIT_EINVAL, "%s: row stride %lld for rows of %lld (at most 2^29)", what, (long long)row_stride, (long long)width);
     return MOSHPIT_OK;
 }
 

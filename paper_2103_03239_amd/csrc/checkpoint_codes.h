@@ -31,13 +31,14 @@ __device__ __forceinline__ float to_value_factor(uint32_t byte)
     return __uint_as_float(byte == kScaleNaN ? 0x7fc00000u : byte << 23);
 }
 
-// Four codes in the bytes of a word, lowest first.
+// Four codes in the bytes of a word, lowest first.  Adding 1.5 * 2^23 rounds to whole numbers, ties to even, and leaves the
+// code, as a signed byte, in the sum's lowest bits.
 __device__ __forceinline__ uint32_t pack_codes(const float *x, float factor)
 {
-    uint32_t w = 0;
+    uint32_t u[4];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) w |= (static_cast<uint32_t>(static_cast<int>(rintf(x[k] * factor))) & 0xffu) << (8 * k);
-    return w;
+    for (int k = 0; k < 4; ++k) u[k] = __float_as_uint(fmaf(x[k], factor, 12582912.f));
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(u[3], u[2], 0x00000400), __builtin_amdgcn_perm(u[1], u[0], 0x00000400), 0x05040100);
 }
 
 __device__ __forceinline__ float code_of(uint32_t w, int k) { return static_cast<float>(static_cast<int>(w << (24 - 8 * k)) >> 24); }

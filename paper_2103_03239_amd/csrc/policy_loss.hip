@@ -39,19 +39,49 @@ __device__ __forceinline__ TopSum join(const TopSum &a, const TopSum &b)
     return {top, a.sum * fa + b.sum * fb};
 }
 
+// v of a lane further down the wave (CTRL: a DPP control), `old` where there is none.
+template <int CTRL, int ROWS> __device__ __forceinline__ float from_lane(float old, float v)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, old), __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false));
+}
+// A whole wave's largest value and sum, in the same order every time: within rows of 16 lanes, then across them.
+__device__ __forceinline__ float wave_top(float v)
+{
+    v = fmaxf(v, from_lane<0x111, 0xf>(-INFINITY, v));
+    v = fmaxf(v, from_lane<0x112, 0xf>(-INFINITY, v));
+    v = fmaxf(v, from_lane<0x114, 0xf>(-INFINITY, v));
+    v = fmaxf(v, from_lane<0x118, 0xf>(-INFINITY, v));
+    v = fmaxf(v, from_lane<0x142, 0xa>(-INFINITY, v));
+    v = fmaxf(v, from_lane<0x143, 0xc>(-INFINITY, v));
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+}
+__device__ __forceinline__ float wave_sum(float v)
+{
+    v += from_lane<0x111, 0xf>(0.f, v);
+    v += from_lane<0x112, 0xf>(0.f, v);
+    v += from_lane<0x114, 0xf>(0.f, v);
+    v += from_lane<0x118, 0xf>(0.f, v);
+    v += from_lane<0x142, 0xa>(0.f, v);
+    v += from_lane<0x143, 0xc>(0.f, v);
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+}
+__device__ __forceinline__ TopSum wave_join(const TopSum &t)
+{
+    const float top = wave_top(t.top);
+    return {top, wave_sum(t.sum * (t.top == top ? 1.f : exp_above(t.top, top)))};
+}
+
+// The first wave gets the block's.
 template <int THREADS>
 __device__ __forceinline__ TopSum block_join(TopSum t)
 {
     constexpr int WAVES = THREADS / 64;
     __shared__ TopSum of_wave[WAVES];
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) t = join(t, TopSum{__shfl_xor(t.top, off, 64), __shfl_xor(t.sum, off, 64)});
+    t = wave_join(t);
     if constexpr (WAVES > 1) {
         if ((threadIdx.x & 63) == 0) of_wave[threadIdx.x >> 6] = t;
         __syncthreads();
-        t = of_wave[0];
-#pragma unroll
-        for (int w = 1; w < WAVES; ++w) t = join(t, of_wave[w]);
+        if (threadIdx.x < 64) t = wave_join(threadIdx.x < WAVES ? of_wave[threadIdx.x] : TopSum{-INFINITY, 0.f});
     }
     return t;
 }
@@ -84,20 +114,45 @@ template <int DT> __device__ __forceinline__ void widen_vec(const u32x4 &m, floa
     } else Vec<1, 8>::widen(m, f);
 }
 
-template <int VE> __device__ __forceinline__ void add_values(TopSum &t, const float (&f)[VE])
+template <int VE> __device__ __forceinline__ float largest(const float (&f)[VE])
 {
     float top = f[0];
 #pragma unroll
     for (int k = 1; k < VE; ++k) top = fmaxf(top, f[k]);
+    return top;
+}
+
+// The sum of exp(f - m), with less = -m log2 e: one fused multiply-add and one exponential a value.  Its rounding of m log2 e is
+// the same for all values of a row, so it cancels in exp(z - m) / sum and is one rounding of m in the log-probability.
+template <int VE> __device__ __forceinline__ float sum_exp(const float (&f)[VE], float less)
+{
+    float e[VE];
+#pragma unroll
+    for (int k = 0; k < VE; ++k) e[k] = __builtin_amdgcn_exp2f(fmaf(f[k], kLog2e, less));
+#pragma unroll
+    for (int w = VE / 2; w > 0; w /= 2)
+#pragma unroll
+        for (int k = 0; k < w; ++k) e[k] += e[k + w];
+    return e[0];
+}
+// What `less` is for a largest value: -inf alone gives exp(-inf) = 0.
+__device__ __forceinline__ float less_of(float top) { return top == -INFINITY ? 0.f : -top * kLog2e; }
+
+template <int VE> __device__ __forceinline__ void add_values(TopSum &t, const float (&f)[VE])
+{
+    const float top = largest(f);
     if (top > t.top) {
         t.sum *= t.top == -INFINITY ? 0.f : exp_above(t.top, top);
         t.top = top;
     }
-    const float m = t.top == -INFINITY ? 0.f : t.top;      // (-inf alone: exp(-inf) = 0)
-    float sum = 0.f;
+    t.sum += sum_exp(f, less_of(t.top));
+}
+
+// What was made of these registers is not to be kept for the next pass over them: the row as it came is all there is room for.
+template <int N> __device__ __forceinline__ void keep_packed(u32x4 (&held)[N])
+{
 #pragma unroll
-    for (int k = 0; k < VE; ++k) sum += exp_above(f[k], m);
-    t.sum += sum;
+    for (int v = 0; v < N; ++v) asm volatile("" : "+v"(held[v]));
 }
 
 struct RowPlace {
@@ -141,7 +196,7 @@ __device__ __forceinline__ void store_zeros(char *grad, int64_t n)
 // One row a block, in registers.  The gradient may take the logits' place (here and below): every element is read
 // before it is written, by the same thread.
 template <int DT, int THREADS, int VECS>
-__global__ __launch_bounds__(THREADS) void policy_row_kernel(const char *logits, RowPlace at, const int32_t *__restrict__ tokens,
+__global__ __launch_bounds__(THREADS, VECS == 8 ? 8 : 4) void policy_row_kernel(const char *logits, RowPlace at, const int32_t *__restrict__ tokens,
                                                              PolicyTerms p, char *grad, int64_t grad_stride,
                                                              float *__restrict__ logp, RowTerms *__restrict__ terms)
 {
@@ -169,23 +224,44 @@ __global__ __launch_bounds__(THREADS) void policy_row_kernel(const char *logits,
         if (i < s.count) held[v] = load_vec<true, u32x4>(s.vectors + int64_t(i) * 16);
     }
     if (static_cast<int32_t>(threadIdx.x) < s.head + s.tail) single = load_one<DT>(from + s.single(threadIdx.x) * ES);
-    TopSum t{single, single == -INFINITY ? 0.f : 1.f};
+    // first this thread's largest value, then its sum: its values are all here
+    TopSum t{single, 0.f};
 #pragma unroll
     for (int v = 0; v < VECS; ++v) {
         if (v * THREADS + static_cast<int32_t>(threadIdx.x) >= s.count) continue;
         float f[VE];
         widen_vec<DT>(held[v], f);
-        add_values(t, f);
+        t.top = fmaxf(t.top, largest(f));
     }
+    keep_packed(held);
+    const float own_less = less_of(t.top);
+    t.sum = __builtin_amdgcn_exp2f(fmaf(single, kLog2e, own_less));
+#pragma unroll
+    for (int v = 0; v < VECS; ++v) {
+        if (v * THREADS + static_cast<int32_t>(threadIdx.x) >= s.count) continue;
+        float f[VE];
+        widen_vec<DT>(held[v], f);
+        t.sum += sum_exp(f, own_less);
+    }
+    keep_packed(held);
     t = block_join<THREADS>(t);
-    const float lp = z_token - t.top - logf(t.sum);
-    RowTerms mine;
-    const float slope = row_terms(p, row, w, lp, mine);
-    if (threadIdx.x == 0) {
-        logp[row] = lp;
-        terms[row] = mine;
+    __shared__ float of_row[3];
+    if (threadIdx.x < 64) {                                           // (the same for all its lanes)
+        const float lp = z_token - t.top - logf(t.sum);
+        RowTerms mine;
+        const float slope = row_terms(p, row, w, lp, mine);
+        if (threadIdx.x == 0) {
+            logp[row] = lp;
+            terms[row] = mine;
+            of_row[0] = slope;
+            of_row[1] = -slope / t.sum;
+            of_row[2] = -t.top * kLog2e;                              // (a row of -inf alone: NaN)
+        }
     }
-    const float factor = -slope / t.sum;
+    __syncthreads();
+    const float slope = of_row[0], factor = of_row[1], less = of_row[2];
+    const int32_t token_vec = static_cast<int32_t>((token - s.head) >> (DT == 0 ? 2 : 3));       // (may be none of the whole ones)
+    const int32_t token_elem = static_cast<int32_t>(token - s.head) & (VE - 1);
 #pragma unroll
     for (int v = 0; v < VECS; ++v) {
         const int32_t i = v * THREADS + threadIdx.x;
@@ -193,18 +269,17 @@ __global__ __launch_bounds__(THREADS) void policy_row_kernel(const char *logits,
         float f[VE];
         widen_vec<DT>(held[v], f);
 #pragma unroll
-        for (int k = 0; k < VE; ++k) f[k] = factor * exp_above(f[k], t.top);
-        const int64_t e = s.head + int64_t(i) * VE;
-        if (token >= e && token < e + VE) {
+        for (int k = 0; k < VE; ++k) f[k] = factor * __builtin_amdgcn_exp2f(fmaf(f[k], kLog2e, less));
+        if (i == token_vec) {
 #pragma unroll
             for (int k = 0; k < VE; ++k)
-                if (token == e + k) f[k] += slope;
+                if (k == token_elem) f[k] += slope;
         }
-        store_elems<DT, VE, true>(to + e * ES, f);
+        store_elems<DT, VE, true>(to + (s.head + i * VE) * ES, f);
     }
     if (static_cast<int32_t>(threadIdx.x) < s.head + s.tail) {
         const int64_t e = s.single(threadIdx.x);
-        store_one<DT>(to + e * ES, factor * exp_above(single, t.top) + (token == e ? slope : 0.f));
+        store_one<DT>(to + e * ES, factor * __builtin_amdgcn_exp2f(fmaf(single, kLog2e, less)) + (token == e ? slope : 0.f));
     }
 }
 
@@ -261,9 +336,7 @@ __device__ __forceinline__ TopSum joined(const TopSum *__restrict__ sums, int32_
 {
     TopSum t{-INFINITY, 0.f};
     for (int32_t k = threadIdx.x & 63; k < slices; k += 64) t = join(t, sums[k]);
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) t = join(t, TopSum{__shfl_xor(t.top, off, 64), __shfl_xor(t.sum, off, 64)});
-    return t;
+    return wave_join(t);
 }
 
 template <int DT, int THREADS>
@@ -294,7 +367,7 @@ __global__ __launch_bounds__(THREADS) void policy_slice_kernel(const char *logit
         logp[row] = lp;
         terms[row] = mine;
     }
-    const float factor = -slope / t.sum;
+    const float factor = -slope / t.sum, less = -t.top * kLog2e;
     const char *from = logits + (row * at.stride + begin) * ES;
     const Slice<DT> s(from, end - begin);
     for (int32_t i0 = threadIdx.x; i0 < s.count; i0 += THREADS * kBatch) {
@@ -310,13 +383,18 @@ __global__ __launch_bounds__(THREADS) void policy_slice_kernel(const char *logit
             widen_vec<DT>(m[u], f);
             const int64_t e = s.head + int64_t(i) * VE;
 #pragma unroll
-            for (int k = 0; k < VE; ++k) f[k] = factor * exp_above(f[k], t.top) + (token == begin + e + k ? slope : 0.f);
+            for (int k = 0; k < VE; ++k) f[k] = factor * __builtin_amdgcn_exp2f(fmaf(f[k], kLog2e, less));
+            if (token >= begin + e && token < begin + e + VE) {
+#pragma unroll
+                for (int k = 0; k < VE; ++k)
+                    if (token == begin + e + k) f[k] += slope;
+            }
             store_elems<DT, VE, true>(to + e * ES, f);
         }
     }
     for (int k = threadIdx.x; k < s.head + s.tail; k += THREADS) {
         const int64_t e = s.single(k);
-        store_one<DT>(to + e * ES, factor * exp_above(load_one<DT>(from + e * ES), t.top) + (token == begin + e ? slope : 0.f));
+        store_one<DT>(to + e * ES, factor * __builtin_amdgcn_exp2f(fmaf(load_one<DT>(from + e * ES), kLog2e, less)) + (token == begin + e ? slope : 0.f));
     }
 }
 
