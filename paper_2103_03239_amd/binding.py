@@ -51,6 +51,16 @@ class Schedule:
 
 
 _lib = None
+_torch_module = None
+
+
+def _torch():
+    """torch, imported at the first call that needs it (an import statement per call costs as much as a kernel's launch)."""
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
 
 
 def load_library() -> ctypes.CDLL:
@@ -320,11 +330,12 @@ class Moshpit:
                     "set_tuning")
 
     # -- the local step of language-model peers --------------------------------
-    def _type_code(self, dtype) -> int:
-        import torch
-        if dtype == torch.float32:
+    @staticmethod
+    def _type_code(dtype) -> int:
+        torch = _torch()
+        if dtype is torch.float32:
             return F32
-        if dtype == torch.bfloat16:
+        if dtype is torch.bfloat16:
             return BF16
         raise ValueError("activations must be float32 or bfloat16")
 
@@ -344,13 +355,13 @@ class Moshpit:
 
     def _tokens(self, tokens):
         """tokens: int32 [N, T] on the GPU, contiguous."""
-        import torch
+        torch = _torch()
         if tokens.dtype != torch.int32 or tokens.dim() != 2 or tokens.shape[0] != self.N or not tokens.is_cuda or not tokens.is_contiguous():
             raise ValueError("tokens must be a contiguous int32 GPU tensor [N, T]")
         return tokens.data_ptr(), tokens.shape[1]
 
     def _per_token(self, x, T: int, name: str):
-        import torch
+        torch = _torch()
         if x.dtype != torch.float32 or tuple(x.shape) != (self.N, T) or not x.is_cuda or not x.is_contiguous():
             raise ValueError(f"{name} must be a contiguous float32 GPU tensor [N, {T}]")
         return x.data_ptr()
@@ -358,7 +369,7 @@ class Moshpit:
     def embed(self, tokens, column: int, vocab: int, width: int, scale: float = 1.0, out=None, dtype=None):
         """Token embeddings [N, T, width] from the tables [vocab, width] that start at parameter `column` of
         every peer.  out: tensor to write; without it a new one of `dtype` (the state's if not given)."""
-        import torch
+        torch = _torch()
         tp, T = self._tokens(tokens)
         if out is None:
             dtype = dtype or (torch.float32 if self.dtype == F32 else torch.bfloat16)
@@ -379,7 +390,7 @@ class Moshpit:
 
     def checkpoint(self, x):
         """x [N, T, width] in 8 bits: (codes int8 [N, T, width], scales uint8 [N, T, ceil(width / 32)])."""
-        import torch
+        torch = _torch()
         xp, code, T, width, stride = self._rows(x, "x")
         codes = torch.empty((self.N, T, width), dtype=torch.int8, device=x.device)
         scales = torch.empty((self.N, T, -(-width // 32)), dtype=torch.uint8, device=x.device)
@@ -388,7 +399,7 @@ class Moshpit:
         return codes, scales
 
     def _saved(self, codes, scales):
-        import torch
+        torch = _torch()
         if codes.dtype != torch.int8 or scales.dtype != torch.uint8 or codes.dim() != 3 or codes.shape[0] != self.N or \
                 tuple(scales.shape) != (*codes.shape[:2], -(-codes.shape[2] // 32)) or not codes.is_cuda or not scales.is_cuda or \
                 not codes.is_contiguous() or not scales.is_contiguous():
@@ -397,7 +408,7 @@ class Moshpit:
 
     def checkpoint_restore(self, codes, scales, dtype=None, out=None):
         """The activations that codes and scales stand for, in `dtype` (float32 if not given) or into `out`."""
-        import torch
+        torch = _torch()
         cp, sp = self._saved(codes, scales)
         if out is None:
             out = torch.empty(codes.shape, dtype=dtype or torch.float32, device=codes.device)
@@ -418,7 +429,7 @@ class Moshpit:
 
     def token_logp(self, logits, tokens):
         """Log-probabilities [N, T] (float32) of `tokens` under logits [N, T, vocab]."""
-        import torch
+        torch = _torch()
         tp, T = self._tokens(tokens)
         zp, code, _, vocab, stride = self._rows(logits, "logits", T)
         logp = torch.empty((self.N, T), dtype=torch.float32, device=logits.device)
@@ -429,7 +440,7 @@ class Moshpit:
                     kl_coef: float = 0.0, grad=None):
         """Clipped policy loss with a KL term: (stats [N, 3] = loss, KL, clipped weight of every peer; logp [N, T]).  The
         logits' gradient goes into `grad` (like logits; None: into the logits themselves)."""
-        import torch
+        torch = _torch()
         tp, T = self._tokens(tokens)
         zp, code, _, vocab, stride = self._rows(logits, "logits", T)
         grad = logits if grad is None else grad

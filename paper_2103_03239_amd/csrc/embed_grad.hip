@@ -490,6 +490,67 @@ __global__ __launch_bounds__(kBlock) void embed_grad_kernel(const uint32_t *__re
     else columns.store_partial(head ? slot : slot + g.width, acc);         // the row goes on in the next share
 }
 
+// Few places and small tables in one launch, without a sort: a wave has kScanRows rows of a table and a column slice, looks at
+// all tokens of the peer, four a lane, and takes those of each of its rows in ascending order of their places.
+constexpr int kScanRows = 16, kScanPlaces = 256;
+
+template <int ST, int YT, int VE, bool ADD>
+__global__ __launch_bounds__(kBlock) void embed_grad_scan_kernel(const int32_t *__restrict__ tokens, const char *__restrict__ dy, int64_t dy_stride,
+                                                                 char *__restrict__ base, TableGeom g, ShareGeom s, float scale)
+{
+    constexpr int ES = ST == 0 ? 4 : 2, EY = YT == 0 ? 4 : 2, CHUNKS = kScanPlaces / kWave;
+    const uint32_t peer = blockIdx.x / s.blocks;
+    const uint32_t part = blockIdx.x % s.blocks * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t run = part / s.slices, slice = part % s.slices;
+    const uint32_t vocab = static_cast<uint32_t>(g.vocab), row0 = run * kScanRows;
+    if (row0 >= vocab) return;
+    const uint32_t rows = vocab - row0 < kScanRows ? vocab - row0 : kScanRows;
+    const int lane = threadIdx.x & 63;
+    uint32_t mine[CHUNKS];                                            // a token's row of this wave's, or any number from `rows` on
+    uint64_t any = 0;
+#pragma unroll
+    for (int q = 0; q < CHUNKS; ++q) {
+        const int64_t at = q * kWave + lane;
+        mine[q] = at < g.T ? static_cast<uint32_t>(tokens[peer * g.T + at]) - row0 : rows;
+        any |= __ballot(mine[q] < rows);
+    }
+    const Columns<ST, YT, VE, ADD> columns(g.width, slice);
+    char *table = base + (peer * g.peer_stride + int64_t(row0) * g.width) * ES;
+    const char *from = dy + peer * g.T * dy_stride * EY;
+    if (any == 0 && ADD) return;
+    for (uint32_t r = 0; r < rows; ++r) {
+        float acc[VE] = {};
+        bool some = false;
+        if (any != 0) {
+#pragma unroll
+            for (int q = 0; q < CHUNKS; ++q) {
+                uint64_t places = __ballot(mine[q] == r);
+                some |= places != 0;
+                while (places != 0) {
+                    Raw<YT, VE> v[kBatch];
+                    uint64_t rest = places;
+#pragma unroll
+                    for (int u = 0; u < kBatch; ++u) {                // the lowest kBatch of them; where there are fewer, the last one again
+                        columns.load(from + int64_t(q * kWave + __builtin_ctzll(rest)) * dy_stride * EY, v[u]);
+                        if ((rest & (rest - 1)) != 0) rest &= rest - 1;
+                    }
+#pragma unroll
+                    for (int u = 0; u < kBatch; ++u) {
+                        if (places == 0) break;
+#pragma unroll
+                        for (int e = 0; e < VE; ++e) acc[e] += v[u][e];
+                        places &= places - 1;
+                    }
+                }
+            }
+        }
+        if (!some && ADD) continue;
+#pragma unroll
+        for (int e = 0; e < VE; ++e) acc[e] *= scale;
+        columns.store(table + int64_t(r) * g.width * ES, acc);
+    }
+}
+
 // Rows cut by shares: the share in which such a row ends adds its partial sums, in the order of the shares.
 template <int ST, bool ADD>
 __global__ __launch_bounds__(kBlock) void embed_grad_join_kernel(char *__restrict__ base, TableGeom g, ShareGeom s, float scale,
@@ -613,10 +674,31 @@ void launch_sums(void *base, const TableGeom &g, float scale, const void *dy, in
     embed_grad_join_kernel<ST, ADD><<<joins, kBlock, 0, stream>>>(static_cast<char *>(base), g, s, scale, cuts, partials);
 }
 
-template <int ST, int YT, bool ADD>
-void launch(void *base, const TableGeom &g, float scale, const void *dy, int64_t dy_stride, const uint32_t *keys, const int32_t *places,
-            Cut *cuts, float *partials, hipStream_t stream)
+// Without a sort: few places, and tables that are written in about the time of a launch.
+bool scan_does(const TableGeom &g) { return g.T > 0 && g.T <= kScanPlaces && g.N * g.vocab * g.width <= (int64_t(1) << 23); }
+
+template <int ST, int YT, int VE, bool ADD>
+void launch_scan(void *base, const TableGeom &g, const int32_t *tokens, float scale, const void *dy, int64_t dy_stride, hipStream_t stream)
 {
+    ShareGeom s{(g.vocab + kScanRows - 1) / kScanRows, static_cast<uint32_t>((g.width + kWave * VE - 1) / (kWave * VE)), 0};
+    s.blocks = static_cast<uint32_t>((s.shares * s.slices + kWaves - 1) / kWaves);
+    embed_grad_scan_kernel<ST, YT, VE, ADD><<<static_cast<uint32_t>(s.blocks * g.N), kBlock, 0, stream>>>(
+        tokens, static_cast<const char *>(dy), dy_stride, static_cast<char *>(base), g, s, scale);
+}
+
+template <int ST, int YT, bool ADD>
+void launch(void *base, const TableGeom &g, const int32_t *tokens, float scale, const void *dy, int64_t dy_stride, const uint32_t *keys,
+            const int32_t *places, Cut *cuts, float *partials, hipStream_t stream)
+{
+    if (scan_does(g)) {
+        auto scan = [&](auto f) { f(base, g, tokens, scale, dy, dy_stride, stream); };
+        switch (lane_elems(g, ST)) {
+        case 1: return scan(launch_scan<ST, YT, 1, ADD>);
+        case 2: return scan(launch_scan<ST, YT, 2, ADD>);
+        case 4: return scan(launch_scan<ST, YT, 4, ADD>);
+        default: return scan(launch_scan<ST, YT, ST == 0 ? 4 : 8, ADD>);
+        }
+    }
     auto go = [&](auto f) { f(base, g, scale, dy, dy_stride, keys, places, cuts, partials, stream); };
     switch (lane_elems(g, ST)) {
     case 1: return go(launch_sums<ST, YT, 1, ADD>);
@@ -654,7 +736,8 @@ hipError_t launch_embed_grad(void *base, int state_dtype, const TableGeom &g, co
     fill.blocks = accumulate ? 0 : static_cast<uint32_t>((fill.table_bytes + 16 * threads - 1) / (16 * threads));
     const uint32_t fill_blocks = fill.blocks * N;
     int sorted = 0;
-    if (g.T > kOneBlock) {
+    if (scan_does(g)) {
+    } else if (g.T > kOneBlock) {
         p.tiles = static_cast<uint32_t>((g.T + kTile - 1) / kTile);
         p.sort_blocks = p.tiles * N;
         uint32_t *bins = reinterpret_cast<uint32_t *>(at + w.bins);
@@ -685,7 +768,7 @@ hipError_t launch_embed_grad(void *base, int state_dtype, const TableGeom &g, co
     auto go = [&](auto add) {
         constexpr bool ADD = decltype(add)::value;
         auto f = state_dtype == 0 ? (dy_dtype == 0 ? launch<0, 0, ADD> : launch<0, 1, ADD>) : (dy_dtype == 0 ? launch<1, 0, ADD> : launch<1, 1, ADD>);
-        f(base, g, scale, dy, dy_stride, keys[sorted], places[sorted], cuts, partials, stream);
+        f(base, g, tokens, scale, dy, dy_stride, keys[sorted], places[sorted], cuts, partials, stream);
     };
     if (accumulate) go(std::true_type{});
     else go(std::false_type{});

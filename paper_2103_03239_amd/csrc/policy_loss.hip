@@ -183,6 +183,21 @@ __device__ __forceinline__ float row_terms(const PolicyTerms &p, int64_t row, fl
     return w * (p.kl_coef * dk - (clipped ? 0.f : plain));
 }
 
+// Where a row's log-probability and terms go: the terms wait for the others of the peer, or are the peer's sums already (T = 1).
+struct RowOut {
+    float *logp, *stats;                 // stats: of peers with one row each, or nullptr
+    RowTerms *terms;
+    __device__ __forceinline__ void put(int64_t row, float lp, const RowTerms &t) const
+    {
+        logp[row] = lp;
+        if (stats) {
+            stats[3 * row] = t.loss;
+            stats[3 * row + 1] = t.kl;
+            stats[3 * row + 2] = t.clipped;
+        } else terms[row] = t;
+    }
+};
+
 template <int DT, int THREADS>
 __device__ __forceinline__ void store_zeros(char *grad, int64_t n)
 {
@@ -193,24 +208,24 @@ __device__ __forceinline__ void store_zeros(char *grad, int64_t n)
     for (int k = threadIdx.x; k < s.head + s.tail; k += THREADS) store_one<DT>(grad + s.single(k) * ES, 0.f);
 }
 
-// One row a block, in registers.  The gradient may take the logits' place (here and below): every element is read
-// before it is written, by the same thread.
+// A row by THREADS threads, in registers; rows of 64 threads four to a block.  The gradient may take the logits' place (here and
+// below): every element is read before it is written, by the same thread.
+constexpr int rows_of_block(int threads) { return threads == 64 ? 4 : 1; }
+
 template <int DT, int THREADS, int VECS>
-__global__ __launch_bounds__(THREADS, VECS == 8 ? 8 : 4) void policy_row_kernel(const char *logits, RowPlace at, const int32_t *__restrict__ tokens,
-                                                             PolicyTerms p, char *grad, int64_t grad_stride,
-                                                             float *__restrict__ logp, RowTerms *__restrict__ terms)
+__global__ __launch_bounds__(THREADS * rows_of_block(THREADS), VECS == 8 ? 8 : 4)
+void policy_row_kernel(const char *logits, int64_t rows, RowPlace at, const int32_t *__restrict__ tokens, PolicyTerms p, char *grad,
+                       int64_t grad_stride, RowOut out)
 {
     constexpr int ES = DT == 0 ? 4 : 2, VE = 16 / ES;
-    const int64_t row = blockIdx.x;
+    const int64_t row = int64_t(blockIdx.x) * rows_of_block(THREADS) + threadIdx.y;
+    if (row >= rows) return;
     const float w = p.weight[row];
     const int64_t token = tokens[row];
     char *to = grad + row * grad_stride * ES;
     if (w == 0.f || token < 0 || token >= at.vocab) {
         store_zeros<DT, THREADS>(to, at.vocab);
-        if (threadIdx.x == 0) {
-            logp[row] = 0.f;
-            terms[row] = RowTerms{0.f, 0.f, 0.f};
-        }
+        if (threadIdx.x == 0) out.put(row, 0.f, RowTerms{0.f, 0.f, 0.f});
         return;
     }
     const char *from = logits + row * at.stride * ES;
@@ -245,21 +260,27 @@ __global__ __launch_bounds__(THREADS, VECS == 8 ? 8 : 4) void policy_row_kernel(
     }
     keep_packed(held);
     t = block_join<THREADS>(t);
-    __shared__ float of_row[3];
+    float slope, factor, less;
     if (threadIdx.x < 64) {                                           // (the same for all its lanes)
         const float lp = z_token - t.top - logf(t.sum);
         RowTerms mine;
-        const float slope = row_terms(p, row, w, lp, mine);
-        if (threadIdx.x == 0) {
-            logp[row] = lp;
-            terms[row] = mine;
-            of_row[0] = slope;
-            of_row[1] = -slope / t.sum;
-            of_row[2] = -t.top * kLog2e;                              // (a row of -inf alone: NaN)
-        }
+        slope = row_terms(p, row, w, lp, mine);
+        factor = -slope / t.sum;
+        less = -t.top * kLog2e;                                       // (a row of -inf alone: NaN)
+        if (threadIdx.x == 0) out.put(row, lp, mine);
     }
-    __syncthreads();
-    const float slope = of_row[0], factor = of_row[1], less = of_row[2];
+    if constexpr (THREADS > 64) {
+        __shared__ float of_row[3];
+        if (threadIdx.x == 0) {
+            of_row[0] = slope;
+            of_row[1] = factor;
+            of_row[2] = less;
+        }
+        __syncthreads();
+        slope = of_row[0];
+        factor = of_row[1];
+        less = of_row[2];
+    }
     const int32_t token_vec = static_cast<int32_t>((token - s.head) >> (DT == 0 ? 2 : 3));       // (may be none of the whole ones)
     const int32_t token_elem = static_cast<int32_t>(token - s.head) & (VE - 1);
 #pragma unroll
@@ -342,7 +363,7 @@ __device__ __forceinline__ TopSum joined(const TopSum *__restrict__ sums, int32_
 template <int DT, int THREADS>
 __global__ __launch_bounds__(THREADS) void policy_slice_kernel(const char *logits, RowPlace at, Cut cut, const int32_t *__restrict__ tokens,
                                                                PolicyTerms p, const TopSum *__restrict__ sums, const float *__restrict__ z_token, char *grad, int64_t grad_stride,
-                                                               float *__restrict__ logp, RowTerms *__restrict__ terms)
+                                                               RowOut out)
 {
     constexpr int ES = DT == 0 ? 4 : 2, VE = 16 / ES, kBatch = 4;
     const int64_t row = blockIdx.x / static_cast<uint32_t>(cut.slices);
@@ -353,20 +374,14 @@ __global__ __launch_bounds__(THREADS) void policy_slice_kernel(const char *logit
     char *to = grad + (row * grad_stride + begin) * ES;
     if (w == 0.f || token < 0 || token >= at.vocab) {
         store_zeros<DT, THREADS>(to, end - begin);
-        if (slice == 0 && threadIdx.x == 0) {
-            logp[row] = 0.f;
-            terms[row] = RowTerms{0.f, 0.f, 0.f};
-        }
+        if (slice == 0 && threadIdx.x == 0) out.put(row, 0.f, RowTerms{0.f, 0.f, 0.f});
         return;
     }
     const TopSum t = joined(sums + row * cut.slices, cut.slices);
     const float lp = z_token[row] - t.top - logf(t.sum);             // (kept aside: another block's gradient may be in the logit's place by now)
     RowTerms mine;
     const float slope = row_terms(p, row, w, lp, mine);
-    if (slice == 0 && threadIdx.x == 0) {
-        logp[row] = lp;
-        terms[row] = mine;
-    }
+    if (slice == 0 && threadIdx.x == 0) out.put(row, lp, mine);
     const float factor = -slope / t.sum, less = -t.top * kLog2e;
     const char *from = logits + (row * at.stride + begin) * ES;
     const Slice<DT> s(from, end - begin);
@@ -466,18 +481,20 @@ Work layout(int64_t rows, const Cut &cut)
 
 template <int DT>
 void launch_policy(const void *logits, int64_t rows, int64_t vocab, int64_t stride, const int32_t *tokens, const PolicyTerms &p, void *grad,
-                   int64_t grad_stride, float *logp, char *work, int compute_units, hipStream_t stream)
+                   int64_t grad_stride, float *logp, float *stats, char *work, int compute_units, hipStream_t stream)
 {
     const Cut cut = cut_of(rows, vocab, DT, compute_units);
     const Work w = layout(rows, cut);
     const RowPlace at{vocab, stride};
     const char *from = static_cast<const char *>(logits);
     char *to = static_cast<char *>(grad);
-    RowTerms *terms = reinterpret_cast<RowTerms *>(work + w.terms);
+    const RowOut out{logp, stats, reinterpret_cast<RowTerms *>(work + w.terms)};
     const int64_t bytes = vocab * elem_size(DT);
     if (bytes <= kRowBytes) {
-        const uint32_t blocks = static_cast<uint32_t>(rows);
-        auto go = [&](auto kernel, int threads) { kernel<<<blocks, threads, 0, stream>>>(from, at, tokens, p, to, grad_stride, logp, terms); };
+        auto go = [&](auto kernel, int threads) {
+            const int each = rows_of_block(threads);
+            kernel<<<static_cast<uint32_t>((rows + each - 1) / each), dim3(threads, each), 0, stream>>>(from, rows, at, tokens, p, to, grad_stride, out);
+        };
         if (bytes <= 64 * 8 * 16) go(policy_row_kernel<DT, 64, 8>, 64);
         else if (bytes <= 128 * 8 * 16) go(policy_row_kernel<DT, 128, 8>, 128);
         else if (bytes <= 256 * 8 * 16) go(policy_row_kernel<DT, 256, 8>, 256);
@@ -490,7 +507,7 @@ void launch_policy(const void *logits, int64_t rows, int64_t vocab, int64_t stri
     float *z = reinterpret_cast<float *>(work + w.z_token);
     const uint32_t blocks = static_cast<uint32_t>(rows * cut.slices);
     slice_sum_kernel<DT, kSliceThreads><<<blocks, kSliceThreads, 0, stream>>>(from, at, cut, tokens, p.weight, sums, z, nullptr);
-    policy_slice_kernel<DT, kSliceThreads><<<blocks, kSliceThreads, 0, stream>>>(from, at, cut, tokens, p, sums, z, to, grad_stride, logp, terms);
+    policy_slice_kernel<DT, kSliceThreads><<<blocks, kSliceThreads, 0, stream>>>(from, at, cut, tokens, p, sums, z, to, grad_stride, out);
 }
 
 }  // namespace
@@ -507,8 +524,9 @@ hipError_t launch_policy_loss(const void *logits, int dtype, int64_t N, int64_t 
     char *at = static_cast<char *>(work);
     if (!launchable(N * T, 1024) && !launchable(N * T, (vocab * elem_size(dtype) + 127) / 128 + 63)) return hipErrorInvalidConfiguration;
     if (T > 0)
-        (dtype == 0 ? launch_policy<0> : launch_policy<1>)(logits, N * T, vocab, stride, tokens, p, grad, grad_stride, logp, at, compute_units, stream);
-    policy_stats_kernel<<<static_cast<uint32_t>(N), 256, 0, stream>>>(reinterpret_cast<const RowTerms *>(at), T, stats);
+        (dtype == 0 ? launch_policy<0> : launch_policy<1>)(logits, N * T, vocab, stride, tokens, p, grad, grad_stride, logp, T == 1 ? stats : nullptr, at,
+                                                           compute_units, stream);
+    if (T != 1) policy_stats_kernel<<<static_cast<uint32_t>(N), 256, 0, stream>>>(reinterpret_cast<const RowTerms *>(at), T, stats);
     return hipGetLastError();
 }
 
