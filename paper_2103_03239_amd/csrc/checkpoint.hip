@@ -45,10 +45,20 @@ template <> struct Elems8<0> {
     u32x4 w[2];
     __device__ __forceinline__ void load(const char *p)
     {
-        w[0] = load_vec<true, u32x4>(p);
-        w[1] = load_vec<true, u32x4>(p + 16);
+        w[0] = load_vec<false, u32x4>(p);                             // (the two halves share cache lines: no streaming hint)
+        w[1] = load_vec<false, u32x4>(p + 16);
     }
     __device__ __forceinline__ void put(int k, const char *p) { w[k >> 2][k & 3] = *reinterpret_cast<const uint32_t *>(p); }
+    __device__ __forceinline__ void move_down(int n)                  // elements n .. 7 to 0 .., zeros behind them
+    {
+#pragma unroll
+        for (int by = 4; by > 0; by /= 2)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const uint32_t from = k + by < 8 ? w[(k + by) >> 2 & 1][(k + by) & 3] : 0u;
+                w[k >> 2][k & 3] = n & by ? from : w[k >> 2][k & 3];
+            }
+    }
     __device__ __forceinline__ uint32_t most() const
     {
         uint32_t m = 0;
@@ -72,6 +82,20 @@ template <> struct Elems8<1> {
     __device__ __forceinline__ void put(int k, const char *p)
     {
         w[k >> 1] |= static_cast<uint32_t>(*reinterpret_cast<const uint16_t *>(p)) << (16 * (k & 1));
+    }
+    __device__ __forceinline__ void move_down(int n)
+    {
+        uint64_t low = uint64_t(w[1]) << 32 | w[0], high = uint64_t(w[3]) << 32 | w[2];
+        if (n >= 4) {
+            low = high;
+            high = 0;
+        }
+        const int bits = 16 * (n & 3);
+        if (bits > 0) {
+            low = low >> bits | high << (64 - bits);
+            high >>= bits;
+        }
+        w = u32x4{static_cast<uint32_t>(low), static_cast<uint32_t>(low >> 32), static_cast<uint32_t>(high), static_cast<uint32_t>(high >> 32)};
     }
     __device__ __forceinline__ uint32_t most() const                  // two elements at a time
     {
@@ -105,8 +129,12 @@ __global__ __launch_bounds__(kBlock) void checkpoint_kernel(const char *__restri
         if (down[n] >= rows) at[n] = width;
         if (at[n] >= width) continue;
         const char *from = x + uint64_t(down[n]) * stride + at[n] * ES;
+        // a row's last elements, where they are no whole unit: the row's last 8 moved to their place, so that one access does
         if (at[n] + kVec <= width) e[n].load(from);
-        else
+        else if (width >= kVec) {
+            e[n].load(from - (at[n] + kVec - width) * ES);
+            e[n].move_down(at[n] + kVec - width);
+        } else
 #pragma unroll
             for (int k = 0; k < kVec; ++k)
                 if (at[n] + k < width) e[n].put(k, from + k * ES);
@@ -133,9 +161,23 @@ __global__ __launch_bounds__(kBlock) void checkpoint_kernel(const char *__restri
         if (at[n] + kVec <= width) {
             typedef u32x2 any_t __attribute__((aligned(1)));
             __builtin_nontemporal_store(w, reinterpret_cast<any_t *>(to));
-        } else
-            for (int k = 0; k < kVec; ++k)
-                if (at[n] + k < width) to[k] = static_cast<int8_t>(w[k >> 2] >> (8 * (k & 3)));
+        } else {                                                      // 4, 2 and 1 codes as there are
+            typedef uint32_t word_t __attribute__((aligned(1)));
+            typedef uint16_t half_t __attribute__((aligned(1)));
+            const int left = width - at[n];
+            uint32_t v = w.x;
+            if (left & 4) {
+                *reinterpret_cast<word_t *>(to) = v;
+                to += 4;
+                v = w.y;
+            }
+            if (left & 2) {
+                *reinterpret_cast<half_t *>(to) = static_cast<uint16_t>(v);
+                to += 2;
+                v >>= 16;
+            }
+            if (left & 1) *to = static_cast<int8_t>(v);
+        }
     }
 }
 
@@ -179,7 +221,7 @@ __global__ __launch_bounds__(kBlock) void restore_kernel(const int8_t *__restric
 #pragma unroll
         for (int k = 0; k < kVec; ++k) f[k] = factor * code_of(w[n][k >> 2], k & 3);
         char *to = out + uint64_t(down[n]) * stride + at[n] * ES;
-        if (at[n] + kVec <= width) store_elems<DT, kVec, true>(to, f);
+        if (at[n] + kVec <= width) store_elems<DT, kVec, DT == 1>(to, f);
         else
             for (int k = 0; k < kVec; ++k)
                 if (at[n] + k < width) store_one<DT>(to + k * ES, f[k]);

@@ -2,8 +2,8 @@
 // state, times a scale.  out[i][t][:] = round(scale * table_i[tokens[i][t]][:]), the product in binary32.
 //
 // Bound by HBM: every distinct table row is read once, every output row written once.  A group of lanes
-// (a power of two, up to 64) moves a row, 8 elements a lane and step (16 bytes of bfloat16), and takes
-// kRows places, whose tokens and then whose rows are requested together: one dependent pair of
+// (a power of two, up to a wave) moves a row, or a wave 64 vectors of a longer one, 16 bytes of output a lane, and
+// takes kRows places, whose tokens and then whose rows are requested together: one dependent pair of
 // latencies for all of them.
 #include <hip/hip_runtime.h>
 
@@ -13,49 +13,51 @@
 namespace moshpit {
 namespace {
 
-constexpr int kBlock = 256, kRows = 4, kVec = 8;
+constexpr int kBlock = 256, kRows = 4;
 
 template <int ST, int OT, bool WIDE>
 __global__ __launch_bounds__(kBlock) void embed_kernel(const char *__restrict__ base, TableGeom g, const int32_t *__restrict__ tokens,
-                                                        float scale, char *__restrict__ out, int64_t out_stride, int32_t lanes_log2)
+                                                        float scale, char *__restrict__ out, int64_t out_stride, int32_t lanes_log2, uint32_t chunks)
 {
-    constexpr int ES = ST == 0 ? 4 : 2, EO = OT == 0 ? 4 : 2;
-    const int32_t lanes = 1 << lanes_log2, lane = threadIdx.x & (lanes - 1);
-    const int32_t groups = kBlock >> lanes_log2;
+    constexpr int ES = ST == 0 ? 4 : 2, EO = OT == 0 ? 4 : 2, kVec = 16 / EO;
+    const int32_t lanes = 1 << lanes_log2;
     const int64_t places = g.N * g.T;
-    const int64_t first = int64_t(blockIdx.x) * (groups * kRows) + (threadIdx.x >> lanes_log2);
+    // this group's part of the block, its column chunk and its first place
+    const uint32_t groups = kBlock >> lanes_log2, part = blockIdx.x * groups + (threadIdx.x >> lanes_log2);
+    const uint32_t set = part / chunks;
+    const int64_t c = (int64_t(part - set * chunks) * lanes + (threadIdx.x & (lanes - 1))) * kVec;
+    const int64_t first = int64_t(set) * kRows;
+    if (c >= g.width) return;
     const char *row[kRows];
 #pragma unroll
     for (int u = 0; u < kRows; ++u) {
-        const int64_t at = first + u * groups;
+        const int64_t at = first + u;
         row[u] = nullptr;
         if (at >= places) continue;
         const int64_t tok = tokens[at];
         if (tok >= 0 && tok < g.vocab) row[u] = base + ((at / g.T) * g.peer_stride + tok * g.width) * ES;
     }
-    for (int64_t c = int64_t(lane) * kVec; c < g.width; c += lanes * kVec) {
-        if constexpr (WIDE) {
-            // the last vector of a row ends with the row: it repeats elements of the one before it
-            const int64_t at_c = c + kVec <= g.width ? c : g.width - kVec;
-            float v[kRows][kVec];
+    if constexpr (WIDE) {
+        // the last vector of a row ends with the row: it repeats elements of the one before it
+        const int64_t at_c = c + kVec <= g.width ? c : g.width - kVec;
+        float v[kRows][kVec];
 #pragma unroll
-            for (int u = 0; u < kRows; ++u)
-                if (row[u]) load_elems<ST, kVec>(row[u] + at_c * ES, v[u]);
+        for (int u = 0; u < kRows; ++u)
+            if (row[u]) load_elems<ST, kVec>(row[u] + at_c * ES, v[u]);
 #pragma unroll
-            for (int u = 0; u < kRows; ++u) {
-                const int64_t at = first + u * groups;
-                if (at >= places) continue;
-                float r[kVec];
+        for (int u = 0; u < kRows; ++u) {
+            const int64_t at = first + u;
+            if (at >= places) continue;
+            float r[kVec];
 #pragma unroll
-                for (int k = 0; k < kVec; ++k) r[k] = row[u] ? scale * v[u][k] : 0.f;
-                store_elems<OT, kVec>(out + (at * out_stride + at_c) * EO, r);
-            }
-        } else {
-            for (int u = 0; u < kRows; ++u) {
-                const int64_t at = first + u * groups;
-                for (int64_t k = c; at < places && k < g.width && k < c + kVec; ++k)
-                    store_one<OT>(out + (at * out_stride + k) * EO, row[u] ? scale * load_one<ST>(row[u] + k * ES) : 0.f);
-            }
+            for (int k = 0; k < kVec; ++k) r[k] = row[u] ? scale * v[u][k] : 0.f;
+            store_elems<OT, kVec>(out + (at * out_stride + at_c) * EO, r);
+        }
+    } else {
+        for (int u = 0; u < kRows; ++u) {
+            const int64_t at = first + u;
+            for (int64_t k = c; at < places && k < g.width && k < c + kVec; ++k)
+                store_one<OT>(out + (at * out_stride + k) * EO, row[u] ? scale * load_one<ST>(row[u] + k * ES) : 0.f);
         }
     }
 }
@@ -63,14 +65,15 @@ __global__ __launch_bounds__(kBlock) void embed_kernel(const char *__restrict__ 
 template <int ST, int OT>
 hipError_t launch(const void *base, const TableGeom &g, const int32_t *tokens, float scale, void *out, int64_t out_stride, hipStream_t stream)
 {
+    constexpr int kVec = OT == 0 ? 4 : 8;
     int32_t lanes_log2 = 0;
     while (lanes_log2 < 6 && (int64_t(kVec) << lanes_log2) < g.width) ++lanes_log2;
-    const int64_t per_block = int64_t(kBlock >> lanes_log2) * kRows;
-    const int64_t blocks = (g.N * g.T + per_block - 1) / per_block;
-    if (!launchable(blocks, kBlock)) return hipErrorInvalidConfiguration;
+    const int64_t chunks = (g.width + (int64_t(kVec) << lanes_log2) - 1) / (int64_t(kVec) << lanes_log2);
+    const int64_t parts = (g.N * g.T + kRows - 1) / kRows * chunks, blocks = (parts + (kBlock >> lanes_log2) - 1) / (kBlock >> lanes_log2);
+    if (!launchable(blocks, kBlock) || !launchable(parts, 1)) return hipErrorInvalidConfiguration;
     auto kernel = g.width >= kVec ? embed_kernel<ST, OT, true> : embed_kernel<ST, OT, false>;
     kernel<<<static_cast<uint32_t>(blocks), kBlock, 0, stream>>>(static_cast<const char *>(base), g, tokens, scale, static_cast<char *>(out), out_stride,
-                                                                 lanes_log2);
+                                                                 lanes_log2, static_cast<uint32_t>(chunks));
     return hipGetLastError();
 }
 

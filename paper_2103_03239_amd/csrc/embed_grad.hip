@@ -759,7 +759,9 @@ hipError_t launch_embed_grad(void *base, int state_dtype, const TableGeom &g, co
         sorted = 1 - sorted;
     } else if (p.sort_blocks + fill_blocks > 0) {
         auto go = [&](auto kernel) { kernel<<<p.sort_blocks + fill_blocks, threads, 0, stream>>>(tokens, p, keys[0], places[0], fill); };
-        if (threads == 1024) go(sort_block_kernel<1024, 8>);
+        if (g.T > 4096) go(sort_block_kernel<1024, 8>);
+        else if (g.T > 2048) go(sort_block_kernel<1024, 4>);
+        else if (threads == 1024) go(sort_block_kernel<1024, 2>);
         else if (threads == 256) go(sort_block_kernel<256, 4>);
         else go(sort_block_kernel<64, 4>);
     }

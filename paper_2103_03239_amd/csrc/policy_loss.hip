@@ -304,6 +304,105 @@ void policy_row_kernel(const char *logits, int64_t rows, RowPlace at, const int3
     }
 }
 
+// Short rows, up to 2 KiB: a wave takes kShort of them, finds each one's largest value and sum, does the arithmetic of their terms
+// side by side, a row a lane, and writes the gradients.  (A wave a row spends more on the terms than on the row.)
+constexpr int kShort = 8, kShortVecs = 2;
+
+template <int DT, bool GRAD>
+__global__ __launch_bounds__(256, 4)
+void short_rows_kernel(const char *logits, int64_t rows, RowPlace at, const int32_t *__restrict__ tokens, PolicyTerms p, char *grad,
+                       int64_t grad_stride, RowOut out)
+{
+    constexpr int ES = DT == 0 ? 4 : 2, VE = 16 / ES;
+    const int lane = threadIdx.x & 63;
+    const int64_t first = (int64_t(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * kShort;
+    if (first >= rows) return;
+    const int count = rows - first < kShort ? static_cast<int>(rows - first) : kShort;
+    // lane r looks after row first + r
+    const int64_t own = first + (lane < count ? lane : 0);
+    const int32_t token = tokens[own];
+    const float w = GRAD ? p.weight[own] : 1.f;
+    const bool live = lane < count && w != 0.f && token >= 0 && token < at.vocab;
+    const uint64_t alive = __ballot(live);
+    const float z_token = live ? load_one<DT>(logits + (own * at.stride + token) * ES) : 0.f;
+    u32x4 held[kShort][kShortVecs];
+    float single[kShort];
+#pragma unroll
+    for (int r = 0; r < kShort; ++r) {
+        single[r] = -INFINITY;
+        if (!(alive >> r & 1)) continue;
+        const char *from = logits + (first + r) * at.stride * ES;
+        const Slice<DT> s(from, at.vocab);
+#pragma unroll
+        for (int v = 0; v < kShortVecs; ++v)
+            if (v * 64 + lane < s.count) held[r][v] = load_vec<true, u32x4>(s.vectors + (v * 64 + lane) * 16);
+        if (lane < s.head + s.tail) single[r] = load_one<DT>(from + s.single(lane) * ES);
+    }
+    TopSum mine{0.f, 1.f};
+#pragma unroll
+    for (int r = 0; r < kShort; ++r) {
+        if (!(alive >> r & 1)) continue;
+        const Slice<DT> s(logits + (first + r) * at.stride * ES, at.vocab);
+        float f[kShortVecs][VE], top = single[r];
+#pragma unroll
+        for (int v = 0; v < kShortVecs; ++v) {
+            if (v * 64 + lane >= s.count) continue;
+            widen_vec<DT>(held[r][v], f[v]);
+            top = fmaxf(top, largest(f[v]));
+        }
+        top = wave_top(top);
+        const float less = less_of(top);
+        float sum = __builtin_amdgcn_exp2f(fmaf(single[r], kLog2e, less));
+#pragma unroll
+        for (int v = 0; v < kShortVecs; ++v)
+            if (v * 64 + lane < s.count) sum += sum_exp(f[v], less);
+        sum = wave_sum(sum);
+        if (lane == r) mine = TopSum{top, sum};
+        if constexpr (GRAD) keep_packed(held[r]);
+    }
+    const float lp = live ? z_token - mine.top - logf(mine.sum) : 0.f;
+    RowTerms terms{0.f, 0.f, 0.f};
+    float slope = 0.f;
+    if constexpr (GRAD) {
+        if (live) slope = row_terms(p, own, w, lp, terms);
+        if (lane < count) out.put(own, lp, terms);
+    } else if (lane < count) out.logp[own] = lp;
+    if constexpr (!GRAD) return;
+    const float factor = -slope / mine.sum, less = -mine.top * kLog2e;
+    auto lane_value = [](float v, int r) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), r)); };
+#pragma unroll
+    for (int r = 0; r < kShort; ++r) {
+        if (r >= count) break;
+        char *to = grad + (first + r) * grad_stride * ES;
+        if (!(alive >> r & 1)) {
+            const Slice<DT> s(to, at.vocab);
+            for (int v = lane; v < s.count; v += 64) store_vec<true, u32x4>(const_cast<char *>(s.vectors) + v * 16, u32x4{0, 0, 0, 0});
+            if (lane < s.head + s.tail) store_one<DT>(to + s.single(lane) * ES, 0.f);
+            continue;
+        }
+        const Slice<DT> s(logits + (first + r) * at.stride * ES, at.vocab);
+        const float row_slope = lane_value(slope, r), row_factor = lane_value(factor, r), row_less = lane_value(less, r);
+        const int32_t row_token = __builtin_amdgcn_readlane(token, r);
+#pragma unroll
+        for (int v = 0; v < kShortVecs; ++v) {
+            const int32_t i = v * 64 + lane;
+            if (i >= s.count) continue;
+            float f[VE];
+            widen_vec<DT>(held[r][v], f);
+            const int32_t e = s.head + i * VE;
+#pragma unroll
+            for (int k = 0; k < VE; ++k) f[k] = row_factor * __builtin_amdgcn_exp2f(fmaf(f[k], kLog2e, row_less)) + (row_token == e + k ? row_slope : 0.f);
+            store_elems<DT, VE, true>(to + e * ES, f);
+        }
+        if (lane < s.head + s.tail) {
+            const int64_t e = s.single(lane);
+            store_one<DT>(to + e * ES, row_factor * __builtin_amdgcn_exp2f(fmaf(single[r], kLog2e, row_less)) + (row_token == e ? row_slope : 0.f));
+        }
+    }
+}
+
+constexpr int64_t kShortBytes = kShortVecs * 64 * 16;
+
 // Rows cut into slices: block b works on slice b % slices of row b / slices.
 struct Cut {
     int32_t slices;
@@ -311,13 +410,15 @@ struct Cut {
 };
 
 template <int DT, int THREADS>
-__global__ __launch_bounds__(THREADS) void slice_sum_kernel(const char *__restrict__ logits, RowPlace at, Cut cut, const int32_t *__restrict__ tokens,
-                                                            const float *__restrict__ weight, TopSum *__restrict__ sums, float *__restrict__ z_token,
-                                                            float *__restrict__ logp)
+__global__ __launch_bounds__(THREADS * rows_of_block(THREADS))
+void slice_sum_kernel(const char *__restrict__ logits, int64_t rows, RowPlace at, Cut cut, const int32_t *__restrict__ tokens,
+                      const float *__restrict__ weight, TopSum *__restrict__ sums, float *__restrict__ z_token, float *__restrict__ logp)
 {
     constexpr int ES = DT == 0 ? 4 : 2, VE = 16 / ES, kBatch = 8;
-    const int64_t row = blockIdx.x / static_cast<uint32_t>(cut.slices);
-    const int32_t slice = blockIdx.x % static_cast<uint32_t>(cut.slices);
+    const int64_t block = int64_t(blockIdx.x) * rows_of_block(THREADS) + threadIdx.y;       // (rows of 64 threads are not cut)
+    const int64_t row = THREADS == 64 ? block : block / cut.slices;
+    if (row >= rows) return;
+    const int32_t slice = THREADS == 64 ? 0 : blockIdx.x % static_cast<uint32_t>(cut.slices);
     const int64_t token = tokens[row];
     const bool live = (!weight || weight[row] != 0.f) && token >= 0 && token < at.vocab;
     if (!live) {
@@ -348,7 +449,7 @@ __global__ __launch_bounds__(THREADS) void slice_sum_kernel(const char *__restri
         logp[row] = load_one<DT>(logits + (row * at.stride + token) * ES) - t.top - logf(t.sum);
         return;
     }
-    sums[blockIdx.x] = t;
+    sums[block] = t;
     if (slice == 0) z_token[row] = load_one<DT>(logits + (row * at.stride + token) * ES);
 }
 
@@ -422,17 +523,26 @@ __global__ __launch_bounds__(64) void logp_join_kernel(const TopSum *__restrict_
     if (threadIdx.x == 0) logp[row] = z_token[row] - t.top - logf(t.sum);
 }
 
-// The terms of a peer's rows, summed in binary64 in an order that depends on T alone.
-__global__ __launch_bounds__(256) void policy_stats_kernel(const RowTerms *__restrict__ terms, int64_t T, float *__restrict__ stats)
+// The terms of a peer's rows, summed in binary64 in an order that depends on T alone.  A thread requests four rows' terms before
+// it adds the first: one block is bound by the latency of its loads.
+constexpr int kStatsThreads = 1024;
+
+__global__ __launch_bounds__(kStatsThreads) void policy_stats_kernel(const RowTerms *__restrict__ terms, int64_t T, float *__restrict__ stats)
 {
-    __shared__ double of_wave[4][3];
+    __shared__ double of_wave[kStatsThreads / 64][3];
     const RowTerms *mine = terms + int64_t(blockIdx.x) * T;
+    const int32_t step = blockDim.x;
     double sum[3] = {0.0, 0.0, 0.0};
-    for (int64_t t = threadIdx.x; t < T; t += 256) {
-        const RowTerms v = mine[t];
-        sum[0] += v.loss;
-        sum[1] += v.kl;
-        sum[2] += v.clipped;
+    for (int64_t t0 = threadIdx.x; t0 < T; t0 += 4 * step) {
+        RowTerms v[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[u] = t0 + u * step < T ? mine[t0 + u * step] : RowTerms{0.f, 0.f, 0.f};
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            sum[0] += v[u].loss;
+            sum[1] += v[u].kl;
+            sum[2] += v[u].clipped;
+        }
     }
 #pragma unroll
     for (int q = 0; q < 3; ++q) {
@@ -442,8 +552,9 @@ __global__ __launch_bounds__(256) void policy_stats_kernel(const RowTerms *__res
     }
     __syncthreads();
     if (threadIdx.x < 3) {
-        const int q = threadIdx.x;
-        stats[int64_t(blockIdx.x) * 3 + q] = static_cast<float>((of_wave[0][q] + of_wave[1][q]) + (of_wave[2][q] + of_wave[3][q]));
+        double all = 0.0;
+        for (int w = 0; w < step / 64; ++w) all += of_wave[w][threadIdx.x];
+        stats[int64_t(blockIdx.x) * 3 + threadIdx.x] = static_cast<float>(all);
     }
 }
 
@@ -495,7 +606,10 @@ void launch_policy(const void *logits, int64_t rows, int64_t vocab, int64_t stri
             const int each = rows_of_block(threads);
             kernel<<<static_cast<uint32_t>((rows + each - 1) / each), dim3(threads, each), 0, stream>>>(from, rows, at, tokens, p, to, grad_stride, out);
         };
-        if (bytes <= 64 * 8 * 16) go(policy_row_kernel<DT, 64, 8>, 64);
+        if (bytes <= kShortBytes && rows >= 16 * compute_units)
+            short_rows_kernel<DT, true><<<static_cast<uint32_t>((rows + 4 * kShort - 1) / (4 * kShort)), 256, 0, stream>>>(from, rows, at, tokens, p, to,
+                                                                                                                       grad_stride, out);
+        else if (bytes <= 64 * 8 * 16) go(policy_row_kernel<DT, 64, 8>, 64);
         else if (bytes <= 128 * 8 * 16) go(policy_row_kernel<DT, 128, 8>, 128);
         else if (bytes <= 256 * 8 * 16) go(policy_row_kernel<DT, 256, 8>, 256);
         else if (bytes <= 512 * 8 * 16) go(policy_row_kernel<DT, 512, 8>, 512);
@@ -506,7 +620,7 @@ void launch_policy(const void *logits, int64_t rows, int64_t vocab, int64_t stri
     TopSum *sums = reinterpret_cast<TopSum *>(work + w.sums);
     float *z = reinterpret_cast<float *>(work + w.z_token);
     const uint32_t blocks = static_cast<uint32_t>(rows * cut.slices);
-    slice_sum_kernel<DT, kSliceThreads><<<blocks, kSliceThreads, 0, stream>>>(from, at, cut, tokens, p.weight, sums, z, nullptr);
+    slice_sum_kernel<DT, kSliceThreads><<<blocks, kSliceThreads, 0, stream>>>(from, rows, at, cut, tokens, p.weight, sums, z, nullptr);
     policy_slice_kernel<DT, kSliceThreads><<<blocks, kSliceThreads, 0, stream>>>(from, at, cut, tokens, p, sums, z, to, grad_stride, out);
 }
 
@@ -526,7 +640,7 @@ hipError_t launch_policy_loss(const void *logits, int dtype, int64_t N, int64_t 
     if (T > 0)
         (dtype == 0 ? launch_policy<0> : launch_policy<1>)(logits, N * T, vocab, stride, tokens, p, grad, grad_stride, logp, T == 1 ? stats : nullptr, at,
                                                            compute_units, stream);
-    if (T != 1) policy_stats_kernel<<<static_cast<uint32_t>(N), 256, 0, stream>>>(reinterpret_cast<const RowTerms *>(at), T, stats);
+    if (T != 1) policy_stats_kernel<<<static_cast<uint32_t>(N), T <= 256 ? 64 : T <= 1024 ? 256 : kStatsThreads, 0, stream>>>(reinterpret_cast<const RowTerms *>(at), T, stats);
     return hipGetLastError();
 }
 
@@ -539,9 +653,17 @@ hipError_t launch_token_logp(const void *logits, int dtype, int64_t rows, int64_
     const Work w = layout(rows, cut);
     TopSum *sums = reinterpret_cast<TopSum *>(static_cast<char *>(work) + w.sums);
     float *z = cut.slices > 1 ? reinterpret_cast<float *>(static_cast<char *>(work) + w.z_token) : nullptr;
-    const uint32_t blocks = static_cast<uint32_t>(rows * cut.slices);
-    (dtype == 0 ? slice_sum_kernel<0, kSliceThreads> : slice_sum_kernel<1, kSliceThreads>)<<<blocks, kSliceThreads, 0, stream>>>(
-        static_cast<const char *>(logits), RowPlace{vocab, stride}, cut, tokens, nullptr, sums, z, logp);
+    if (vocab * elem_size(dtype) <= kShortBytes && rows >= 16 * compute_units) {
+        (dtype == 0 ? short_rows_kernel<0, false> : short_rows_kernel<1, false>)<<<static_cast<uint32_t>((rows + 4 * kShort - 1) / (4 * kShort)), 256, 0, stream>>>(
+            static_cast<const char *>(logits), rows, RowPlace{vocab, stride}, tokens, PolicyTerms{}, nullptr, 0, RowOut{logp, nullptr, nullptr});
+        return hipGetLastError();
+    }
+    // rows of up to 8 KiB by a wave, four to a block
+    const int threads = cut.slices == 1 && vocab * elem_size(dtype) <= 8192 ? 64 : kSliceThreads, each = rows_of_block(threads);
+    auto kernel = threads == 64 ? (dtype == 0 ? slice_sum_kernel<0, 64> : slice_sum_kernel<1, 64>)
+                                : (dtype == 0 ? slice_sum_kernel<0, kSliceThreads> : slice_sum_kernel<1, kSliceThreads>);
+    kernel<<<static_cast<uint32_t>((rows * cut.slices + each - 1) / each), dim3(threads, each), 0, stream>>>(
+        static_cast<const char *>(logits), rows, RowPlace{vocab, stride}, cut, tokens, nullptr, sums, z, logp);
     if (cut.slices > 1) logp_join_kernel<<<static_cast<uint32_t>(rows), 64, 0, stream>>>(sums, z, cut.slices, tokens, vocab, logp);
     return hipGetLastError();
 }

@@ -377,6 +377,7 @@ def policy_want(c, kl, low=0.2, high=0.3, ref=True):
     (2, 1, 0, 9, 0, 0.1), (2, 1, 1, 1, 0, 0.1), (2, 1, 1, 2, 1, 0.0), (2, 2, 5, 7, 0, 0.1), (3, 2, 3, 63, 3, 0.05), (2, 2, 9, 1_000, 1, 0.1),
     (2, 1, 4, 4_096, 0, 0.0), (2, 1, 3, 4_097, 0, 0.1), (2, 2, 40, 8_200, 2, 0.1), (2, 1, 7, 16_500, 1, 0.02), (2, 1, 2, 33_001, 0, 0.1),
     (2, 2, 30, 50_001, 0, 0.1), (2, 1, 3, 65_600, 1, 0.1), (2, 1, 1, 131_072, 0, 0.1), (2, 1, 2, 200_003, 5, 0.1), (2, 2, 300, 70_000, 0, 0.1),
+    (2, 2, 1_100, 300, 1, 0.1), (2, 2, 1_030, 7, 0, 0.1), (3, 2, 500, 512, 3, 0.05), (8, 4, 1, 100, 0, 0.1), (2, 3, 700, 1_024, 0, 0.0),     # many short rows
 ])
 @pytest.mark.parametrize("in_place", [False, True])
 def test_policy_loss(act, M, d, T, V, pad, kl, in_place):
