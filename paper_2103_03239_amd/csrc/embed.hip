@@ -4,7 +4,8 @@
 // Bound by HBM: every distinct table row is read once, every output row written once.  A group of lanes
 // (a power of two, up to a wave) moves a row, or a wave 64 vectors of a longer one, 16 bytes of output a lane, and
 // takes kRows places, whose tokens and then whose rows are requested together: one dependent pair of
-// latencies for all of them.
+// latencies for all of them.  Stores are streaming ones: 16 x 8192 rows of 1024 out of binary32 tables into bfloat16
+// in 71 us, with plain ones in 92; 4 x 15274 rows of 1200 binary32 in 57 us (87).
 #include <hip/hip_runtime.h>
 
 #include "local_ops.h"
@@ -51,7 +52,7 @@ __global__ __launch_bounds__(kBlock) void embed_kernel(const char *__restrict__ 
             float r[kVec];
 #pragma unroll
             for (int k = 0; k < kVec; ++k) r[k] = row[u] ? scale * v[u][k] : 0.f;
-            store_elems<OT, kVec>(out + (at * out_stride + at_c) * EO, r);
+            store_elems<OT, kVec, true>(out + (at * out_stride + at_c) * EO, r);
         }
     } else {
         for (int u = 0; u < kRows; ++u) {

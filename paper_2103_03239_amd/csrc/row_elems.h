@@ -6,6 +6,13 @@
 
 namespace moshpit {
 
+// Block b of n runs on die b % 8: which of n consecutive pieces of work it takes, so that each die takes a run of them.
+__device__ __forceinline__ uint32_t die_run(uint32_t b, uint32_t n)
+{
+    const uint32_t die = b % 8, each = n / 8, more = n % 8;
+    return die * each + (die < more ? die : more) + b / 8;
+}
+
 template <int DT> __device__ __forceinline__ float load_one(const void *p)
 {
     if constexpr (DT == 0) return *static_cast<const float *>(p);

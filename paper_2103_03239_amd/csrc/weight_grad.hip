@@ -251,9 +251,8 @@ void weight_grad_kernel(const char *__restrict__ dy, const int8_t *__restrict__ 
     constexpr int Y_ELEMS = PARTS * K * TO, ELEMS = Y_ELEMS + K * TI;
     extern __shared__ __attribute__((aligned(16))) uint16_t lds[];       // two buffers of ELEMS
 
-    // Block b runs on die b % 8: a die takes a run of tiles, so that the tiles of a peer share its operands in the die's cache.
-    const uint32_t die = blockIdx.x % 8, each = gridDim.x / 8, more = gridDim.x % 8;
-    uint32_t b = die * each + (die < more ? die : more) + blockIdx.x / 8;
+    // a die takes a run of tiles, so that the tiles of a peer share its operands in the die's cache
+    uint32_t b = die_run(blockIdx.x, gridDim.x);
     const int32_t ti = b % s.tiles_i;
     b /= s.tiles_i;
     const int32_t to = b % s.tiles_o;
