@@ -63,6 +63,13 @@ def _torch():
     return _torch_module
 
 
+def _current_stream(device) -> int:
+    """Handle of the device's current stream (torch's Stream object for it takes 2 us to make, as long as a launch)."""
+    torch = _torch()
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return torch.cuda.current_stream(device).cuda_stream if raw is None or device.index is None else raw(device.index)
+
+
 def load_library() -> ctypes.CDLL:
     """Load libmoshpit.so (built in-tree by __graft_entry__.build())."""
     global _lib
@@ -339,6 +346,16 @@ class Moshpit:
             return BF16
         raise ValueError("activations must be float32 or bfloat16")
 
+    def _new(self, device, *wanted):
+        """New tensors, one per (shape, dtype), out of the bound stream's memory: a block that another stream has just given back may
+        still be in use there."""
+        torch = _torch()
+        stream = self._state[1] if self._state else None
+        if stream is None or _current_stream(device) == stream.cuda_stream:
+            return [torch.empty(shape, dtype=dtype, device=device) for shape, dtype in wanted]
+        with torch.cuda.stream(stream):
+            return [torch.empty(shape, dtype=dtype, device=device) for shape, dtype in wanted]
+
     def _rows(self, x, name: str, T: int | None = None):
         """x: [N, T, width] on the GPU, unit column stride, row i * T + t at a constant stride.
         Returns (pointer, type code, T, width, row stride)."""
@@ -360,11 +377,13 @@ class Moshpit:
             raise ValueError("tokens must be a contiguous int32 GPU tensor [N, T]")
         return tokens.data_ptr(), tokens.shape[1]
 
-    def _per_token(self, x, T: int, name: str):
-        torch = _torch()
-        if x.dtype != torch.float32 or tuple(x.shape) != (self.N, T) or not x.is_cuda or not x.is_contiguous():
-            raise ValueError(f"{name} must be a contiguous float32 GPU tensor [N, {T}]")
-        return x.data_ptr()
+    def _per_token(self, shape, *named):
+        """Pointers of float32 GPU tensors [N, T]; named: (tensor, name) pairs."""
+        f32 = _torch().float32
+        for x, name in named:
+            if x.dtype is not f32 or x.shape != shape or not x.is_cuda or not x.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous float32 GPU tensor {list(shape)}")
+        return [x.data_ptr() for x, _ in named]
 
     def embed(self, tokens, column: int, vocab: int, width: int, scale: float = 1.0, out=None, dtype=None):
         """Token embeddings [N, T, width] from the tables [vocab, width] that start at parameter `column` of
@@ -373,7 +392,7 @@ class Moshpit:
         tp, T = self._tokens(tokens)
         if out is None:
             dtype = dtype or (torch.float32 if self.dtype == F32 else torch.bfloat16)
-            out = torch.empty((self.N, T, width), dtype=dtype, device=tokens.device)
+            out, = self._new(tokens.device, ((self.N, T, width), dtype))
         op, code, _, w, stride = self._rows(out, "out", T)
         if w != width:
             raise ValueError("out must be [N, T, width]")
@@ -392,8 +411,7 @@ class Moshpit:
         """x [N, T, width] in 8 bits: (codes int8 [N, T, width], scales uint8 [N, T, ceil(width / 32)])."""
         torch = _torch()
         xp, code, T, width, stride = self._rows(x, "x")
-        codes = torch.empty((self.N, T, width), dtype=torch.int8, device=x.device)
-        scales = torch.empty((self.N, T, -(-width // 32)), dtype=torch.uint8, device=x.device)
+        codes, scales = self._new(x.device, ((self.N, T, width), torch.int8), ((self.N, T, -(-width // 32)), torch.uint8))
         self._check(self._lib.moshpit_checkpoint(self._h, xp, code, self.N * T, width, stride, codes.data_ptr(), scales.data_ptr()),
                     "checkpoint")
         return codes, scales
@@ -411,7 +429,7 @@ class Moshpit:
         torch = _torch()
         cp, sp = self._saved(codes, scales)
         if out is None:
-            out = torch.empty(codes.shape, dtype=dtype or torch.float32, device=codes.device)
+            out, = self._new(codes.device, (codes.shape, dtype or torch.float32))
         op, code, T, width, stride = self._rows(out, "out", codes.shape[1])
         if width != codes.shape[2]:
             raise ValueError("out must have the shape of codes")
@@ -432,7 +450,7 @@ class Moshpit:
         torch = _torch()
         tp, T = self._tokens(tokens)
         zp, code, _, vocab, stride = self._rows(logits, "logits", T)
-        logp = torch.empty((self.N, T), dtype=torch.float32, device=logits.device)
+        logp, = self._new(logits.device, ((self.N, T), torch.float32))
         self._check(self._lib.moshpit_token_logp(self._h, zp, code, stride, tp, T, vocab, logp.data_ptr()), "token_logp")
         return logp
 
@@ -443,14 +461,13 @@ class Moshpit:
         torch = _torch()
         tp, T = self._tokens(tokens)
         zp, code, _, vocab, stride = self._rows(logits, "logits", T)
-        grad = logits if grad is None else grad
-        dp, dcode, _, dvocab, dstride = self._rows(grad, "grad", T)
+        dp, dcode, _, dvocab, dstride = (zp, code, T, vocab, stride) if grad is None else self._rows(grad, "grad", T)
         if dcode != code or dvocab != vocab:
             raise ValueError("grad must have the type and shape of logits")
-        old, adv, w = self._per_token(old_logp, T, "old_logp"), self._per_token(advantage, T, "advantage"), self._per_token(weight, T, "weight")
-        ref = None if ref_logp is None else self._per_token(ref_logp, T, "ref_logp")
-        logp = torch.empty((self.N, T), dtype=torch.float32, device=logits.device)
-        stats = torch.empty((self.N, 3), dtype=torch.float32, device=logits.device)
+        shape = tokens.shape
+        old, adv, w = self._per_token(shape, (old_logp, "old_logp"), (advantage, "advantage"), (weight, "weight"))
+        ref = None if ref_logp is None else self._per_token(shape, (ref_logp, "ref_logp"))[0]
+        logp, stats = self._new(logits.device, ((self.N, T), torch.float32), ((self.N, 3), torch.float32))
         self._check(self._lib.moshpit_policy_loss(self._h, zp, code, stride, tp, T, vocab, old, ref, adv, w, clip_low, clip_high, kl_coef, dp,
                                                   dstride, logp.data_ptr(), stats.data_ptr()), "policy_loss")
         return stats, logp

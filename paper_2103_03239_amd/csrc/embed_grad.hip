@@ -590,20 +590,19 @@ __global__ __launch_bounds__(kBlock) void embed_grad_join_kernel(char *__restric
             float acc = 0.f;
             if (c < g.width) {
                 const int64_t q_end = (wave + 1) * each < count ? (wave + 1) * each : count;
-                int64_t q = wave * each;
-                for (; q + 8 <= q_end; q += 8) {
+                for (int64_t q = wave * each; q < q_end; q += 8) {    // eight partial sums requested at a time
                     float v[8];
-    #pragma unroll
-                    for (int u = 0; u < 8; ++u) v[u] = mine[((first + q + u) * 2 + (q + u == 0 ? 1 : 0)) * g.width + c];
+#pragma unroll
+                    for (int u = 0; u < 8; ++u)
+                        v[u] = q + u < q_end ? mine[((first + q + u) * 2 + (q + u == 0 ? 1 : 0)) * g.width + c] : 0.f;
                     acc += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
                 }
-                for (; q < q_end; ++q) acc += mine[((first + q) * 2 + (q == 0 ? 1 : 0)) * g.width + c];
             }
             wave_sum[wave][lane] = acc;
             __syncthreads();
             if (wave == 0 && c < g.width) {
                 float sum = 0.f;
-    #pragma unroll
+#pragma unroll
                 for (int w = 0; w < kWaves; ++w) sum += wave_sum[w][lane];
                 char *to = base + (peer * g.peer_stride + int64_t(row) * g.width + c) * ES;
                 const float f = scale * sum;

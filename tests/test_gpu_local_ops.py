@@ -519,6 +519,33 @@ def test_on_another_stream_and_in_a_graph():
                 assert torch.equal(a, b), k
 
 
+def test_new_tensors_belong_to_the_bound_stream():
+    """Called with another stream current, the operators' new tensors are not out of blocks that stream still uses: here
+    a block that a long queue of its work reads after it was freed."""
+    g = rng(12)
+    N, T, W = 4, 256, 1_024
+    X, x = torch.zeros((N, 16), device=DEV), normal((N, T, W), torch.float32, g)
+    big = normal((4_096, 4_096), torch.float32, g)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with binding.Moshpit(N, 16, 2, 2, binding.F32) as m:
+        m.bind_state(X, side)
+        want, scales = m.checkpoint(x)
+        want, value = want.clone(), m.checkpoint_restore(want, scales).clone()
+        torch.cuda.synchronize()
+        for _ in range(10):
+            big = (big @ big).clamp_(-1, 1)
+        held = value.clone()                                          # queued behind the products
+        total = held.double().sum()
+        del held                                                      # its block is free to this stream, and still to be read
+        out = m.checkpoint_restore(want, scales)
+        m.sync()
+        assert torch.equal(out, value)
+        torch.cuda.synchronize()
+        assert float(total) == float(value.double().sum())
+        assert torch.equal(out, value)
+
+
 def test_refusals():
     X = torch.zeros((4, 1_000), device=DEV)
     G = torch.zeros_like(X)
