@@ -2,7 +2,7 @@
 //   grad_i[v][:] = scale * sum over t with tokens[i][t] == v of dy[i][t][:]      (binary32 sums, rounded once)
 // for every row v of every table (rows without a token: zeros, or untouched where the gradient is added).
 //
-// Tokens first: each peer's places are sorted by token, stably (a radix sort, 8 bits a pass), so that the
+// Tokens first: each peer's places are sorted by token, stably (a radix sort, up to 8 bits a pass), so that the
 // places of a row lie side by side in ascending order.  Meanwhile other blocks of the same launch clear the tables:
 // most rows of a vocabulary have no token, and a plain fill writes them at 6.8 TB/s, while waves that each
 // write the empty rows between their own reached 4.7 (64 tables of 30000 x 128 binary32).
@@ -25,7 +25,7 @@ namespace {
 constexpr int kBins = 256;
 
 struct SortPlan {
-    int32_t T, passes;
+    int32_t T, passes, bits;             // bits of a pass
     uint32_t vocab;
     uint32_t tiles;                      // of a peer; block b works on tile b % tiles of peer b / tiles
     uint32_t sort_blocks;                // blocks beyond these clear the tables
@@ -45,31 +45,46 @@ __device__ __forceinline__ void wave_order()
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
-// Where each of a block's items goes within the block when they are ordered by the 8 bits of their key from
+// The sums of v over the lanes up to each.
+__device__ __forceinline__ uint32_t upto_lane(uint32_t v)
+{
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, false);    // within rows of 16 lanes: 1, 2, 4 and 8 lanes down
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);    // the last lane of rows 0 and 2 to rows 1 and 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);    // lane 31 to rows 2 and 3
+    return v;
+}
+
+// Where each of a block's items goes within the block when they are ordered by the `bits` (up to 8) bits of their key from
 // `shift` on, stably.  Item i of lane l of wave w is number w * 64 * ITEMS + i * 64 + l of the block.
 // count: LDS, (waves + 1) * kBins; afterwards count[waves * kBins + b] is where bin b begins in the block.
 template <int THREADS, int ITEMS>
-__device__ __forceinline__ void block_rank(const uint32_t (&key)[ITEMS], int shift, uint32_t *count, uint32_t (&rank)[ITEMS])
+__device__ __forceinline__ void block_rank(const uint32_t (&key)[ITEMS], int shift, int bits, uint32_t *count, uint32_t (&rank)[ITEMS])
 {
     constexpr int WAVES = THREADS / 64;
+    const uint32_t bins = (1u << bits) - 1;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     for (int b = threadIdx.x; b < WAVES * kBins; b += THREADS) count[b] = 0;
     __syncthreads();
     uint32_t *mine = count + wave * kBins;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-        const uint32_t digit = (key[i] >> shift) & (kBins - 1);
-        uint64_t same = ~uint64_t(0);
+        const uint32_t digit = (key[i] >> shift) & bins;
+        uint32_t low = ~0u, high = ~0u;                               // lanes whose digit is this one's
 #pragma unroll
-        for (int b = 0; b < 8; ++b) {
+        for (int b = 0; b < 8; ++b) {                                 // (bits beyond `bits` are 0 in every lane)
             const uint64_t has = __ballot((digit >> b) & 1);
-            same &= ((digit >> b) & 1) ? has : ~has;
+            const uint32_t mine_has = 0u - ((digit >> b) & 1);
+            low &= ~(static_cast<uint32_t>(has) ^ mine_has);
+            high &= ~(static_cast<uint32_t>(has >> 32) ^ mine_has);
         }
-        const uint32_t below = __popcll(same & ((uint64_t(1) << lane) - 1));
+        const uint32_t below = __builtin_amdgcn_mbcnt_hi(high, __builtin_amdgcn_mbcnt_lo(low, 0));
         const uint32_t before = mine[digit];
         rank[i] = before + below;
         wave_order();                                            // every lane has read before one adds
-        if (below == 0) mine[digit] = before + static_cast<uint32_t>(__popcll(same));
+        if (below == 0) mine[digit] = before + static_cast<uint32_t>(__popc(low) + __popc(high));
         wave_order();
     }
     __syncthreads();
@@ -92,19 +107,14 @@ __device__ __forceinline__ void block_rank(const uint32_t (&key)[ITEMS], int shi
             c[k] = sum;
             sum += start[lane * 4 + k];
         }
-        uint32_t upto = sum;
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const uint32_t v = __shfl_up(upto, off, 64);
-            if (lane >= off) upto += v;
-        }
+        const uint32_t upto = upto_lane(sum);
 #pragma unroll
         for (int k = 0; k < 4; ++k) start[lane * 4 + k] = upto - sum + c[k];
     }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-        const uint32_t digit = (key[i] >> shift) & (kBins - 1);
+        const uint32_t digit = (key[i] >> shift) & bins;
         rank[i] += mine[digit] + start[digit];
     }
 }
@@ -153,7 +163,7 @@ __global__ __launch_bounds__(THREADS) void sort_block_kernel(const int32_t *__re
         place[i] = static_cast<uint16_t>(at);
     }
     for (int pass = 0; pass < p.passes; ++pass) {
-        block_rank<THREADS, ITEMS>(key, 8 * pass, count, rank);
+        block_rank<THREADS, ITEMS>(key, p.bits * pass, p.bits, count, rank);
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
             swap_key[rank[i]] = key[i];
@@ -197,7 +207,7 @@ __global__ __launch_bounds__(kTileThreads) void sort_count_kernel(const int32_t 
 #pragma unroll
     for (int i = 0; i < kTileItems; ++i) {
         const int64_t at = int64_t(tile) * kTile + i * kTileThreads + threadIdx.x;
-        if (at < p.T) atomicAdd(&count[(pass_key(tokens, keys, row + at, p.vocab) >> shift) & (kBins - 1)], 1u);
+        if (at < p.T) atomicAdd(&count[(pass_key(tokens, keys, row + at, p.vocab) >> shift) & ((1u << p.bits) - 1)], 1u);
     }
     __syncthreads();
     uint32_t *mine = bins + int64_t(peer) * kBins * p.tiles;
@@ -220,12 +230,7 @@ __global__ __launch_bounds__(1024) void sort_scan_kernel(uint32_t *__restrict__ 
             v[u] = sum;
             sum += c;
         }
-        uint32_t upto = sum;
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const uint32_t w = __shfl_up(upto, off, 64);
-            if (lane >= off) upto += w;
-        }
+        const uint32_t upto = upto_lane(sum);
         if (lane == 63) wave_sum[wave] = upto;
         __syncthreads();
         uint32_t waves_before = 0, all = 0;
@@ -261,7 +266,7 @@ __global__ __launch_bounds__(kTileThreads) void sort_move_kernel(const int32_t *
         const int64_t at = base + i * 64;
         key[i] = at < p.T ? pass_key(tokens, keys, row + at, p.vocab) : 0xffffffffu;
     }
-    block_rank<kTileThreads, kTileItems>(key, shift, count, rank);
+    block_rank<kTileThreads, kTileItems>(key, shift, p.bits, count, rank);
     for (int b = threadIdx.x; b < kBins; b += kTileThreads)
         goes_to[b] = mine[int64_t(b) * p.tiles + tile] - count[(kTileThreads / 64) * kBins + b];
     __syncthreads();
@@ -269,7 +274,7 @@ __global__ __launch_bounds__(kTileThreads) void sort_move_kernel(const int32_t *
     for (int i = 0; i < kTileItems; ++i) {
         const int64_t at = base + i * 64;
         if (at >= p.T) continue;
-        const int64_t to = row + (goes_to[(key[i] >> shift) & (kBins - 1)] + rank[i]);
+        const int64_t to = row + (goes_to[(key[i] >> shift) & ((1u << p.bits) - 1)] + rank[i]);
         keys_out[to] = key[i];
         places_out[to] = keys ? places[row + at] : static_cast<int32_t>(at);
     }
@@ -726,8 +731,11 @@ hipError_t launch_embed_grad(void *base, int state_dtype, const TableGeom &g, co
     uint32_t *keys[2] = {reinterpret_cast<uint32_t *>(at + w.keys[0]), reinterpret_cast<uint32_t *>(at + w.keys[1])};
     int32_t *places[2] = {reinterpret_cast<int32_t *>(at + w.places[0]), reinterpret_cast<int32_t *>(at + w.places[1])};
     const uint32_t N = static_cast<uint32_t>(g.N);
-    SortPlan p{static_cast<int32_t>(g.T), 0, static_cast<uint32_t>(g.vocab), 0, g.T > 0 ? N : 0};
-    while ((uint64_t(g.vocab) >> (8 * p.passes)) != 0) ++p.passes;    // keys 0 .. vocab
+    SortPlan p{static_cast<int32_t>(g.T), 0, 0, static_cast<uint32_t>(g.vocab), 0, g.T > 0 ? N : 0};
+    int key_bits = 0;
+    while ((uint64_t(g.vocab) >> key_bits) != 0) ++key_bits;          // keys 0 .. vocab
+    p.passes = (key_bits + 7) / 8;
+    p.bits = (key_bits + p.passes - 1) / p.passes;
     const int32_t es = state_dtype == 0 ? 4 : 2;
     Fill fill{static_cast<char *>(base), g.peer_stride * es, g.vocab * g.width * es, 0, 0};
     // threads of the sort's blocks, and so of those that clear: many only where one block sorts many places
@@ -747,10 +755,10 @@ hipError_t launch_embed_grad(void *base, int state_dtype, const TableGeom &g, co
         for (int pass = 0; pass < p.passes; ++pass) {
             const uint32_t *from = pass ? keys[1 - sorted] : nullptr;
             const int32_t *from_places = pass ? places[1 - sorted] : nullptr;
-            sort_count_kernel<<<p.sort_blocks + some(), kTileThreads, 0, stream>>>(tokens, from, p, 8 * pass, bins, fill);
+            sort_count_kernel<<<p.sort_blocks + some(), kTileThreads, 0, stream>>>(tokens, from, p, p.bits * pass, bins, fill);
             fill.first += some();
             sort_scan_kernel<<<N, 1024, 0, stream>>>(bins, int64_t(kBins) * p.tiles);
-            sort_move_kernel<<<p.sort_blocks + some(), kTileThreads, 0, stream>>>(tokens, from, from_places, p, 8 * pass, bins, keys[sorted],
+            sort_move_kernel<<<p.sort_blocks + some(), kTileThreads, 0, stream>>>(tokens, from, from_places, p, p.bits * pass, bins, keys[sorted],
                                                                                   places[sorted], fill);
             fill.first += some();
             sorted = 1 - sorted;
