@@ -495,21 +495,22 @@ __global__ __launch_bounds__(kBlock) void embed_grad_kernel(const uint32_t *__re
     else columns.store_partial(head ? slot : slot + g.width, acc);         // the row goes on in the next share
 }
 
-// Few places and small tables in one launch, without a sort: a wave has kScanRows rows of a table and a column slice, looks at
-// all tokens of the peer, four a lane, and takes those of each of its rows in ascending order of their places.
-constexpr int kScanRows = 16, kScanPlaces = 256;
+// Few places and small tables in one launch, without a sort: a wave has a few rows of a table and a column slice, looks at all
+// tokens of the peer, up to four a lane, and takes those of each of its rows in ascending order of their places.
+constexpr int kScanPlaces = 256;
 
 template <int ST, int YT, int VE, bool ADD>
 __global__ __launch_bounds__(kBlock) void embed_grad_scan_kernel(const int32_t *__restrict__ tokens, const char *__restrict__ dy, int64_t dy_stride,
-                                                                 char *__restrict__ base, TableGeom g, ShareGeom s, float scale)
+                                                                 char *__restrict__ base, TableGeom g, ShareGeom s, uint32_t run_rows,
+                                                                 float scale)
 {
     constexpr int ES = ST == 0 ? 4 : 2, EY = YT == 0 ? 4 : 2, CHUNKS = kScanPlaces / kWave;
     const uint32_t peer = blockIdx.x / s.blocks;
     const uint32_t part = blockIdx.x % s.blocks * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const uint32_t run = part / s.slices, slice = part % s.slices;
-    const uint32_t vocab = static_cast<uint32_t>(g.vocab), row0 = run * kScanRows;
+    const uint32_t vocab = static_cast<uint32_t>(g.vocab), row0 = run * run_rows;
     if (row0 >= vocab) return;
-    const uint32_t rows = vocab - row0 < kScanRows ? vocab - row0 : kScanRows;
+    const uint32_t rows = vocab - row0 < run_rows ? vocab - row0 : run_rows;
     const int lane = threadIdx.x & 63;
     uint32_t mine[CHUNKS];                                            // a token's row of this wave's, or any number from `rows` on
     uint64_t any = 0;
@@ -684,10 +685,15 @@ bool scan_does(const TableGeom &g) { return g.T > 0 && g.T <= kScanPlaces && g.N
 template <int ST, int YT, int VE, bool ADD>
 void launch_scan(void *base, const TableGeom &g, const int32_t *tokens, float scale, const void *dy, int64_t dy_stride, hipStream_t stream)
 {
-    ShareGeom s{(g.vocab + kScanRows - 1) / kScanRows, static_cast<uint32_t>((g.width + kWave * VE - 1) / (kWave * VE)), 0};
+    // as few rows a wave (2 .. 16) as keep the waves at 16384: rows with places wait for their loads one after the other (27 tables of
+    // 1001 x 100: 2 rows 8.2 us, 16 rows 9.6), and a wave's start costs as much as some rows (64 of 3785 x 24: 25.6 and 10.8)
+    const int64_t slices = (g.width + kWave * VE - 1) / (kWave * VE);
+    uint32_t rows = 2;
+    while (rows < 16 && g.N * g.vocab * slices / rows > 16384) rows *= 2;
+    ShareGeom s{(g.vocab + rows - 1) / rows, static_cast<uint32_t>(slices), 0};
     s.blocks = static_cast<uint32_t>((s.shares * s.slices + kWaves - 1) / kWaves);
     embed_grad_scan_kernel<ST, YT, VE, ADD><<<static_cast<uint32_t>(s.blocks * g.N), kBlock, 0, stream>>>(
-        tokens, static_cast<const char *>(dy), dy_stride, static_cast<char *>(base), g, s, scale);
+        tokens, static_cast<const char *>(dy), dy_stride, static_cast<char *>(base), g, s, rows, scale);
 }
 
 template <int ST, int YT, bool ADD>
