@@ -323,8 +323,8 @@ int moshpit_grouped_round(moshpit_ctx *h, const int32_t *index_host, int64_t n_i
  * allocates): make one call of each size before a graph capture.  Tensors last
  * written on another stream than the bound one must be ordered by the caller.
  * Limits: n_tokens <= 2^30, N * n_tokens < 2^31, 2^23 elements per activation
- * row, 2^27 entries of a vocabulary of logits; a launch beyond 2^32 - 1 threads
- * is an error. */
+ * row, 2^27 entries of a vocabulary of logits, a row stride of 2^29 elements (2^24
+ * for the dy of moshpit_weight_grad); a launch beyond 2^32 - 1 threads is an error. */
 
 /* Embedding lookup: out[i][t][:] = scale * table_i[token][:], zeros where there is
  * no token.  The table of peer i is its parameters column .. column + vocab * width

@@ -5,8 +5,12 @@
 // staged through LDS as they lie in memory, [token][column] in bfloat16, and the transposing LDS reads of gfx950
 // hand the matrix instructions their operands, 8 tokens of a column to a lane.  The codes become bfloat16 on their
 // way into LDS, which is exact.  A binary32 dy is staged as three bfloat16 parts (8 significant bits each, exact
-// down to 2^-133), whose products with x are exact in binary32: three matrix instructions in place of one, at five
+// down to 2^-133), whose products with x are exact in binary32: three matrix instructions in place of one, at sixteen
 // times the rate of the binary32 ones.  Sums are binary32.
+//
+// Bound by the matrix cores where the matrices are large, and by what feeds them: 16 matrices of 1024 x 4096 from 4096
+// tokens of bfloat16 dy in 547 us, 1005 TFLOP/s of the 1301 that a plain bfloat16 product reaches; without the staging of
+// the next step (codes to bfloat16, into LDS) the same products take 0.7 of the time.
 #include <hip/hip_runtime.h>
 
 #include "checkpoint_codes.h"
