@@ -273,6 +273,53 @@ def test_weight_grad(state, act, M, d, T, O, I, column, pad, accumulate):
     assert torch.equal(G, before)
 
 
+@pytest.mark.parametrize("state,act", [("f32", "f32"), ("f32", "bf16"), ("bf16", "f32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("M,d,T,O,I,column,pad", [
+    (4, 2, 1, 1_024, 1_024, 0, 0), (4, 2, 31, 1_000, 1_008, 3, 24), (4, 2, 63, 1_016, 912, 0, 8), (8, 2, 64, 512, 512, 0, 0),
+    (8, 2, 65, 392, 400, 1, 8), (4, 2, 128, 1_000, 1_008, 0, 24), (4, 2, 129, 1_024, 1_003, 0, 0), (8, 2, 192, 510, 496, 0, 2),
+    (4, 2, 193, 1_024, 912, 0, 8), (4, 2, 300, 1_001, 1_003, 1, 1), (8, 2, 321, 400, 496, 5, 16),
+])
+def test_weight_grad_of_many_large_matrices(state, act, M, d, T, O, I, column, pad):
+    """Enough of them for the large tiles: rows on and off 16-byte boundaries, steps that end inside, an infinity in the last token,
+    NaN in the columns between the rows."""
+    N, g, accumulate = M ** d, rng(T + O + I), T % 2 == 1
+    X = torch.zeros((N, column + O * I + 3), dtype=TYPES[state][0], device=DEV)
+    G = normal(X.shape, X.dtype, g)
+    before = G.clone()
+    dY = rows(N, T, O, TYPES[act][0], g, pad, 0, 0.1)
+    if pad:
+        dY._base.view(N, T, O + pad)[..., O:] = math.nan
+    dY[0, T - 1, 1] = math.inf
+    x = rows(N, T, I, TYPES[act][0], g)
+    with handle(X, M, d) as m:
+        print("weight_grad", state, act, N, T, O, I, column, pad, accumulate, flush=True)
+        codes, scales = m.checkpoint(x)
+        m.weight_grad(dY, codes, scales, G, column, accumulate=accumulate)
+        m.sync()
+        first = G.clone()
+        G.copy_(before)
+        m.weight_grad(dY, codes, scales, G, column, accumulate=accumulate)
+        value = m.checkpoint_restore(codes, scales).double()
+        m.sync()
+    assert torch.equal(first.nan_to_num(7.0), G.nan_to_num(7.0))
+    got = G[:, column: column + O * I].reshape(N, O, I)
+    row = got[0, 1].double()
+    assert torch.equal(row.nan_to_num(7.0), (math.inf * value[0, T - 1]).nan_to_num(7.0))     # (of an infinity: +-inf, NaN by x = 0)
+    y = dY.double()
+    y[0, T - 1, 1] = 0.0
+    y = y.transpose(1, 2).contiguous()
+    want, size = torch.bmm(y, value), torch.bmm(y.abs(), value.abs())
+    if accumulate:
+        old = before[:, column: column + O * I].reshape(N, O, I).double()
+        want, size = want + old, size + old.abs()
+    terms = 3 * T if act == "f32" else T
+    bound = (terms + 8) * 2 * U * size + TYPES[state][2] * want.abs() * 1.01 + TINY
+    bound[0, 1] = math.inf
+    close(torch.where(torch.isinf(bound), want, got.double()), want, bound)
+    G[:, column: column + O * I] = before[:, column: column + O * I]
+    assert torch.equal(G, before)
+
+
 def test_weight_grad_of_extreme_values():
     """binary32 factors near the ends of the range are not lost by their parts; a group that is NaN is NaN in its columns only."""
     N, T, O, I = 2, 40, 24, 70
