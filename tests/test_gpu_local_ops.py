@@ -578,7 +578,9 @@ def test_new_tensors_belong_to_the_bound_stream():
     with binding.Moshpit(N, 16, 2, 2, binding.F32) as m:
         m.bind_state(X, side)
         want, scales = m.checkpoint(x)
-        want, value = want.clone(), m.checkpoint_restore(want, scales).clone()
+        value = m.checkpoint_restore(want, scales)
+        m.sync()                                                      # (the clones are the current stream's)
+        want, value = want.clone(), value.clone()
         torch.cuda.synchronize()
         for _ in range(10):
             big = (big @ big).clamp_(-1, 1)
