@@ -9,8 +9,8 @@
 // times the rate of the binary32 ones.  Sums are binary32.
 //
 // Bound by the matrix cores where the matrices are large, and by what feeds them: 16 matrices of 1024 x 4096 from 4096
-// tokens of bfloat16 dy in 547 us, 1005 TFLOP/s of the 1301 that a plain bfloat16 product reaches; without the staging of
-// the next step (codes to bfloat16, into LDS) the same products take 0.7 of the time.
+// tokens of bfloat16 dy in 501 us, 1098 TFLOP/s of the 1301 that a plain bfloat16 product reaches (dy through registers on
+// its way into LDS: 547).  What remains is the codes' way through registers: without any staging the products take 0.74 of it.
 #include <hip/hip_runtime.h>
 
 #include "checkpoint_codes.h"
@@ -93,12 +93,17 @@ __device__ __forceinline__ u32x4 moved_down(const u32x4 &v, int bytes)
 // What a thread has in flight of a step's tiles: 8 outputs of YN tokens as they lie in memory, 16 codes of XN tokens and their scale
 // bytes.  Columns beyond a row's end: the thread reads the row's last ones instead and moves them to their place on the way into LDS;
 // tokens beyond the last: it reads the last one and puts zeros into LDS.
-template <int YT, typename T> struct Staged {
+//
+// DIRECT: dy goes from memory into LDS without passing through registers, a wave 1 KiB at a time: lane l's 16 bytes to where the wave's
+// rows begin + 16 * l, so the lane reads the columns that lds_at() puts there.  Columns beyond the row's end are read as the tile's
+// first ones (their sums are not stored), tokens beyond the last as the last one and then overwritten with zeros.
+template <int YT, typename T, bool DIRECT> struct Staged {
     static constexpr int PARTS = YT == 0 ? 3 : 1, EY = YT == 0 ? 4 : 2;
     static constexpr int TO = T::O, TI = T::I, K = T::K;
     static constexpr int Y_THREADS = TO / 8, YR = T::THREADS / Y_THREADS, YN = K / YR;        // threads of a token, tokens at a time, times
     static constexpr int X_THREADS = TI / 16, XR = T::THREADS / X_THREADS, XN = K / XR;
-    u32x4 y[YN][EY / 2], x[XN];
+    static constexpr int YH = DIRECT ? 0 : YN;                                 // of them through registers
+    u32x4 y[YH > 0 ? YH : 1][EY / 2], x[XN];
     uint32_t byte[XN];
 
     struct Place {
@@ -124,12 +129,45 @@ template <int YT, typename T> struct Staged {
         p.y_over = y_col() + 8 > yl ? y_col() + 8 - yl : 0;
         p.x_over = x_col() + 16 > xl ? x_col() + 16 - xl : 0;
         const int32_t yc = y_col() - p.y_over, xc = x_col() - p.x_over;         // (may be before the tile, not before the row)
-        p.y_from = static_cast<uint32_t>((o0 + yc) * EY);
+        if constexpr (DIRECT) {
+            const int32_t col = ((y_col() >> 5 ^ (y_row() & 3)) << 5) + (y_col() & 31);
+            p.y_from = static_cast<uint32_t>((o0 + (col < yl ? col : 0)) * EY);
+        } else
+            p.y_from = static_cast<uint32_t>((o0 + yc) * EY);
         p.x_from = static_cast<uint32_t>(c0 + xc);
         p.scale_from = static_cast<uint32_t>((c0 + (x_col() < xl ? x_col() : xl - 1)) / kCheckpointGroup);
         p.y_at = p.y_from + static_cast<uint32_t>(y_row() * p.y_step);
         p.x_at = p.x_from + static_cast<uint32_t>(x_row() * p.x_step);
         p.scale_at = p.scale_from + static_cast<uint32_t>(x_row() * p.scale_step);
+    }
+
+    // dy of the step whose first token is number t of the part's `count`, on its way into LDS.  FULL: the step is known to have K tokens.
+    template <bool FULL> __device__ __forceinline__ static void direct_y(const Place &p, int64_t t, int64_t count, uint16_t *lds_y)
+    {
+        typedef __attribute__((address_space(3))) uint16_t lds_u16;
+        static_assert(YR % 4 == 0 && 64 % Y_THREADS == 0 && YT == 1);           // (rows of a thread have the same number mod 4)
+        const int wave_row = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * (64 / Y_THREADS);
+        const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(p.y + t * p.y_step), 0, 0xffffffffu, 0x00027000);
+#pragma unroll
+        for (int n = 0; n < YN; ++n) {
+            uint32_t at = p.y_at, down = static_cast<uint32_t>(YR * n * p.y_step);       // below 2^31: K rows of up to 2^25 bytes
+            if constexpr (!FULL) {
+                const int64_t row = t + y_row() + YR * n < count ? y_row() + YR * n : count - 1 - t;
+                at = p.y_from + static_cast<uint32_t>(row) * static_cast<uint32_t>(p.y_step);
+                down = 0;
+            }
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_u16 *)(lds_y + (wave_row + YR * n) * TO), 16, at, down, 0, 0);
+        }
+    }
+    // All that this wave requested with direct_y() is in LDS; tokens from number `left` on become zeros.
+    template <bool FULL> __device__ __forceinline__ static void direct_done(int64_t left, uint16_t *lds_y)
+    {
+        __builtin_amdgcn_s_waitcnt(0x0f70);                                     // vmcnt(0)
+        if (!FULL && left < K) {
+#pragma unroll
+            for (int n = 0; n < YN; ++n)
+                if (y_row() + YR * n >= left) *reinterpret_cast<u32x4 *>(lds_y + (y_row() + YR * n) * TO + y_col()) = u32x4{0, 0, 0, 0};
+        }
     }
 
     // The step whose first token is number t of the part's `count`.
@@ -138,7 +176,7 @@ template <int YT, typename T> struct Staged {
         typedef u32x4 any_t __attribute__((aligned(1)));
         if (t + K <= count) {
 #pragma unroll
-            for (int n = 0; n < YN; ++n) {
+            for (int n = 0; n < YH; ++n) {
                 const char *from = p.y + (t + YR * n) * p.y_step + p.y_at;
 #pragma unroll
                 for (int q = 0; q < EY / 2; ++q) y[n][q] = *reinterpret_cast<const any_t *>(from + 16 * q);
@@ -152,7 +190,7 @@ template <int YT, typename T> struct Staged {
         }
         const int32_t left = static_cast<int32_t>(count - t);                   // 1 .. K - 1
 #pragma unroll
-        for (int n = 0; n < YN; ++n) {
+        for (int n = 0; n < YH; ++n) {
             const int32_t row = y_row() + YR * n < left ? y_row() + YR * n : left - 1;
             const char *from = p.y + t * p.y_step + (int64_t(row) * p.y_step + p.y_from);
 #pragma unroll
@@ -170,7 +208,7 @@ template <int YT, typename T> struct Staged {
     {
         if (!p.whole) {
 #pragma unroll
-            for (int n = 0; n < YN; ++n) {
+            for (int n = 0; n < YH; ++n) {
                 if constexpr (YT == 1) y[n][0] = moved_down(y[n][0], 2 * p.y_over);
                 else {
                     const int over = p.y_over < 8 ? p.y_over : 8;               // 8 values of 4 bytes: 4 and more move a vector down
@@ -192,7 +230,7 @@ template <int YT, typename T> struct Staged {
         }
         if (left < K) {
 #pragma unroll
-            for (int n = 0; n < YN; ++n)
+            for (int n = 0; n < YH; ++n)
                 if (y_row() + YR * n >= left)
 #pragma unroll
                     for (int q = 0; q < EY / 2; ++q) y[n][q] = u32x4{0, 0, 0, 0};
@@ -203,6 +241,14 @@ template <int YT, typename T> struct Staged {
                     byte[n] = 1;
                 }
         }
+    }
+
+    // Nothing of the codes and scales is waited for before this point.
+    __device__ __forceinline__ void wanted()
+    {
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int n = 0; n < XN; ++n) asm volatile("" : "+v"(x[n]), "+v"(byte[n]));
     }
 
     // Outputs of times n: into LDS, in parts.
@@ -246,15 +292,20 @@ template <int YT, typename T> struct Staged {
     }
 };
 
-template <int YT, int ST, bool ADD, bool PARTIAL, typename T>
+template <int YT, int ST, bool ADD, bool PARTIAL, typename T, bool DIRECT>
 __global__ __launch_bounds__(T::THREADS, 2)
 void weight_grad_kernel(const char *__restrict__ dy, const int8_t *__restrict__ codes, const uint8_t *__restrict__ scales, WeightGradGeom g,
                         Split s, char *__restrict__ base, float *__restrict__ partials)
 {
-    using St = Staged<YT, T>;
+    using St = Staged<YT, T, DIRECT>;
     constexpr int PARTS = St::PARTS, TO = T::O, TI = T::I, K = T::K, MO = T::MO, MI = T::MI, STEPS = K / 16;
     constexpr int Y_ELEMS = PARTS * K * TO, ELEMS = Y_ELEMS + K * TI;
-    extern __shared__ __attribute__((aligned(16))) uint16_t lds[];       // two buffers of ELEMS
+    // Two buffers of a step's tiles.  With DIRECT they are four variables: an access to one does not wait for what is on its way
+    // into another.
+    __shared__ __attribute__((aligned(16))) uint16_t y_even[DIRECT ? Y_ELEMS : 2 * ELEMS];
+    __shared__ __attribute__((aligned(16))) uint16_t y_odd[DIRECT ? Y_ELEMS : 8];
+    __shared__ __attribute__((aligned(16))) uint16_t x_even[DIRECT ? K * TI : 8];
+    __shared__ __attribute__((aligned(16))) uint16_t x_odd[DIRECT ? K * TI : 8];
 
     // a die takes a run of tiles, so that the tiles of a peer share its operands in the die's cache
     uint32_t b = die_run(blockIdx.x, gridDim.x);
@@ -286,12 +337,12 @@ void weight_grad_kernel(const char *__restrict__ dy, const int8_t *__restrict__ 
     constexpr int UNITS = STEPS * PARTS, LATE = UNITS / 2;
     St st;
     bf16x8 xi[2][MI], yo[2][MO];
-    auto read = [&](uint32_t buffer, int u) {
-        const uint16_t *tile_y = lds + buffer + (PARTS - 1 - u % PARTS) * K * TO, *tile_x = lds + buffer + Y_ELEMS;
+    auto read = [&](const uint16_t *lds_y, const uint16_t *lds_x, int u) {
+        const uint16_t *tile_y = lds_y + (PARTS - 1 - u % PARTS) * K * TO;
         const int k = u / PARTS;
         if (u % PARTS == 0)
 #pragma unroll
-            for (int n = 0; n < MI; ++n) xi[k & 1][n] = operand<TI>(tile_x, 16 * k, wi + 32 * n);
+            for (int n = 0; n < MI; ++n) xi[k & 1][n] = operand<TI>(lds_x, 16 * k, wi + 32 * n);
 #pragma unroll
         for (int m = 0; m < MO; ++m) yo[u & 1][m] = operand<TO>(tile_y, 16 * k, wo + 32 * m);
     };
@@ -302,38 +353,69 @@ void weight_grad_kernel(const char *__restrict__ dy, const int8_t *__restrict__ 
             for (int n = 0; n < MI; ++n)
                 acc[m][n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(yo[u & 1][m], xi[u / PARTS & 1][n], acc[m][n], 0, 0, 0);
     };
-    auto to_lds = [&](uint32_t buffer, int part, int parts) {
+    auto to_lds = [&](uint16_t *lds_y, uint16_t *lds_x, int part, int parts) {
 #pragma unroll
-        for (int n = part * St::YN / parts; n < (part + 1) * St::YN / parts; ++n) st.store_y(n, lds + buffer);
+        for (int n = part * St::YH / parts; n < (part + 1) * St::YH / parts; ++n) st.store_y(n, lds_y);
 #pragma unroll
-        for (int n = part * St::XN / parts; n < (part + 1) * St::XN / parts; ++n) st.store_x(n, lds + buffer + Y_ELEMS);
+        for (int n = part * St::XN / parts; n < (part + 1) * St::XN / parts; ++n) st.store_x(n, lds_x);
     };
-    uint32_t buffer = 0;
     int64_t t = 0;
     if (count > 0) {
+        if constexpr (DIRECT) St::template direct_y<false>(place, 0, count, y_even);
         st.load(place, 0, count);
         st.trim(place, count);
-        to_lds(0, 0, 1);
+        to_lds(y_even, DIRECT ? x_even : y_even + Y_ELEMS, 0, 1);
+        if constexpr (DIRECT) St::template direct_done<false>(count, y_even);
         if (K < count) st.load(place, K, count);
         __syncthreads();
     }
-    for (; t + K < count; t += K, buffer = ELEMS - buffer) {
-        read(buffer, 0);
+    // step t's products from `now`, step t + K's tiles into `next`
+    auto step = [&](auto full, const uint16_t *y_now, const uint16_t *x_now, uint16_t *y_next, uint16_t *x_next) {
+        constexpr bool FULL = decltype(full)::value;
+        if constexpr (DIRECT) St::template direct_y<FULL>(place, t + K, count, y_next);
+        if constexpr (DIRECT) __builtin_amdgcn_sched_barrier(0);                // (requested now, not when the products are through)
+        read(y_now, x_now, 0);
 #pragma unroll
         for (int u = 0; u < UNITS; ++u) {
-            if (u == LATE && (!place.whole || t + 2 * K > count)) st.trim(place, count - t - K);
-            if (u + 1 < UNITS) read(buffer, u + 1);
+            if constexpr (DIRECT)
+                if (u == LATE) st.wanted();
+            if (!FULL && u == LATE && (!place.whole || t + 2 * K > count)) st.trim(place, count - t - K);
+            if (u + 1 < UNITS) read(y_now, x_now, u + 1);
             multiply(u);
-            if (u >= LATE) to_lds(ELEMS - buffer, u - LATE, UNITS - LATE);
+            if (u >= LATE) to_lds(y_next, x_next, u - LATE, UNITS - LATE);
         }
+        if constexpr (DIRECT) St::template direct_done<FULL>(count - t - K, y_next);
         if (t + 2 * K < count) st.load(place, t + 2 * K, count);
         __syncthreads();
+        t += K;
+    };
+    const uint16_t *y_last = y_even, *x_last = x_even;
+    if constexpr (DIRECT) {              // (two steps by name: which variable an access meets has to be known where it stands)
+        while (t + 3 * K <= count) {
+            step(std::true_type{}, y_even, x_even, y_odd, x_odd);
+            step(std::true_type{}, y_odd, x_odd, y_even, x_even);
+        }
+        const bool odd_whole = t + 2 * K <= count;
+        if (odd_whole) step(std::true_type{}, y_even, x_even, y_odd, x_odd);
+        bool odd = odd_whole;
+        if (t + K < count) {
+            step(std::false_type{}, odd ? y_odd : y_even, odd ? x_odd : x_even, odd ? y_even : y_odd, odd ? x_even : x_odd);
+            odd = !odd;
+        }
+        y_last = odd ? y_odd : y_even;
+        x_last = odd ? x_odd : x_even;
+    } else {
+        uint32_t now = 0;
+        for (; t + K < count; now = ELEMS - now)
+            step(std::false_type{}, y_even + now, y_even + now + Y_ELEMS, y_even + (ELEMS - now), y_even + (ELEMS - now) + Y_ELEMS);
+        y_last = y_even + now;
+        x_last = y_last + Y_ELEMS;
     }
     if (count > 0) {
-        read(buffer, 0);
+        read(y_last, x_last, 0);
 #pragma unroll
         for (int u = 0; u < UNITS; ++u) {
-            if (u + 1 < UNITS) read(buffer, u + 1);
+            if (u + 1 < UNITS) read(y_last, x_last, u + 1);
             __builtin_amdgcn_sched_barrier(0);
             multiply(u);
         }
@@ -427,16 +509,18 @@ hipError_t launch_products(const char *dy, const int8_t *codes, const uint8_t *s
 {
     constexpr int WIDE_K = YT == 0 ? 32 : 64, NARROW_K = 32;
     const uint32_t blocks = static_cast<uint32_t>(g.N * s.parts * s.tiles_o * s.tiles_i);
-    auto go = [&](auto kernel, int threads, int lds) {
-        const hipError_t e = ensure_dynamic_lds(reinterpret_cast<const void *>(kernel), lds);
-        if (e != hipSuccess) return e;
-        kernel<<<blocks, threads, lds, stream>>>(dy, codes, scales, g, s, base, work);
+    auto go = [&](auto kernel, int threads) {
+        kernel<<<blocks, threads, 0, stream>>>(dy, codes, scales, g, s, base, work);
         return hipGetLastError();
     };
-    constexpr int PARTS = YT == 0 ? 3 : 1;
+    if constexpr (!PARTIAL && YT == 1)
+        // dy straight into LDS where its rows are whole 16-byte vectors: 16 x 1024 x 2048 from 1024 tokens in 84 us (through registers 93),
+        // 16 x 1000 x 1008 from 4096 in 129 (147); 64 x 512 x 3584 from 64, a single step, in 101 (100)
+        if (wide && (reinterpret_cast<uintptr_t>(dy) & 15) == 0 && g.dy_stride % 8 == 0 && g.outs % 8 == 0 && g.ins % 16 == 0)
+            return go(weight_grad_kernel<YT, ST, ADD, false, Tile<2, 4, 4, 2, WIDE_K>, true>, 512);
     if constexpr (!PARTIAL)
-        if (wide) return go(weight_grad_kernel<YT, ST, ADD, false, Tile<2, 4, 4, 2, WIDE_K>>, 512, 2 * 2 * WIDE_K * 256 * (PARTS + 1));
-    return go(weight_grad_kernel<YT, ST, ADD, PARTIAL, Tile<2, 2, 2, 2, NARROW_K>>, 256, 2 * 2 * NARROW_K * 128 * (PARTS + 1));
+        if (wide) return go(weight_grad_kernel<YT, ST, ADD, false, Tile<2, 4, 4, 2, WIDE_K>, false>, 512);
+    return go(weight_grad_kernel<YT, ST, ADD, PARTIAL, Tile<2, 2, 2, 2, NARROW_K>, false>, 256);
 }
 
 template <int YT, int ST, bool ADD>
