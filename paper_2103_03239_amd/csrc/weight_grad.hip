@@ -513,11 +513,14 @@ hipError_t launch_products(const char *dy, const int8_t *codes, const uint8_t *s
         kernel<<<blocks, threads, 0, stream>>>(dy, codes, scales, g, s, base, work);
         return hipGetLastError();
     };
-    if constexpr (!PARTIAL && YT == 1)
-        // dy straight into LDS where its rows are whole 16-byte vectors: 16 x 1024 x 2048 from 1024 tokens in 84 us (through registers 93),
-        // 16 x 1000 x 1008 from 4096 in 129 (147); 64 x 512 x 3584 from 64, a single step, in 101 (100)
-        if (wide && (reinterpret_cast<uintptr_t>(dy) & 15) == 0 && g.dy_stride % 8 == 0 && g.outs % 8 == 0 && g.ins % 16 == 0)
-            return go(weight_grad_kernel<YT, ST, ADD, false, Tile<2, 4, 4, 2, WIDE_K>, true>, 512);
+    // dy straight into LDS where its rows are whole 16-byte vectors: 16 x 1024 x 2048 from 1024 tokens in 84 us (through registers 93),
+    // 16 x 1000 x 1008 from 4096 in 129 (147), 2 x 1024 x 1024 from 4096 in 41 (43); 64 x 512 x 3584 from 64, a single step, in 101 (100)
+    if constexpr (YT == 1)
+        if ((reinterpret_cast<uintptr_t>(dy) & 15) == 0 && g.dy_stride % 8 == 0 && g.outs % 8 == 0 && g.ins % 16 == 0) {
+            if constexpr (!PARTIAL)
+                if (wide) return go(weight_grad_kernel<YT, ST, ADD, false, Tile<2, 4, 4, 2, WIDE_K>, true>, 512);
+            return go(weight_grad_kernel<YT, ST, ADD, PARTIAL, Tile<2, 2, 2, 2, NARROW_K>, true>, 256);
+        }
     if constexpr (!PARTIAL)
         if (wide) return go(weight_grad_kernel<YT, ST, ADD, false, Tile<2, 4, 4, 2, WIDE_K>, false>, 512);
     return go(weight_grad_kernel<YT, ST, ADD, PARTIAL, Tile<2, 2, 2, 2, NARROW_K>, false>, 256);
