@@ -9,8 +9,9 @@
 // times the rate of the binary32 ones.  Sums are binary32.
 //
 // Bound by the matrix cores where the matrices are large, and by what feeds them: 16 matrices of 1024 x 4096 from 4096
-// tokens of bfloat16 dy in 501 us, 1098 TFLOP/s of the 1301 that a plain bfloat16 product reaches (dy through registers on
-// its way into LDS: 547).  What remains is the codes' way through registers: without any staging the products take 0.74 of it.
+// tokens of bfloat16 dy in 501 to 535 us by card, 1030 to 1100 TFLOP/s of the 1301 that a plain bfloat16 product reaches.  dy
+// through registers on its way into LDS takes 6 % longer (613 against 578 us on one card, back to back); what remains is the
+// codes' way through registers: without any staging the products take 0.74 of it.
 #include <hip/hip_runtime.h>
 
 #include "checkpoint_codes.h"
@@ -471,7 +472,13 @@ __global__ __launch_bounds__(kBlock) void weight_grad_join_kernel(const float *_
     const int64_t all = N * count;
     for (int64_t k = int64_t(blockIdx.x) * kBlock + threadIdx.x; k < all; k += int64_t(gridDim.x) * kBlock) {
         float sum = 0.f;
-        for (int32_t p = 0; p < parts; ++p) sum += partials[p * all + k];
+        for (int32_t p = 0; p < parts; p += 8) {                      // eight requested at a time
+            float v[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) v[u] = p + u < parts ? partials[(p + u) * all + k] : 0.f;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) sum += v[u];
+        }
         char *at = base + ((k / count) * peer_stride + k % count) * ES;
         store_one<ST>(at, ADD ? load_one<ST>(at) + sum : sum);
     }
@@ -493,9 +500,12 @@ Split split_of(const WeightGradGeom &g, int dy_dtype, int compute_units)
     s.tiles_o = static_cast<int32_t>((g.outs + tile - 1) / tile);
     s.tiles_i = static_cast<int32_t>((g.ins + tile - 1) / tile);
     const int64_t tiles = g.N * s.tiles_o * s.tiles_i, steps = (g.T + step - 1) / step;
-    // parts of at least 8 steps until every compute unit has two blocks
+    // Parts of at least 8 steps until every compute unit has two blocks.  A step of binary32 takes 1 to 2 us, three times one of bfloat16, the
+    // join about 4: where the sums are few, 4 steps there (2 x 393 x 68 from 371 tokens: 13.6 us, with 8 23.5; 16 x 256 x 256 from 300:
+    // 18.0 and 16.1; in bfloat16 2 x 392 x 64 from 371: 12.7 and 10.0).
+    const int64_t least = dy_dtype == 0 && g.N * g.outs * g.ins <= (1 << 19) ? 4 : 8;
     int64_t parts = wide ? 1 : 2 * compute_units / tiles;
-    if (parts > steps / 8) parts = steps / 8;
+    if (parts > steps / least) parts = steps / least;
     if (parts < 1) parts = 1;
     const int64_t each = (steps + parts - 1) / parts;
     s.tokens = (each > 0 ? each : 1) * step;
