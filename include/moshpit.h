@@ -377,7 +377,9 @@ int moshpit_token_logp(moshpit_ctx *h, const void *logits_dev, int32_t dtype, in
  * The caller's weights hold the mask and the mean (1 / number of tokens, for
  * instance).  Places with weight 0 or without a token are not read: gradient and lp
  * are 0 there, whatever the logits hold.  Logits of -inf (excluded tokens) have
- * probability and gradient 0; a row of nothing else gives NaN.
+ * probability and gradient 0; a row of nothing else gives NaN.  Finite logits count as
+ * what they are, the type's lowest value too: beside larger ones it excludes a token, a
+ * row of nothing else has all tokens alike.
  * ref_logp_dev may be NULL when kl_coef is 0.  grad_dev: laid out like the logits and
  * of their type; it may be the logits themselves (same row stride) but must not
  * overlap them in any other way.  logp_dev: [N][n_tokens] floats.  stats_dev: [N][3]

@@ -21,7 +21,7 @@
 namespace moshpit {
 namespace {
 
-constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+constexpr float kLog2e = 1.44269504088896340736f;
 
 // exp(x - m), m finite or x = m = -inf excluded by the caller
 __device__ __forceinline__ float exp_above(float x, float m) { return __builtin_amdgcn_exp2f((x - m) * kLog2e); }
@@ -126,21 +126,21 @@ template <int VE> __device__ __forceinline__ float largest(const float (&f)[VE])
     return top;
 }
 
-// The sum of exp(f - m), with less = -m log2 e: one fused multiply-add and one exponential a value.  Its rounding of m log2 e is
-// the same for all values of a row, so it cancels in exp(z - m) / sum and is one rounding of m in the log-probability.
-template <int VE> __device__ __forceinline__ float sum_exp(const float (&f)[VE], float less)
+// The sum of exp(f - m).  The difference comes first: -m log2 e in a fused multiply-add would be off by 2^-24 of its own size, which
+// grows with an offset common to the row, and infinite for m near the type's lowest value, as a mask may be.
+template <int VE> __device__ __forceinline__ float sum_exp(const float (&f)[VE], float m)
 {
     float e[VE];
 #pragma unroll
-    for (int k = 0; k < VE; ++k) e[k] = __builtin_amdgcn_exp2f(fmaf(f[k], kLog2e, less));
+    for (int k = 0; k < VE; ++k) e[k] = exp_above(f[k], m);
 #pragma unroll
     for (int w = VE / 2; w > 0; w /= 2)
 #pragma unroll
         for (int k = 0; k < w; ++k) e[k] += e[k + w];
     return e[0];
 }
-// What `less` is for a largest value: -inf alone gives exp(-inf) = 0.
-__device__ __forceinline__ float less_of(float top) { return top == -INFINITY ? 0.f : -top * kLog2e; }
+// What is taken from values whose largest is `top`: of -inf alone nothing, so that exp(-inf) = 0.
+__device__ __forceinline__ float base_of(float top) { return top == -INFINITY ? 0.f : top; }
 
 template <int VE> __device__ __forceinline__ void add_values(TopSum &t, const float (&f)[VE])
 {
@@ -149,7 +149,7 @@ template <int VE> __device__ __forceinline__ void add_values(TopSum &t, const fl
         t.sum *= t.top == -INFINITY ? 0.f : exp_above(t.top, top);
         t.top = top;
     }
-    t.sum += sum_exp(f, less_of(t.top));
+    t.sum += sum_exp(f, base_of(t.top));
 }
 
 // What was made of these registers is not to be kept for the next pass over them: the row as it came is all there is room for.
@@ -254,24 +254,24 @@ void policy_row_kernel(const char *logits, int64_t rows, RowPlace at, const int3
         t.top = fmaxf(t.top, largest(f));
     }
     keep_packed(held);
-    const float own_less = less_of(t.top);
-    t.sum = __builtin_amdgcn_exp2f(fmaf(single, kLog2e, own_less));
+    const float own_base = base_of(t.top);
+    t.sum = exp_above(single, own_base);
 #pragma unroll
     for (int v = 0; v < VECS; ++v) {
         if (v * THREADS + static_cast<int32_t>(threadIdx.x) >= s.count) continue;
         float f[VE];
         widen_vec<DT>(held[v], f);
-        t.sum += sum_exp(f, own_less);
+        t.sum += sum_exp(f, own_base);
     }
     keep_packed(held);
     t = block_join<THREADS>(t);
-    float slope, factor, less;
+    float slope, factor, top;
     if (threadIdx.x < 64) {                                           // (the same for all its lanes)
         const float lp = z_token - t.top - logf(t.sum);
         RowTerms mine;
         slope = row_terms(p, row, w, lp, mine);
         factor = -slope / t.sum;
-        less = -t.top * kLog2e;                                       // (a row of -inf alone: NaN)
+        top = t.top;                                                  // (a row of -inf alone: NaN)
         if (threadIdx.x == 0) out.put(row, lp, mine);
     }
     if constexpr (THREADS > 64) {
@@ -279,12 +279,12 @@ void policy_row_kernel(const char *logits, int64_t rows, RowPlace at, const int3
         if (threadIdx.x == 0) {
             of_row[0] = slope;
             of_row[1] = factor;
-            of_row[2] = less;
+            of_row[2] = top;
         }
         __syncthreads();
         slope = of_row[0];
         factor = of_row[1];
-        less = of_row[2];
+        top = of_row[2];
     }
     const int32_t token_vec = static_cast<int32_t>((token - s.head) >> (DT == 0 ? 2 : 3));       // (may be none of the whole ones)
     const int32_t token_elem = static_cast<int32_t>(token - s.head) & (VE - 1);
@@ -295,7 +295,7 @@ void policy_row_kernel(const char *logits, int64_t rows, RowPlace at, const int3
         float f[VE];
         widen_vec<DT>(held[v], f);
 #pragma unroll
-        for (int k = 0; k < VE; ++k) f[k] = factor * __builtin_amdgcn_exp2f(fmaf(f[k], kLog2e, less));
+        for (int k = 0; k < VE; ++k) f[k] = factor * exp_above(f[k], top);
         if (i == token_vec) {
 #pragma unroll
             for (int k = 0; k < VE; ++k)
@@ -305,7 +305,7 @@ void policy_row_kernel(const char *logits, int64_t rows, RowPlace at, const int3
     }
     if (static_cast<int32_t>(threadIdx.x) < s.head + s.tail) {
         const int64_t e = s.single(threadIdx.x);
-        store_one<DT>(to + e * ES, factor * __builtin_amdgcn_exp2f(fmaf(single, kLog2e, less)) + (token == e ? slope : 0.f));
+        store_one<DT>(to + e * ES, factor * exp_above(single, top) + (token == e ? slope : 0.f));
     }
 }
 
@@ -356,11 +356,11 @@ void short_rows_kernel(const char *logits, int64_t rows, RowPlace at, const int3
             top = fmaxf(top, largest(f[v]));
         }
         top = wave_top(top);
-        const float less = less_of(top);
-        float sum = __builtin_amdgcn_exp2f(fmaf(single[r], kLog2e, less));
+        const float base = base_of(top);
+        float sum = exp_above(single[r], base);
 #pragma unroll
         for (int v = 0; v < kShortVecs; ++v)
-            if (v * 64 + lane < s.count) sum += sum_exp(f[v], less);
+            if (v * 64 + lane < s.count) sum += sum_exp(f[v], base);
         sum = wave_sum(sum);
         if (lane == r) mine = TopSum{top, sum};
         if constexpr (GRAD) keep_packed(held[r]);
@@ -373,7 +373,7 @@ void short_rows_kernel(const char *logits, int64_t rows, RowPlace at, const int3
         if (lane < count) out.put(own, lp, terms);
     } else if (lane < count) out.logp[own] = lp;
     if constexpr (!GRAD) return;
-    const float factor = -slope / mine.sum, less = -mine.top * kLog2e;
+    const float factor = -slope / mine.sum;
     auto lane_value = [](float v, int r) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), r)); };
 #pragma unroll
     for (int r = 0; r < kShort; ++r) {
@@ -386,7 +386,7 @@ void short_rows_kernel(const char *logits, int64_t rows, RowPlace at, const int3
             continue;
         }
         const Slice<DT> s(logits + (first + r) * at.stride * ES, at.vocab);
-        const float row_slope = lane_value(slope, r), row_factor = lane_value(factor, r), row_less = lane_value(less, r);
+        const float row_slope = lane_value(slope, r), row_factor = lane_value(factor, r), row_top = lane_value(mine.top, r);
         const int32_t row_token = __builtin_amdgcn_readlane(token, r);
 #pragma unroll
         for (int v = 0; v < kShortVecs; ++v) {
@@ -396,12 +396,12 @@ void short_rows_kernel(const char *logits, int64_t rows, RowPlace at, const int3
             widen_vec<DT>(held[r][v], f);
             const int32_t e = s.head + i * VE;
 #pragma unroll
-            for (int k = 0; k < VE; ++k) f[k] = row_factor * __builtin_amdgcn_exp2f(fmaf(f[k], kLog2e, row_less)) + (row_token == e + k ? row_slope : 0.f);
+            for (int k = 0; k < VE; ++k) f[k] = row_factor * exp_above(f[k], row_top) + (row_token == e + k ? row_slope : 0.f);
             store_elems<DT, VE, true>(to + e * ES, f);
         }
         if (lane < s.head + s.tail) {
             const int64_t e = s.single(lane);
-            store_one<DT>(to + e * ES, row_factor * __builtin_amdgcn_exp2f(fmaf(single[r], kLog2e, row_less)) + (row_token == e ? row_slope : 0.f));
+            store_one<DT>(to + e * ES, row_factor * exp_above(single[r], row_top) + (row_token == e ? row_slope : 0.f));
         }
     }
 }
@@ -488,7 +488,7 @@ __global__ __launch_bounds__(THREADS) void policy_slice_kernel(const char *logit
     RowTerms mine;
     const float slope = row_terms(p, row, w, lp, mine);
     if (slice == 0 && threadIdx.x == 0) out.put(row, lp, mine);
-    const float factor = -slope / t.sum, less = -t.top * kLog2e;
+    const float factor = -slope / t.sum;
     const char *from = logits + (row * at.stride + begin) * ES;
     const Slice<DT, line_of(THREADS)> s(from, end - begin);
     for (int32_t i0 = threadIdx.x; i0 < s.count; i0 += THREADS * kBatch) {
@@ -504,7 +504,7 @@ __global__ __launch_bounds__(THREADS) void policy_slice_kernel(const char *logit
             widen_vec<DT>(m[u], f);
             const int64_t e = s.head + int64_t(i) * VE;
 #pragma unroll
-            for (int k = 0; k < VE; ++k) f[k] = factor * __builtin_amdgcn_exp2f(fmaf(f[k], kLog2e, less));
+            for (int k = 0; k < VE; ++k) f[k] = factor * exp_above(f[k], t.top);
             if (token >= begin + e && token < begin + e + VE) {
 #pragma unroll
                 for (int k = 0; k < VE; ++k)
@@ -515,7 +515,7 @@ __global__ __launch_bounds__(THREADS) void policy_slice_kernel(const char *logit
     }
     for (int k = threadIdx.x; k < s.head + s.tail; k += THREADS) {
         const int64_t e = s.single(k);
-        store_one<DT>(to + e * ES, factor * __builtin_amdgcn_exp2f(fmaf(load_one<DT>(from + e * ES), kLog2e, less)) + (token == begin + e ? slope : 0.f));
+        store_one<DT>(to + e * ES, factor * exp_above(load_one<DT>(from + e * ES), t.top) + (token == begin + e ? slope : 0.f));
     }
 }
 

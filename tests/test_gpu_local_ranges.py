@@ -1,0 +1,109 @@
+"""The local step's operators over the whole range of their values: masks of the type's lowest value, common offsets, saved groups at
+the top of the range.  Bounds follow from the operations as in test_gpu_local_ops.py; a binary32 operation is off by U = 2^-24 of its result."""
+import math
+
+import pytest
+import torch
+
+from test_gpu_local_ops import DEV, TINY, TYPES, U, close, handle, rng, rows
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- policy loss ------------------------------------------------------------------
+
+def loss_inputs(z, tokens, g):
+    """Old and reference log-probabilities around the policy's, advantages and weights; off the kinks by more than rounding."""
+    lp = z.double().log_softmax(-1).gather(2, tokens.long()[..., None])[..., 0]
+    ratio = torch.empty(lp.shape, device=DEV).normal_(0, 0.3, generator=g).exp_()
+    for edge in (0.8, 1.3):
+        ratio = torch.where((ratio / edge - 1).abs() < 2e-3, ratio * 1.01, ratio)
+    return {"z": z, "tokens": tokens, "old": (lp - ratio.log()).float(), "ref": (lp + torch.empty(lp.shape, device=DEV).normal_(0, 0.4, generator=g)).float(),
+            "adv": torch.empty(lp.shape, device=DEV).normal_(generator=g), "w": 0.25 + torch.rand(lp.shape, generator=g, device=DEV)}
+
+
+def loss_want(c, kl):
+    """In binary64: gradient, stats, lp, and how far binary32 may be off each where a row's largest value is taken from every value first.  Then
+    z - m, its product with log2 e and exp2 are off by U (m - z), U (m - z) and 2 U, the sum of n terms by n U, and the log-probability
+    (z_a - m) - log sum by what its terms are, whatever m is."""
+    z, tok = c["z"].double(), c["tokens"].long()[..., None]
+    V = z.shape[2]
+    m, z_a = z.amax(-1), z.gather(2, tok)[..., 0]
+    above = torch.logsumexp(z - m[..., None], -1)
+    lp = (z_a - m) - above
+    p = (z - m[..., None] - above[..., None]).exp()
+    d = torch.where(p == 0.0, 0.0, m[..., None] - z)
+    w, A, old, rf = (c[k].double() for k in ("w", "adv", "old", "ref"))
+    low, high = 1.0 - float(torch.tensor(0.2)), 1.0 + float(torch.tensor(0.3))
+    kl = float(torch.tensor(kl))
+    r, e = (lp - old).exp(), (rf - lp).exp()
+    gain, held, k = A * r, A * r.clamp(low, high), e - (rf - lp) - 1
+    clipped = gain > held
+    loss = w * (kl * k - torch.minimum(gain, held))
+    slope = w * (kl * (1 - e) - torch.where(clipped, torch.zeros_like(gain), gain))
+    grad = -slope[..., None] * p
+    grad.scatter_add_(2, tok, slope[..., None])
+    n = max(128, V / 256) + 32
+    s_off = U * (n + 4 + 3 * (p * d).sum(-1))
+    lp_off = 4 * U * ((m - z_a) + above + lp.abs()) + s_off
+    r_off, e_off = lp_off + U * (lp.abs() + old.abs() + 4), lp_off + U * (lp.abs() + rf.abs() + 4)
+    slope_off = w * (abs(kl) * (e * e_off + 2 * U * (1 + e)) + gain.abs() * (r_off + 4 * U)) + 4 * U * slope.abs()
+    k_off = w * (e * e_off + lp_off + 4 * U * (e + (rf - lp).abs() + 1))
+    loss_off = abs(kl) * k_off + w * gain.abs() * (r_off + 4 * U) + 4 * U * loss.abs()
+    grad_off = slope_off[..., None] * (p + torch.zeros_like(p).scatter_(2, tok, 1.0)) + slope.abs()[..., None] * p * (U * (3 * d + 8) + s_off[..., None]) \
+        + 2 * U * grad.abs()
+    wk, wc = w * k, torch.where(clipped, w, 0.0)
+    off = torch.stack([loss_off.sum(1) + 2 * U * loss.abs().sum(1), k_off.sum(1) + 2 * U * wk.abs().sum(1), 2 * U * wc.sum(1)], 1)
+    return grad, torch.stack([loss.sum(1), wk.sum(1), wc.sum(1)], 1), lp, grad_off, off, lp_off
+
+
+def check_loss(c, act, kl, M, d):
+    X = torch.zeros((M ** d, 16), device=DEV)
+    grad = torch.full_like(c["z"], 7.0)
+    want = loss_want(c, kl)
+    with handle(X, M, d) as m:
+        scored = m.token_logp(c["z"], c["tokens"])
+        stats, logp = m.policy_loss(c["z"], c["tokens"], c["old"], c["adv"], c["w"], ref_logp=c["ref"], clip_low=0.2, clip_high=0.3, kl_coef=kl, grad=grad)
+        m.sync()
+    close(scored, want[2], want[5])
+    close(logp, want[2], want[5])
+    close(stats, want[1], want[4] + TINY)
+    close(grad, want[0], want[3] + TYPES[act][2] * want[0].abs() * 1.01 + TINY)
+
+
+# rows by 64 .. 1024 threads, in slices, many short ones, many that one block each scores
+LOGITS = [(10, 2), (10, 7), (10, 512), (10, 3_000), (10, 6_000), (10, 12_000), (10, 24_000), (10, 50_001), (10, 100_000), (8, 140_003), (2_100, 300), (2_100, 512), (600, 6_001)]
+
+
+@pytest.mark.parametrize("act", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V", LOGITS)
+def test_masks_of_the_types_lowest_value(act, T, V):
+    """Excluded tokens as the type's lowest value: most of a row, all but its token, its first or last part, all of it (every token alike),
+    and beside -inf."""
+    g, dtype = rng(T + V), TYPES[act][0]
+    low = torch.finfo(dtype).min
+    z = rows(2, T, V, dtype, g, scale=2.0).contiguous()
+    tokens = torch.randint(0, V, (2, T), generator=g, device=DEV, dtype=torch.int32)
+    at, kind = torch.arange(V, device=DEV), torch.arange(T, device=DEV) % 6
+    few = torch.rand((2, T, V), generator=g, device=DEV) < 100.0 / V
+    masked = torch.stack([~few, torch.ones_like(few), (at < V * 3 // 4).expand_as(few), (at >= V - 16).expand_as(few), torch.ones_like(few), torch.ones_like(few)])
+    masked = masked[kind, :, torch.arange(T, device=DEV)].transpose(0, 1)
+    masked = masked.scatter(2, tokens.long()[..., None], ((kind == 4) | (kind == 5))[None, :, None].expand(2, T, 1))
+    z[masked] = low
+    z.masked_fill_((kind == 5)[None, :, None] & (at % 3 == 0) & (at != tokens[..., None]), -math.inf)
+    print("lowest", act, T, V, flush=True)
+    check_loss(loss_inputs(z, tokens, g), act, 0.1, 2, 1)
+
+
+@pytest.mark.parametrize("act", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V", LOGITS)
+@pytest.mark.parametrize("offset", [1_024.0, -16_384.0])
+def test_an_offset_common_to_a_row_is_no_error(act, T, V, offset):
+    """The loss does not change when a row's logits move together: nor do its errors, however far."""
+    g, dtype = rng(T + V), TYPES[act][0]
+    spacing = 2.0 ** -7 * abs(offset) if act == "bf16" else 0.25
+    z = (offset - spacing * torch.randint(0, 3 if act == "bf16" else 40, (2, T, V), generator=g, device=DEV)).to(dtype)
+    tokens = torch.randint(0, V, (2, T), generator=g, device=DEV, dtype=torch.int32)
+    c = loss_inputs(z, tokens, g)
+    print("offset", act, T, V, offset, flush=True)
+    check_loss(c, act, 0.1, 2, 1)
