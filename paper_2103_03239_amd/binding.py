@@ -365,7 +365,7 @@ class Moshpit:
         peer, row, col = x.stride()
         if width > 1 and col != 1:
             raise ValueError(f"{name} must have unit column stride")
-        stride = row if n > 1 else (peer if peer >= width else width)
+        stride = row if n > 1 else peer if n == 1 else max(peer, width)      # (of no rows any stride will do)
         if n > 1 and peer != n * row or stride < width:
             raise ValueError(f"rows of {name} must lie at one constant distance over all peers and tokens")
         return x.data_ptr(), self._type_code(x.dtype), n, width, stride
