@@ -319,8 +319,9 @@ int moshpit_grouped_round(moshpit_ctx *h, const int32_t *index_host, int64_t n_i
  * an absent peer has nothing else).  Arithmetic and sums are binary32 (or wider),
  * rounded once when stored; the order of every sum follows from the sizes and the
  * tokens alone, so a call repeats to the bit.  Workspace belongs to the handle and
- * grows at the first call that needs more (that call waits for the stream and
- * allocates): make one call of each size before a graph capture.  Tensors last
+ * grows at the first call that needs more (that call allocates): make one call of
+ * each size before a graph capture.  What it has outgrown is kept until
+ * moshpit_destroy, so a captured graph may be replayed after larger calls.  Tensors last
  * written on another stream than the bound one must be ordered by the caller.
  * Limits: n_tokens <= 2^30, N * n_tokens < 2^31, 2^23 elements per activation
  * row, 2^27 entries of a vocabulary of logits, a row stride of 2^29 elements (2^24

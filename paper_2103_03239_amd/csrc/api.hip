@@ -11,6 +11,7 @@
 #include "local_ops.h"
 #include "moshpit_internal.h"
 #include "pass_rules.h"
+#include "workspace.h"
 
 using namespace moshpit;
 
@@ -43,8 +44,7 @@ struct moshpit_ctx {
     int64_t partials_cap = 0;
     double *d_dist = nullptr;          // dist_cap doubles
     int64_t dist_cap = 0;
-    void *d_work = nullptr;            // workspace of the local step's operators: work_cap bytes
-    int64_t work_cap = 0;
+    Workspace work;                    // of the local step's operators
     std::vector<hipEvent_t> events;    // 2 per timed round
 
     // Host bytes on their way to the device (masks, peer lists): copied out of the caller's
@@ -524,7 +524,7 @@ int moshpit_destroy(moshpit_ctx *h)
     if (h->d_grid) (void)hipFree(h->d_grid);
     if (h->d_grid_partials) (void)hipFree(h->d_grid_partials);
     if (h->d_dist) (void)hipFree(h->d_dist);
-    if (h->d_work) (void)hipFree(h->d_work);
+    h->work.release([](void *p) { (void)hipFree(p); });
     delete h;
     return MOSHPIT_OK;
 }
@@ -1296,16 +1296,17 @@ constexpr int64_t kMostTokens = int64_t(1) << 30, kMostRows = int64_t(1) << 31, 
 
 int reserve_work(moshpit_ctx *h, int64_t bytes)
 {
-    if (bytes <= h->work_cap) return MOSHPIT_OK;
-    if (h->d_work) {
-        HIP_TRY(h, hipStreamSynchronize(h->stream));
-        HIP_TRY(h, hipFree(h->d_work));
-        h->d_work = nullptr;
-        h->work_cap = 0;
-    }
-    HIP_TRY(h, hipMalloc(&h->d_work, static_cast<size_t>(bytes)));
-    h->work_cap = bytes;
-    return MOSHPIT_OK;
+    hipError_t e = hipSuccess;
+    const bool there = h->work.reserve(bytes, [&](int64_t n) -> void * {
+        void *p = nullptr;
+        e = hipMalloc(&p, static_cast<size_t>(n));
+        if (e == hipSuccess) return p;
+        (void)hipGetLastError();
+        return nullptr;
+    });
+    if (there) return MOSHPIT_OK;
+    if (e == hipSuccess) return fail(h, MOSHPIT_EHIP, "the workspace has grown too often");
+    return fail(h, e == hipErrorOutOfMemory ? MOSHPIT_ENOMEM : MOSHPIT_EHIP, "%lld bytes of workspace: %s", (long long)bytes, hipGetErrorString(e));
 }
 
 int check_dtype(moshpit_ctx *h, const char *what, int32_t dtype)
@@ -1391,7 +1392,7 @@ int moshpit_embed_grad(moshpit_ctx *h, const void *dy_dev, int32_t dy_dtype, int
     if (!embed_grad_fits(g)) return fail(h, MOSHPIT_EINVAL, "%lld tables of %lld rows are too many for one call", (long long)h->N, (long long)vocab);
     CHECK(reserve_work(h, embed_grad_work_bytes(g)));
     HIP_TRY(h, launch_embed_grad(static_cast<char *>(grad_dev) + column * elem_bytes(h->dtype), h->dtype, g, tokens_dev, scale, dy_dev,
-                                 dy_dtype, dy_row_stride, accumulate != 0, h->d_work, h->stream));
+                                 dy_dtype, dy_row_stride, accumulate != 0, h->work.block(), h->stream));
     return MOSHPIT_OK;
 }
 
@@ -1443,7 +1444,7 @@ int moshpit_weight_grad(moshpit_ctx *h, const void *dy_dev, int32_t dy_dtype, in
     if (!weight_grad_fits(g)) return fail(h, MOSHPIT_EINVAL, "%lld matrices of %lld x %lld are too many for one call", (long long)h->N, (long long)outs, (long long)ins);
     CHECK(reserve_work(h, weight_grad_work_bytes(g, dy_dtype, compute_units)));
     HIP_TRY(h, launch_weight_grad(dy_dev, dy_dtype, codes_dev, scales_dev, g, static_cast<char *>(grad_dev) + column * elem_bytes(h->dtype),
-                                  h->dtype, accumulate != 0, h->d_work, compute_units, h->stream));
+                                  h->dtype, accumulate != 0, h->work.block(), compute_units, h->stream));
     return MOSHPIT_OK;
 }
 
@@ -1467,7 +1468,7 @@ int moshpit_token_logp(moshpit_ctx *h, const void *logits_dev, int32_t dtype, in
     int compute_units = 0;
     HIP_TRY(h, current_compute_units(&compute_units));
     CHECK(reserve_work(h, policy_work_bytes(h->N, n_tokens, vocab, dtype, compute_units)));
-    HIP_TRY(h, launch_token_logp(logits_dev, dtype, h->N * n_tokens, vocab, logits_row_stride, tokens_dev, logp_dev, h->d_work, compute_units,
+    HIP_TRY(h, launch_token_logp(logits_dev, dtype, h->N * n_tokens, vocab, logits_row_stride, tokens_dev, logp_dev, h->work.block(), compute_units,
                                  h->stream));
     return MOSHPIT_OK;
 }
@@ -1496,7 +1497,7 @@ int moshpit_policy_loss(moshpit_ctx *h, const void *logits_dev, int32_t dtype, i
     CHECK(reserve_work(h, policy_work_bytes(h->N, n_tokens, vocab, dtype, compute_units)));
     const PolicyTerms p{old_logp_dev, ref_logp_dev, advantage_dev, weight_dev, clip_low, clip_high, kl_coef};
     HIP_TRY(h, launch_policy_loss(logits_dev, dtype, h->N, n_tokens, vocab, logits_row_stride, tokens_dev, p, grad_dev, grad_row_stride, logp_dev,
-                                  stats_dev, h->d_work, compute_units, h->stream));
+                                  stats_dev, h->work.block(), compute_units, h->stream));
     return MOSHPIT_OK;
 }
 

@@ -1,0 +1,57 @@
+"""The local step's operators as programs use them: captured graphs replayed after other calls."""
+import pytest
+import torch
+
+from paper_2103_03239_amd import binding
+from test_gpu_local_ops import DEV, normal, rng, some_tokens
+
+pytestmark = pytest.mark.gpu
+
+
+def test_a_graph_replays_after_calls_that_need_more_workspace():
+    """Every operator that has a workspace is captured at a small size, then called eagerly at growing ones, whose workspace does not fit the
+    captured block; memory of that block's size is taken and filled; the replays still give what eager calls give."""
+    g = rng(21)
+    N, V, D, I = 4, 500, 64, 96
+    X, G = normal((N, 4_000_000), torch.float32, g), torch.zeros((N, 4_000_000), device=DEV)
+
+    def inputs(T, vocab):
+        tokens = some_tokens("any", N, T, V, g)
+        return dict(tokens=tokens, x=normal((N, T, I), torch.float32, g), y=normal((N, T, D), torch.float32, g), z=normal((N, T, vocab), torch.float32, g),
+                    v=torch.rand((N, T), generator=g, device=DEV), grad=torch.empty((N, T, vocab), device=DEV))
+
+    def step(m, c):
+        logp = m.token_logp(c["z"], c["tokens"])
+        stats, lp = m.policy_loss(c["z"], c["tokens"], c["v"], c["v"], c["v"], grad=c["grad"])
+        codes, scales = m.checkpoint(c["x"])
+        m.weight_grad(c["y"], codes, scales, G, V * D)
+        m.embed_grad(c["y"], c["tokens"], G, 0, V)
+        return logp, stats, lp
+
+    side = torch.cuda.Stream()
+    small, larger = inputs(300, 70_000), [inputs(T, 600) for T in (2_000, 9_000, 30_000)]
+    torch.cuda.synchronize()
+    with binding.Moshpit(N, X.shape[1], 2, 2, binding.F32) as m, torch.cuda.stream(side):
+        m.bind_state(X, side)
+        step(m, small)
+        side.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            held = step(m, small)
+        for k, c in enumerate(larger):
+            step(m, c)
+            side.synchronize()
+            filled = [torch.full((1 << e,), 0x7fc00000, dtype=torch.int32, device=DEV) for e in range(10, 26)]
+            small["z"].normal_(generator=g)
+            small["y"].normal_(generator=g)
+            G.fill_(9.0)
+            graph.replay()
+            side.synchronize()
+            replayed = [t.clone() for t in (G, small["grad"], *held)]
+            G.fill_(9.0)
+            eager = step(m, small)
+            side.synchronize()
+            for a, b in zip(replayed, (G, small["grad"], *eager)):
+                assert torch.equal(a, b), k
+            assert all(bool((t == 0x7fc00000).all()) for t in filled)
+            del filled
