@@ -52,22 +52,21 @@ class Schedule:
 
 _lib = None
 _torch_module = None
+_raw_stream = None
 
 
 def _torch():
     """torch, imported at the first call that needs it (an import statement per call costs as much as a kernel's launch)."""
-    global _torch_module
+    global _torch_module, _raw_stream
     if _torch_module is None:
         import torch
-        _torch_module = torch
+        _torch_module, _raw_stream = torch, getattr(torch._C, "_cuda_getCurrentRawStream", None)
     return _torch_module
 
 
-def _current_stream(device) -> int:
-    """Handle of the device's current stream (torch's Stream object for it takes 2 us to make, as long as a launch)."""
-    torch = _torch()
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    return torch.cuda.current_stream(device).cuda_stream if raw is None or device.index is None else raw(device.index)
+def _current_stream(index: int) -> int:
+    """Handle of device `index`'s current stream (torch's Stream object for it takes 2 us to make, as long as a launch)."""
+    return _raw_stream(index) if _raw_stream else _torch().cuda.current_stream(index).cuda_stream
 
 
 def load_library() -> ctypes.CDLL:
@@ -138,6 +137,8 @@ def _c_schedule(s: Schedule | None, rounds: int, N: int):
 class Moshpit:
     """One handle = one peer-state matrix of N = M^d rows with P parameters."""
 
+    _bound = None                              # device index and handle of the stream that bind_state was given
+
     def __init__(self, N: int, P: int, M: int, d: int, dtype: int):
         self._lib = load_library()
         self._h = ctypes.c_void_p()
@@ -158,7 +159,7 @@ class Moshpit:
         if self._h:
             self._lib.moshpit_destroy(self._h)
             self._h = ctypes.c_void_p()
-            self._state = None
+            self._state = self._bound = None
 
     def __enter__(self):
         return self
@@ -175,7 +176,7 @@ class Moshpit:
     # -- the C ABI, one method per entry point ------------------------------
     def bind_state(self, X, stream=None) -> None:
         """X: torch tensor [N, P] on the GPU (float32 or bfloat16), unit column stride."""
-        import torch
+        torch = _torch()
         want = torch.float32 if self.dtype == F32 else torch.bfloat16
         if X.dtype != want or X.dim() != 2 or tuple(X.shape) != (self.N, self.P) or not X.is_cuda:
             raise ValueError("state tensor has the wrong dtype, shape or device")
@@ -185,6 +186,7 @@ class Moshpit:
             stream = torch.cuda.current_stream(X.device)
         self._check(self._lib.moshpit_bind_state(self._h, X.data_ptr(), X.stride(0), stream.cuda_stream), "bind_state")
         self._state = (X, stream)              # keep both alive
+        self._bound = (X.device.index, stream.cuda_stream)
 
     def bind_raw(self, ptr: int, row_stride: int, stream_handle: int = 0) -> None:
         self._check(self._lib.moshpit_bind_state(self._h, ptr, row_stride, stream_handle), "bind_state")
@@ -278,17 +280,20 @@ class Moshpit:
     def local_step(self, G, gamma: float, alive=None) -> None:
         keep, ptr = self._alive_ptr(alive)
         gp, gs = self._grad(G)
+        self._lend(G)
         self._check(self._lib.moshpit_local_step(self._h, ptr, gp, gs, gamma), "local_step")
 
     def sgd_round(self, t: int, G, gamma: float, alive=None) -> None:
         keep, ptr = self._alive_ptr(alive)
         gp, gs = self._grad(G)
+        self._lend(G)
         self._check(self._lib.moshpit_sgd_round(self._h, t, ptr, gp, gs, gamma), "sgd_round")
 
     def sgd_run(self, t0: int, rounds: int, G, gamma: float, schedule: Schedule | None = None, want_dist: bool = False,
                 want_times: bool = False, flags: int = 0):
         cs, keep = _c_schedule(schedule, rounds, self.N)
         gp, gs = self._grad(G)
+        self._lend(G)
         dist = np.zeros(rounds + 1, dtype=np.float64) if want_dist else None
         ms = np.zeros(rounds, dtype=np.float32) if want_times else None
         rc = self._lib.moshpit_sgd_run(self._h, t0, rounds, ctypes.byref(cs) if cs is not None else None, flags, gp, gs,
@@ -337,6 +342,8 @@ class Moshpit:
                     "set_tuning")
 
     # -- the local step of language-model peers --------------------------------
+    # Calls are queued on the bound stream.  Where another one is current, the caller orders the two (what a call reads has to be written
+    # by then, what it writes is there after a wait); memory is looked after here, so temporaries may be given and results dropped.
     @staticmethod
     def _type_code(dtype) -> int:
         torch = _torch()
@@ -346,15 +353,27 @@ class Moshpit:
             return BF16
         raise ValueError("activations must be float32 or bfloat16")
 
+    def _lend(self, *tensors) -> None:
+        """Tensors that the bound stream is to use (None among them is passed over).  Where another stream is current, the allocator
+        is told so: their memory, once given back, is not given out again before the bound stream is through with it."""
+        bound = self._bound
+        if bound is not None and _current_stream(bound[0]) != bound[1]:
+            for x in tensors:
+                if x is not None:
+                    x.record_stream(self._state[1])
+
     def _new(self, device, *wanted):
         """New tensors, one per (shape, dtype), out of the bound stream's memory: a block that another stream has just given back may
-        still be in use there."""
-        torch = _torch()
-        stream = self._state[1] if self._state else None
-        if stream is None or _current_stream(device) == stream.cuda_stream:
+        still be in use there.  Where another stream is current it will use them, too, which the allocator is told."""
+        torch, bound = _torch(), self._bound
+        if bound is None or _current_stream(bound[0]) == bound[1]:
             return [torch.empty(shape, dtype=dtype, device=device) for shape, dtype in wanted]
+        stream = self._state[1]
         with torch.cuda.stream(stream):
-            return [torch.empty(shape, dtype=dtype, device=device) for shape, dtype in wanted]
+            new = [torch.empty(shape, dtype=dtype, device=device) for shape, dtype in wanted]
+        for x in new:
+            x.record_stream(torch.cuda.current_stream(device))
+        return new
 
     def _rows(self, x, name: str, T: int | None = None):
         """x: [N, T, width] on the GPU, unit column stride, row i * T + t at a constant stride.
@@ -396,6 +415,7 @@ class Moshpit:
         op, code, _, w, stride = self._rows(out, "out", T)
         if w != width:
             raise ValueError("out must be [N, T, width]")
+        self._lend(tokens, out)
         self._check(self._lib.moshpit_embed(self._h, column, vocab, width, tp, T, scale, op, code, stride), "embed")
         return out
 
@@ -404,6 +424,7 @@ class Moshpit:
         tp, T = self._tokens(tokens)
         yp, code, _, width, stride = self._rows(dY, "dY", T)
         gp, gs = self._grad(G)
+        self._lend(dY, tokens, G)
         self._check(self._lib.moshpit_embed_grad(self._h, yp, code, stride, tp, T, scale, int(accumulate), gp, gs, column, vocab, width),
                     "embed_grad")
 
@@ -411,6 +432,7 @@ class Moshpit:
         """x [N, T, width] in 8 bits: (codes int8 [N, T, width], scales uint8 [N, T, ceil(width / 32)])."""
         torch = _torch()
         xp, code, T, width, stride = self._rows(x, "x")
+        self._lend(x)
         codes, scales = self._new(x.device, ((self.N, T, width), torch.int8), ((self.N, T, -(-width // 32)), torch.uint8))
         self._check(self._lib.moshpit_checkpoint(self._h, xp, code, self.N * T, width, stride, codes.data_ptr(), scales.data_ptr()),
                     "checkpoint")
@@ -433,6 +455,7 @@ class Moshpit:
         op, code, T, width, stride = self._rows(out, "out", codes.shape[1])
         if width != codes.shape[2]:
             raise ValueError("out must have the shape of codes")
+        self._lend(codes, scales, out)
         self._check(self._lib.moshpit_checkpoint_restore(self._h, cp, sp, self.N * T, width, op, code, stride), "checkpoint_restore")
         return out
 
@@ -442,6 +465,7 @@ class Moshpit:
         cp, sp = self._saved(codes, scales)
         yp, code, T, outs, stride = self._rows(dY, "dY", codes.shape[1])
         gp, gs = self._grad(G)
+        self._lend(dY, codes, scales, G)
         self._check(self._lib.moshpit_weight_grad(self._h, yp, code, stride, cp, sp, T, outs, codes.shape[2], int(accumulate), gp, gs, column),
                     "weight_grad")
 
@@ -450,6 +474,7 @@ class Moshpit:
         torch = _torch()
         tp, T = self._tokens(tokens)
         zp, code, _, vocab, stride = self._rows(logits, "logits", T)
+        self._lend(logits, tokens)
         logp, = self._new(logits.device, ((self.N, T), torch.float32))
         self._check(self._lib.moshpit_token_logp(self._h, zp, code, stride, tp, T, vocab, logp.data_ptr()), "token_logp")
         return logp
@@ -467,6 +492,7 @@ class Moshpit:
         shape = tokens.shape
         old, adv, w = self._per_token(shape, (old_logp, "old_logp"), (advantage, "advantage"), (weight, "weight"))
         ref = None if ref_logp is None else self._per_token(shape, (ref_logp, "ref_logp"))[0]
+        self._lend(logits, tokens, old_logp, advantage, weight, ref_logp, grad)
         logp, stats = self._new(logits.device, ((self.N, T), torch.float32), ((self.N, 3), torch.float32))
         self._check(self._lib.moshpit_policy_loss(self._h, zp, code, stride, tp, T, vocab, old, ref, adv, w, clip_low, clip_high, kl_coef, dp,
                                                   dstride, logp.data_ptr(), stats.data_ptr()), "policy_loss")

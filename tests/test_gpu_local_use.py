@@ -55,3 +55,55 @@ def test_a_graph_replays_after_calls_that_need_more_workspace():
                 assert torch.equal(a, b), k
             assert all(bool((t == 0x7fc00000).all()) for t in filled)
             del filled
+
+
+def test_memory_waits_for_the_stream_that_still_uses_it():
+    """With another stream current than the bound one: a temporary input's memory is not given out again while the bound stream has yet to
+    read it, nor a result's while the current stream has yet to."""
+    g = rng(22)
+    N, T, W = 4, 250, 1_000
+    X, x = torch.zeros((N, 16), device=DEV), normal((N, T, W), torch.float32, g)
+    big = normal((8_192, 8_192), torch.float32, g)
+    side, here = torch.cuda.Stream(), torch.cuda.current_stream()
+
+    def busy(stream):
+        """Work of some hundred milliseconds, and an event behind it."""
+        with torch.cuda.stream(stream):
+            for _ in range(30):
+                torch.mm(big, big)
+            return stream.record_event()
+
+    torch.mm(big, big)
+    torch.cuda.synchronize()
+    with binding.Moshpit(N, 16, 2, 2, binding.F32) as m:
+        m.bind_state(X, side)
+        codes, scales = m.checkpoint(x * 2.0)
+        torch.cuda.synchronize()
+        want, want_scales = codes.clone(), scales.clone()
+        value = m.checkpoint_restore(codes, scales)
+        torch.cuda.synchronize()
+        value = value.clone()
+
+        temporary = x * 2.0
+        side.wait_stream(here)
+        end = busy(side)
+        at = temporary.data_ptr()
+        got = m.checkpoint(temporary)
+        del temporary
+        other = [torch.empty_like(x) for _ in range(3)]
+        assert not end.query(), "the queue was too short to tell"
+        assert at not in [t.data_ptr() for t in other]
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want) and torch.equal(got[1], want_scales)
+
+        result = m.checkpoint_restore(codes, scales)
+        here.wait_stream(side)
+        end = busy(here)
+        total = result.double().sum()
+        at = result.data_ptr()
+        del result
+        other = [m.checkpoint_restore(codes, scales) for _ in range(3)]
+        assert not end.query(), "the queue was too short to tell"
+        assert at not in [t.data_ptr() for t in other]
+        torch.cuda.synchronize()
+        assert float(total) == float(value.double().sum())

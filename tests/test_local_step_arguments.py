@@ -1,5 +1,6 @@
 """What the binding hands to the library for the local step's operators, and what it refuses: on the CPU, with tensors that
 say they are on the GPU and a library that writes down its calls."""
+import contextlib
 import ctypes
 
 import pytest
@@ -89,3 +90,61 @@ def test_row_strides_reach_the_library(peers, name, T):
         at = max(i for i, a in enumerate(args) if a == x.data_ptr()) if T else None
         if T:
             assert stride in args[at: at + 6], args
+
+
+class Stream:
+    def __init__(self, handle):
+        self.cuda_stream = handle
+
+
+class Lent(OnGpu):
+    """Writes down the streams that the allocator is told of."""
+
+    def record_stream(self, stream):
+        self.__dict__.setdefault("lent", []).append(stream)
+
+
+@pytest.mark.parametrize("away", [False, True])
+def test_the_allocator_hears_of_the_stream_that_uses_a_tensor(peers, away, monkeypatch):
+    """Every tensor of a call is lent to the bound stream where another one is current, and the new ones, which are the bound stream's, to the
+    current one.  (A temporary's memory could be given out again while the bound stream still reads it, else.)"""
+    bound, current, empty = Stream(7), Stream(5 if away else 7), torch.empty
+    monkeypatch.setattr(binding, "_current_stream", lambda index: current.cuda_stream)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: current)
+    monkeypatch.setattr(torch.cuda, "stream", lambda stream: contextlib.nullcontext())
+    monkeypatch.setattr(torch, "empty", lambda *a, **k: empty(*a, **k).as_subclass(Lent))
+    m, T = peers, 3
+    m._state, m._bound = (m._state[0], bound), (0, bound.cuda_stream)
+
+    def new(shape, dtype=torch.float32):
+        return torch.zeros(shape, dtype=dtype).as_subclass(Lent)
+
+    def tokens():
+        return new((N, T), torch.int32)
+
+    def v():
+        return new((N, T))
+
+    def saved():
+        return new((N, T, W), torch.int8), new((N, T, W // 32), torch.uint8)
+    # of each call: the tensors given to it, and the ones it makes
+    for call, given in (
+            (lambda t, out: (m.embed(t, 0, V, W, out=out), ())[1], [tokens(), new((N, T, W))]),
+            (lambda t: m.embed(t, 0, V, W), [tokens()]),
+            (lambda y, t, G: m.embed_grad(y, t, G, 0, V), [new((N, T, W)), tokens(), new((N, m.P))]),
+            (lambda x: m.checkpoint(x), [new((N, T, W))]),
+            (lambda c, s: m.checkpoint_restore(c, s), [*saved()]),
+            (lambda c, s, out: (m.checkpoint_restore(c, s, out=out), ())[1], [*saved(), new((N, T, W))]),
+            (lambda y, c, s, G: m.weight_grad(y, c, s, G, 0), [new((N, T, V)), *saved(), new((N, m.P))]),
+            (lambda z, t: m.token_logp(z, t), [new((N, T, W)), tokens()]),
+            (lambda z, t, o, a, w: m.policy_loss(z, t, o, a, w), [new((N, T, W)), tokens(), v(), v(), v()]),
+            (lambda z, t, o, a, w, r, g: m.policy_loss(z, t, o, a, w, ref_logp=r, grad=g), [new((N, T, W)), tokens(), v(), v(), v(), v(), new((N, T, W))]),
+            (lambda G: m.local_step(G, 0.1), [new((N, m.P))]),
+            (lambda G: m.sgd_round(0, G, 0.1), [new((N, m.P))]),
+            (lambda G: m.sgd_run(0, 1, G, 0.1), [new((N, m.P))])):
+        made = call(*given)
+        made = [x for x in (made if isinstance(made, tuple) else [made]) if isinstance(x, Lent)]
+        for x in given:
+            assert (bound in x.__dict__.get("lent", [])) == away
+        for x in made:
+            assert (current in x.__dict__.get("lent", [])) == away
