@@ -137,7 +137,7 @@ def _c_schedule(s: Schedule | None, rounds: int, N: int):
 class Moshpit:
     """One handle = one peer-state matrix of N = M^d rows with P parameters."""
 
-    _bound = None                              # device index and handle of the stream that bind_state was given
+    _bound = None                              # device index (None: the tensors') and handle of the bound stream
 
     def __init__(self, N: int, P: int, M: int, d: int, dtype: int):
         self._lib = load_library()
@@ -190,6 +190,17 @@ class Moshpit:
 
     def bind_raw(self, ptr: int, row_stride: int, stream_handle: int = 0) -> None:
         self._check(self._lib.moshpit_bind_state(self._h, ptr, row_stride, stream_handle), "bind_state")
+        self._state = (None, None)             # (the caller keeps the state alive; _stream() makes the stream's object)
+        self._bound = (None, stream_handle)
+
+    def _stream(self):
+        """The bound stream as an object of torch's."""
+        X, stream = self._state
+        if stream is None:
+            cuda, handle = _torch().cuda, self._bound[1]
+            stream = cuda.ExternalStream(handle) if handle else cuda.default_stream()
+            self._state = (X, stream)
+        return stream
 
     def round(self, t: int, alive=None) -> None:
         if alive is None:
@@ -272,8 +283,9 @@ class Moshpit:
         return keys
 
     def _grad(self, G):
-        X = self._state[0]
-        if G.dtype != X.dtype or tuple(G.shape) != (self.N, self.P) or G.stride(1) != 1 or not G.is_cuda:
+        torch = _torch()
+        want = torch.float32 if self.dtype == F32 else torch.bfloat16
+        if G.dtype != want or tuple(G.shape) != (self.N, self.P) or G.stride(1) != 1 or not G.is_cuda:
             raise ValueError("gradient tensor must match the state's dtype, shape and device")
         return G.data_ptr(), G.stride(0)
 
@@ -357,19 +369,19 @@ class Moshpit:
         """Tensors that the bound stream is to use (None among them is passed over).  Where another stream is current, the allocator
         is told so: their memory, once given back, is not given out again before the bound stream is through with it."""
         bound = self._bound
-        if bound is not None and _current_stream(bound[0]) != bound[1]:
+        if bound is not None and _current_stream(bound[0] if bound[0] is not None else tensors[0].device.index) != bound[1]:
+            stream = self._stream()
             for x in tensors:
                 if x is not None:
-                    x.record_stream(self._state[1])
+                    x.record_stream(stream)
 
     def _new(self, device, *wanted):
         """New tensors, one per (shape, dtype), out of the bound stream's memory: a block that another stream has just given back may
         still be in use there.  Where another stream is current it will use them, too, which the allocator is told."""
         torch, bound = _torch(), self._bound
-        if bound is None or _current_stream(bound[0]) == bound[1]:
+        if bound is None or _current_stream(bound[0] if bound[0] is not None else device.index) == bound[1]:
             return [torch.empty(shape, dtype=dtype, device=device) for shape, dtype in wanted]
-        stream = self._state[1]
-        with torch.cuda.stream(stream):
+        with torch.cuda.stream(self._stream()):
             new = [torch.empty(shape, dtype=dtype, device=device) for shape, dtype in wanted]
         for x in new:
             x.record_stream(torch.cuda.current_stream(device))

@@ -107,3 +107,30 @@ def test_memory_waits_for_the_stream_that_still_uses_it():
         assert at not in [t.data_ptr() for t in other]
         torch.cuda.synchronize()
         assert float(total) == float(value.double().sum())
+
+
+def test_a_state_bound_by_address():
+    """bind_raw with a stream's handle, after bind_state with another stream: results as with the tensor."""
+    g = rng(23)
+    N, T, V, D = 4, 90, 70, 32
+    X, G = normal((N, V * D), torch.float32, g), torch.zeros((N, V * D), device=DEV)
+    tokens, y = some_tokens("any", N, T, V, g), normal((N, T, D), torch.float32, g)
+    side, third = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with binding.Moshpit(N, V * D, 2, 2, binding.F32) as m:
+        m.bind_state(X, third)
+        want = m.embed(tokens, 0, V, D)
+        m.embed_grad(y, tokens, G, 0, V)
+        m.sync()
+        want, want_grad = want.clone(), G.clone()
+        torch.cuda.synchronize()
+        for stream in (side, torch.cuda.default_stream()):
+            m.bind_raw(X.data_ptr(), V * D, stream.cuda_stream)
+            G.zero_()
+            torch.cuda.synchronize()
+            out = m.embed(tokens, 0, V, D)
+            codes, scales = m.checkpoint(out)
+            m.embed_grad(y, tokens, G, 0, V)
+            m.sync()
+            assert torch.equal(out, want) and torch.equal(G, want_grad)
+            del out, codes, scales

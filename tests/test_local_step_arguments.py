@@ -148,3 +148,31 @@ def test_the_allocator_hears_of_the_stream_that_uses_a_tensor(peers, away, monke
             assert (bound in x.__dict__.get("lent", [])) == away
         for x in made:
             assert (current in x.__dict__.get("lent", [])) == away
+
+
+@pytest.mark.parametrize("bound_before", [False, True])
+@pytest.mark.parametrize("handle", [0, 9])
+def test_a_raw_binding_takes_the_place_of_the_one_before(peers, bound_before, handle, monkeypatch):
+    """After bind_raw the operators' tensors are lent to its stream, not to an earlier binding's, and gradients are taken."""
+    streams = []
+    monkeypatch.setattr(binding, "_current_stream", lambda index: 5)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: Stream(5))
+    monkeypatch.setattr(torch.cuda, "stream", lambda stream: streams.append(stream) or contextlib.nullcontext())
+    monkeypatch.setattr(torch.cuda, "ExternalStream", Stream)
+    monkeypatch.setattr(torch.cuda, "default_stream", lambda device=None: Stream(0))
+    empty = torch.empty
+    monkeypatch.setattr(torch, "empty", lambda *a, **k: empty(*a, **k).as_subclass(Lent))
+    m = peers
+    m._state, m._bound = ((m._state[0], Stream(7)), (0, 7)) if bound_before else (None, None)
+    m.bind_raw(4096, m.P, handle)
+    x, tokens = torch.zeros((N, 3, W)).as_subclass(Lent), torch.zeros((N, 3), dtype=torch.int32).as_subclass(Lent)
+    G = torch.zeros((N, m.P)).as_subclass(Lent)
+    made = m.checkpoint(x)
+    m.embed_grad(x, tokens, G, 0, V)
+    for t in (x, tokens, G):
+        assert {s.cuda_stream for s in t.__dict__.get("lent", [])} == {handle}
+    assert [s.cuda_stream for s in streams] == [handle]
+    for t in made:
+        assert [s.cuda_stream for s in t.__dict__["lent"]] == [5]
+    with pytest.raises(ValueError, match="gradient tensor"):
+        m.embed_grad(x, tokens, G.bfloat16(), 0, V)
