@@ -270,21 +270,18 @@ template <int YT, typename T, bool DIRECT> struct Staged {
             for (int q = 0; q < PARTS; ++q) *reinterpret_cast<u32x4 *>(lds_y + q * K * TO + at) = Vec<1, 8>::narrow(part[q]);
         }
     }
-    // Codes of times n as bfloat16 values: with u = code + 128 as an unsigned byte, value = u * 2^e - 128 * 2^e, exactly.  (The two
-    // writes meet in the banks; choosing by lane which half goes first avoids that and costs more: 568 us instead of 550 for 16 x
-    // 1024 x 4096 from 4096 tokens.)
+    // Codes of times n as bfloat16 values, code * 2^e.  (Signed bytes convert in one instruction each; unsigned ones, with 128 * 2^e taken
+    // off in a fused multiply-add, would take as many and have no 128 * 2^e for the largest groups.)  The two writes meet in the banks;
+    // choosing by lane which half goes first avoids that and costs more: 568 us instead of 550 for 16 x 1024 x 4096 from 4096 tokens.
     __device__ __forceinline__ void store_x(int n, uint16_t *lds_x) const
     {
-        const float factor = to_value_factor(byte[n]), less = -128.f * factor;
+        const float factor = to_value_factor(byte[n]);
         u32x4 half[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             float f[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const uint32_t w = x[n][2 * h + k / 4] ^ 0x80808080u;
-                f[k] = fmaf(static_cast<float>((w >> (8 * (k & 3))) & 0xffu), factor, less);
-            }
+            for (int k = 0; k < 8; ++k) f[k] = factor * code_of(x[n][2 * h + k / 4], k & 3);
             half[h] = Vec<1, 8>::narrow(f);
         }
         const int row = x_row() + XR * n, col = x_col();

@@ -107,3 +107,32 @@ def test_an_offset_common_to_a_row_is_no_error(act, T, V, offset):
     c = loss_inputs(z, tokens, g)
     print("offset", act, T, V, offset, flush=True)
     check_loss(c, act, 0.1, 2, 1)
+
+
+# ---- weight gradients -------------------------------------------------------------
+
+@pytest.mark.parametrize("state,act", [("f32", "f32"), ("f32", "bf16"), ("bf16", "bf16")])
+@pytest.mark.parametrize("M,d,T,O,I", [(2, 1, 50, 3, 40), (2, 1, 100, 24, 70), (2, 1, 700, 128, 128), (8, 2, 65, 392, 400), (4, 2, 40, 1_001, 1_003)])
+def test_weight_grad_of_every_power_of_two(state, act, M, d, T, O, I):
+    """Codes count as code * 2^e for every scale byte whose values are finite, up to the largest: groups of 2^122 and of codes -1 .. 1 of 2^127
+    beside small ones."""
+    N, g = M ** d, rng(T + O + I)
+    X, G = torch.zeros((N, O * I), dtype=TYPES[state][0], device=DEV), torch.zeros((N, O * I), dtype=TYPES[state][0], device=DEV)
+    dY = rows(N, T, O, TYPES[act][0], g, scale=2.0 ** -60).contiguous()
+    groups = -(-I // 32)
+    codes = torch.randint(-127, 128, (N, T, I), generator=g, device=DEV)
+    byte = torch.tensor([1, 100, 127, 200, 246, 247, 248, 249, 254], device=DEV)[torch.randint(0, 9, (N, T, groups), generator=g, device=DEV)]
+    wide = byte.repeat_interleave(32, -1)[..., :I]
+    codes = torch.where(wide == 249, codes.clamp(-63, 63), torch.where(wide == 254, codes.clamp(-1, 1), codes))
+    value = codes.double() * torch.exp2(wide.double() - 127.0)
+    assert float(value.abs().max()) <= torch.finfo(torch.float32).max
+    with handle(X, M, d) as m:
+        print("powers", state, act, N, T, O, I, flush=True)
+        m.weight_grad(dY, codes.to(torch.int8), byte.to(torch.uint8), G, 0)
+        back = m.checkpoint_restore(codes.to(torch.int8), byte.to(torch.uint8))
+        m.sync()
+    assert torch.equal(back.double(), value)
+    y = dY.double().transpose(1, 2).contiguous()
+    want, size = torch.bmm(y, value), torch.bmm(y.abs(), value.abs())
+    terms = 3 * T if act == "f32" else T
+    close(G.view(N, O, I), want, (terms + 8) * 2 * U * size + TYPES[state][2] * want.abs() * 1.01 + TINY)
