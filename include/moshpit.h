@@ -345,8 +345,9 @@ int moshpit_embed_grad(moshpit_ctx *h, const void *dy_dev, int32_t dy_dtype, int
 /* Activations saved in 8 bits between the forward and the backward pass (the
  * activations of N peers share one GPU's memory with N states and N gradients).
  * 32 consecutive elements of a row (fewer at its end) share a power of two 2^e, e
- * the smallest whole number >= -126 with which all codes x / 2^e, rounded to
- * nearest, ties to even, lie within -127 .. 127; the scale byte is e + 127.  A code
+ * the smallest whole number within -126 .. 121 with which all codes x / 2^e, rounded
+ * to nearest, ties to even, lie within -127 .. 127 (elements from 127.5 * 2^121 on,
+ * 3.39e38, get +-127, so a finite one stays finite); the scale byte is e + 127.  A code
  * stands for code * 2^e, which is exact in bfloat16.  A group that holds an
  * infinity or a NaN gets the scale byte 255 and restores as NaN throughout.
  * codes_dev: rows * width bytes, scales_dev: rows * ceil(width / 32) bytes, both

@@ -163,6 +163,7 @@ __global__ __launch_bounds__(kBlock) void checkpoint_kernel(const char *__restri
         e[n].widen(f);
         uint32_t w[kVec / 4] = {};
         if (byte != kScaleNaN) {
+            if (byte == kScaleTop) keep_finite(f);
             const float factor = to_code_factor(byte);
 #pragma unroll
             for (int k = 0; k < kVec / 4; ++k) w[k] = pack_codes(f + 4 * k, factor);

@@ -5,7 +5,7 @@ import math
 import pytest
 import torch
 
-from test_gpu_local_ops import DEV, TINY, TYPES, U, close, handle, rng, rows
+from test_gpu_local_ops import DEV, TINY, TYPES, U, close, handle, normal, rng, rows
 
 pytestmark = pytest.mark.gpu
 
@@ -136,3 +136,38 @@ def test_weight_grad_of_every_power_of_two(state, act, M, d, T, O, I):
     want, size = torch.bmm(y, value), torch.bmm(y.abs(), value.abs())
     terms = 3 * T if act == "f32" else T
     close(G.view(N, O, I), want, (terms + 8) * 2 * U * size + TYPES[state][2] * want.abs() * 1.01 + TINY)
+
+
+# ---- checkpoints ------------------------------------------------------------------
+
+@pytest.mark.parametrize("act", ["f32", "bf16"])
+@pytest.mark.parametrize("T,W", [(40, 32), (7, 100), (3, 1_003)])
+def test_checkpoint_of_the_largest_values(act, T, W):
+    """Finite elements restore as finite ones, in both types: by the definition with e at most 121 and codes of at most 127, so that elements from
+    127.5 * 2^121 on are off by up to a step and all others by half of one."""
+    g, dtype = rng(T + W), TYPES[act][0]
+    top = torch.finfo(dtype).max
+    x = normal((4, T, W), dtype, g, 2.0 ** 126).clamp_(-top, top)
+    x[0], x[1] = -top, normal((T, W), dtype, g, 2.0 ** 100)
+    x[1, :, ::32] = top
+    edge = [127.5 * 2.0 ** 121, 127.5 * 2.0 ** 121 * (1 - 2.0 ** -24 * 2), 127.25 * 2.0 ** 121, 127.0 * 2.0 ** 121, 126.5 * 2.0 ** 121, 126.0 * 2.0 ** 121, top, 127.5 * 2.0 ** 120]
+    for t in range(T):                                               # a row for each, the group's largest element, beside small ones
+        x[2, t] = normal((W,), dtype, g, 2.0 ** 110)
+        x[2, t, ::32] = min(edge[t % len(edge)], top) * (-1) ** t
+    with handle(torch.zeros((4, 8), device=DEV), 2, 2) as m:
+        print("largest", act, T, W, flush=True)
+        codes, scales = m.checkpoint(x)
+        back, narrow = m.checkpoint_restore(codes, scales), m.checkpoint_restore(codes, scales, dtype=torch.bfloat16)
+        m.sync()
+    v = torch.nn.functional.pad(x.double(), (0, -W % 32)).unflatten(-1, (-1, 32))
+    e = torch.full(v.shape[:-1], -126.0, dtype=torch.float64, device=DEV)
+    for k in range(-125, 122):
+        e = torch.where((v.abs().amax(-1) * 2.0 ** (1 - k)).round() > 127.0, float(k), e)
+    step = torch.exp2(e)[..., None]
+    q = (v / step).round().clamp(-127, 127)
+    assert torch.equal(scales.double(), e + 127.0)
+    assert torch.equal(codes.double(), q.flatten(-2)[..., :W])
+    want = (q * step).flatten(-2)[..., :W]
+    assert torch.equal(back.double(), want) and torch.equal(narrow.double(), want) and bool(torch.isfinite(narrow).all())
+    off, step = (want - x.double()).abs(), step.expand_as(v).flatten(-2)[..., :W]
+    assert bool((off <= torch.where(x.double().abs() >= 127.5 * 2.0 ** 121, step, 0.5 * step)).all())
