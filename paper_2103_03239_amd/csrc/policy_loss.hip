@@ -168,6 +168,17 @@ struct RowTerms {
     float loss, kl, clipped;
 };
 
+// exp(x) - 1 - x, given exp(x) - 1.  Near 0 the difference has few of its terms' digits (none at 1e-4, and a policy starts as its own
+// reference) and may come out negative: within 1/2 the series x^2 / 2 (1 + x / 3 (1 + x / 4 (...))), which ends below 2^-28 of it.
+__device__ __forceinline__ float above_tangent(float x, float exp_less_1)
+{
+    if (!(fabsf(x) < 0.5f)) return exp_less_1 - x;
+    float s = 1.f;
+#pragma unroll
+    for (int n = 10; n >= 3; --n) s = fmaf(x * (1.f / static_cast<float>(n)), s, 1.f);
+    return 0.5f * x * x * s;
+}
+
 // From a row's log-probability: its terms and d loss / d lp.
 __device__ __forceinline__ float row_terms(const PolicyTerms &p, int64_t row, float w, float lp, RowTerms &terms)
 {
@@ -177,9 +188,9 @@ __device__ __forceinline__ float row_terms(const PolicyTerms &p, int64_t row, fl
     const bool clipped = plain > cut;
     float k = 0.f, dk = 0.f;
     if (p.ref_logp) {
-        const float off = p.ref_logp[row] - lp, e = expf(off);
-        k = e - off - 1.f;
-        dk = 1.f - e;
+        const float off = p.ref_logp[row] - lp, e = expm1f(off);
+        k = above_tangent(off, e);
+        dk = -e;
     }
     terms.loss = w * (p.kl_coef * k - (clipped ? cut : plain));
     terms.kl = w * k;

@@ -171,3 +171,33 @@ def test_checkpoint_of_the_largest_values(act, T, W):
     assert torch.equal(back.double(), want) and torch.equal(narrow.double(), want) and bool(torch.isfinite(narrow).all())
     off, step = (want - x.double()).abs(), step.expand_as(v).flatten(-2)[..., :W]
     assert bool((off <= torch.where(x.double().abs() >= 127.5 * 2.0 ** 121, step, 0.5 * step)).all())
+
+
+@pytest.mark.parametrize("act", ["f32", "bf16"])
+@pytest.mark.parametrize("M,d,V", [(8, 4, 2), (16, 2, 2), (16, 2, 70_002)])
+def test_kl_term_near_the_reference(act, M, d, V):
+    """k = exp(x) - 1 - x and its slope for x = ref - lp down to 2^-16, relatively as exact as for large ones, and never negative.  Logits of 0 and -200
+    give the second token the log-probability -200 to the bit (exp(-200) is far below a binary32 rounding of 1), and x is exact."""
+    N, g, dtype = M ** d, rng(V + d), TYPES[act][0]
+    z = torch.full((N, 1, V), -math.inf, dtype=dtype, device=DEV)
+    z[..., 0], z[..., 1] = 0.0, -200.0
+    x = torch.exp2(torch.empty((N, 1), device=DEV).uniform_(-16.0, 2.5, generator=g)) * torch.randint(0, 2, (N, 1), generator=g, device=DEV).mul(2).sub(1)
+    x = (x * 2.0 ** 16).round().div(2.0 ** 16)
+    x[0], x[1], x[2], x[3], x[4] = 0.0, 0.5, -0.5, 2.0 ** -16, -2.0 ** -16
+    tokens, v, grad = torch.ones((N, 1), dtype=torch.int32, device=DEV), torch.full((N, 1), -200.0, device=DEV), torch.empty_like(z)
+    with handle(torch.zeros((N, 16), device=DEV), M, d) as m:
+        print("near", act, N, V, flush=True)
+        stats, logp = m.policy_loss(z, tokens, v, torch.zeros_like(v), torch.ones_like(v), ref_logp=v + x, kl_coef=1.0, grad=grad)
+        m.sync()
+    assert bool((logp == -200.0).all()) and torch.equal((v + x) - v, x)
+    y = x.double()[:, 0]
+    e1 = torch.expm1(y)
+    terms = [y ** n / math.factorial(n) for n in range(2, 20)]       # (taken for |y| < 1: the rest is below 2^-53 of the sum)
+    k = torch.where(y.abs() < 1.0, sum(terms), e1 - y)
+    # within 1/2 a series: squares, sums and products, 8 U of it at most; beyond, expm1 (2 U) less x, each up to 4.5 times the result: 12 U
+    close(stats[:, 1], k, 12 * U * k)
+    close(stats[:, 0], k, 13 * U * k)
+    assert bool((stats[:, 1] >= 0).all()) and float(stats[0, 1]) == 0.0
+    for j, want in ((0, e1), (1, -e1)):
+        close(grad[:, 0, j], want, (6 * U + TYPES[act][2]) * want.abs())
+    assert not grad[..., 2:].any()
