@@ -382,7 +382,8 @@ int moshpit_token_logp(moshpit_ctx *h, const void *logits_dev, int32_t dtype, in
  * probability and gradient 0; a row of nothing else gives NaN.  Finite logits count as
  * what they are, the type's lowest value too: beside larger ones it excludes a token, a
  * row of nothing else has all tokens alike.
- * ref_logp_dev may be NULL when kl_coef is 0.  grad_dev: laid out like the logits and
+ * ref_logp_dev may be NULL when kl_coef is 0; what it holds does not reach loss and
+ * gradient then, k is a statistic alone.  grad_dev: laid out like the logits and
  * of their type; it may be the logits themselves (same row stride) but must not
  * overlap them in any other way.  logp_dev: [N][n_tokens] floats.  stats_dev: [N][3]
  * floats: loss_i, sum of w k, sum of the weights whose ratio was clipped. */

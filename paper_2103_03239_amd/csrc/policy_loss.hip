@@ -192,10 +192,12 @@ __device__ __forceinline__ float row_terms(const PolicyTerms &p, int64_t row, fl
         k = above_tangent(off, e);
         dk = -e;
     }
-    terms.loss = w * (p.kl_coef * k - (clipped ? cut : plain));
+    // (with the coefficient 0 k is a statistic alone: 0 times an infinite one would be NaN)
+    const float kl = p.kl_coef != 0.f ? p.kl_coef * k : 0.f, dkl = p.kl_coef != 0.f ? p.kl_coef * dk : 0.f;
+    terms.loss = w * (kl - (clipped ? cut : plain));
     terms.kl = w * k;
     terms.clipped = clipped ? w : 0.f;
-    return w * (p.kl_coef * dk - (clipped ? 0.f : plain));
+    return w * (dkl - (clipped ? 0.f : plain));
 }
 
 // Where a row's log-probability and terms go: the terms wait for the others of the peer, or are the peer's sums already (T = 1).

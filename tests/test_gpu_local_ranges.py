@@ -201,3 +201,21 @@ def test_kl_term_near_the_reference(act, M, d, V):
     for j, want in ((0, e1), (1, -e1)):
         close(grad[:, 0, j], want, (6 * U + TYPES[act][2]) * want.abs())
     assert not grad[..., 2:].any()
+
+
+@pytest.mark.parametrize("act", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V", [(10, 300), (10, 100_000), (1, 300), (2_100, 300)])
+def test_kl_as_a_statistic_does_not_reach_the_gradient(act, T, V):
+    """With a coefficient of 0 loss and gradient are those without a reference, whatever the reference holds; the statistic tells."""
+    g, dtype = rng(T + V), TYPES[act][0]
+    c = loss_inputs(rows(4, T, V, dtype, g), torch.randint(0, V, (4, T), generator=g, device=DEV, dtype=torch.int32), g)
+    grad, plain = torch.empty_like(c["z"]), torch.empty_like(c["z"])
+    c["ref"][1, 0], c["ref"][2, 0], c["ref"][3, 0] = c["ref"][1, 0] + 100.0, math.nan, -math.inf
+    args = c["z"], c["tokens"], c["old"], c["adv"], c["w"]
+    with handle(torch.zeros((4, 16), device=DEV), 2, 2) as m:
+        stats, logp = m.policy_loss(*args, ref_logp=c["ref"], grad=grad)
+        without, logp_without = m.policy_loss(*args, grad=plain)
+        m.sync()
+    assert torch.equal(grad, plain) and torch.equal(logp, logp_without) and torch.equal(stats[:, 0], without[:, 0]) and torch.equal(stats[:, 2], without[:, 2])
+    assert bool(torch.isfinite(stats[:, 0]).all()) and bool(torch.isfinite(grad).all())
+    assert math.isfinite(float(stats[0, 1])) and float(stats[1, 1]) == math.inf and math.isnan(float(stats[2, 1])) and float(stats[3, 1]) == math.inf
