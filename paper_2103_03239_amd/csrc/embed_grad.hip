@@ -746,8 +746,11 @@ hipError_t launch_embed_grad(void *base, int state_dtype, const TableGeom &g, co
     p.bits = (key_bits + p.passes - 1) / p.passes;
     const int32_t es = state_dtype == 0 ? 4 : 2;
     Fill fill{static_cast<char *>(base), g.peer_stride * es, g.vocab * g.width * es, 0, 0};
-    // threads of the sort's blocks, and so of those that clear: many only where one block sorts many places
-    const int threads = g.T > kOneBlock ? kTileThreads : g.T > 1024 ? 1024 : g.T > 256 || fill.table_bytes > (1 << 20) ? 256 : 64;
+    // Threads of the sort's blocks, and so of those that clear.  From 257 to 1024 places 256 (16 tables of 30000 x 128 from 1000: 50.6 us,
+    // with 1024 threads 55.3).  Up to 256 places 64 sort as well and leave room for more blocks, but clear slower: 4096 tables of 200 x 16
+    // from 50 added to in 41.5 us (with 256 threads 45.3), cleared and written in 37.0 (37.1), 1024 of 200 x 64 from 64 in 25.4 (22.2),
+    // 256 of 600 x 64 from 200 in 22.6 (19.3), 16 of 30000 x 128 from 200 in 64 (48).
+    const int threads = g.T > kOneBlock ? kTileThreads : g.T > 1024 ? 1024 : g.T > 256 || (!accumulate && fill.table_bytes > (32 << 10)) ? 256 : 64;
     fill.blocks = accumulate ? 0 : static_cast<uint32_t>((fill.table_bytes + 16 * threads - 1) / (16 * threads));
     const uint32_t fill_blocks = fill.blocks * N;
     int sorted = 0;
