@@ -5,7 +5,8 @@
 // (a power of two, up to a wave) moves a row, or a wave 64 vectors of a longer one, 16 bytes of output a lane, and
 // takes kRows places, whose tokens and then whose rows are requested together: one dependent pair of
 // latencies for all of them.  Stores are streaming ones: 16 x 8192 rows of 1024 out of binary32 tables into bfloat16
-// in 71 us, with plain ones in 92; 4 x 15274 rows of 1200 binary32 in 57 us (87).
+// in 68 us, with plain ones in 87; 4 x 15274 rows of 1200 binary32 in 57 us (76).  These are calls on the same inputs one after the
+// other; with other tables every time, which no cache holds yet, the first takes 82.
 #include <hip/hip_runtime.h>
 
 #include "local_ops.h"

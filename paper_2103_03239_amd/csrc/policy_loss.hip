@@ -542,7 +542,8 @@ __global__ __launch_bounds__(64) void logp_join_kernel(const TopSum *__restrict_
 }
 
 // The terms of a peer's rows, summed in binary64 in an order that depends on T alone.  A thread requests four rows' terms before
-// it adds the first: one block is bound by the latency of its loads.
+// it adds the first: one block is bound by the latency of its loads.  Threads by what a loss with rows of 64 entries took with 64, 256
+// and 1024: 256 peers of 100 rows 19.8, 19.9 and 20.6 us, 256 of 1024 105.6, 102.8 and 103.2, 4 of 8192 44.3, 24.2 and 20.3.
 constexpr int kStatsThreads = 1024;
 
 __global__ __launch_bounds__(kStatsThreads) void policy_stats_kernel(const RowTerms *__restrict__ terms, int64_t T, float *__restrict__ stats)

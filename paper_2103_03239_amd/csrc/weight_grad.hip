@@ -10,8 +10,8 @@
 //
 // Bound by the matrix cores where the matrices are large, and by what feeds them: 16 matrices of 1024 x 4096 from 4096
 // tokens of bfloat16 dy in 501 to 535 us by card, 1030 to 1100 TFLOP/s of the 1301 that a plain bfloat16 product reaches.  dy
-// through registers on its way into LDS takes 6 % longer (613 against 578 us on one card, back to back); what remains is the
-// codes' way through registers: without any staging the products take 0.74 of it.
+// through registers on its way into LDS takes 6 % longer (613 against 578 us on one card, back to back).  The codes go through
+// registers, since they become bfloat16 on the way.
 #include <hip/hip_runtime.h>
 
 #include "checkpoint_codes.h"
