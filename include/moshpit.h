@@ -321,8 +321,10 @@ int moshpit_grouped_round(moshpit_ctx *h, const int32_t *index_host, int64_t n_i
  * tokens alone, so a call repeats to the bit.  Workspace belongs to the handle and
  * grows at the first call that needs more (that call allocates): make one call of
  * each size before a graph capture.  What it has outgrown is kept until
- * moshpit_destroy, so a captured graph may be replayed after larger calls.  Tensors last
- * written on another stream than the bound one must be ordered by the caller.
+ * moshpit_destroy, so a captured graph may be replayed after larger calls (one after
+ * the other: calls and replays share the workspace).  Tensors last written on another
+ * stream than the bound one must be ordered by the caller, and stay allocated until the
+ * bound stream is through with them.
  * Limits: n_tokens <= 2^30, N * n_tokens < 2^31, 2^23 elements per activation
  * row, 2^27 entries of a vocabulary of logits, a row stride of 2^29 elements (2^24
  * for the dy of moshpit_weight_grad); a launch beyond 2^32 - 1 threads is an error. */

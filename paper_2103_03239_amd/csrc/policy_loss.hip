@@ -12,7 +12,7 @@
 // wave and block) to the second (gradient).  Rows that do not fit, and few rows, are cut into slices: a first
 // kernel leaves (largest, sum) of every slice, a second joins them and writes the gradient, its second
 // read of the logits coming from the caches where they are small.  16384 bfloat16 rows of 50001, 0.7 of
-// them with a token, in 489 us, 5.7 TB/s; log-probabilities alone of 8192 binary32 rows of 30000 in 161 us, 6.1 TB/s.
+// them with a token, in 487 to 499 us, 5.7 TB/s; log-probabilities alone of 8192 binary32 rows of 30000 in 161 us, 6.1 TB/s.
 #include <hip/hip_runtime.h>
 
 #include "local_ops.h"
