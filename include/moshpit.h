@@ -394,6 +394,36 @@ int moshpit_policy_loss(moshpit_ctx *h, const void *logits_dev, int32_t dtype, i
                         const float *advantage_dev, const float *weight_dev, float clip_low, float clip_high, float kl_coef,
                         void *grad_dev, int64_t grad_row_stride, float *logp_dev, float *stats_dev);
 
+/* Root-mean-square norm of h = x + residual, with gains that are the peer's parameters column .. column + width - 1:
+ *   y[i][t][c] = h[c] * (mean over the row of h^2 + eps)^(-1/2) * gain_i[c].
+ * residual_dev NULL: h = x.  total_dev: NULL, or a matrix that gets h.  codes_dev, scales_dev: NULL, or what
+ * moshpit_checkpoint makes of out, in the same pass.  All matrices are of type dtype; h is not rounded before the norm.
+ * total and out may take the place of x or of the residual (same row stride; not both the same one). */
+int moshpit_norm(moshpit_ctx *h, const void *x_dev, int32_t dtype, int64_t x_row_stride, const void *residual_dev, int64_t residual_row_stride,
+                 int64_t n_tokens, int64_t column, int64_t width, float eps, void *total_dev, int64_t total_row_stride, void *out_dev,
+                 int64_t out_row_stride, int8_t *codes_dev, uint8_t *scales_dev);
+
+/* Its backward pass.  x: the rows that were normed (total, or x where there was no residual); dy: the gradient of out; dtotal:
+ * NULL, or the gradient of total from elsewhere (the residual stream).  With x^ = x / root mean square and u = gain dy:
+ *   dx[i][t][c] = (u[c] - x^[c] * mean(u x^)) / root mean square + dtotal[c]     (the gradient of x and of residual alike)
+ *   grad_i[column + c] = sum over t of dy[i][t][c] * x^[c];  accumulate != 0 adds to what is there.
+ * The sum takes every row, so dy is to be 0 where there is no token.  dx may take the place of dy, of x or of dtotal (same row
+ * stride). */
+int moshpit_norm_grad(moshpit_ctx *h, const void *dy_dev, int32_t dtype, int64_t dy_row_stride, const void *x_dev, int64_t x_row_stride,
+                      const void *dtotal_dev, int64_t dtotal_row_stride, int64_t n_tokens, int64_t column, int64_t width, float eps, void *dx_dev,
+                      int64_t dx_row_stride, int32_t accumulate, void *grad_dev, int64_t grad_row_stride_elems);
+
+/* Dropout: out = residual + x * 2^16 / (2^16 - cut) for the elements that are kept, residual for the others (NULL: zeros), cut =
+ * p * 2^16 rounded to nearest (0 <= p; cut <= 65535).  Element c of row n = i * n_tokens + t is kept when
+ * bits 16 (c mod 4) .. + 15 of
+ *   mix(mix(mix(seed + 0xE7037ED1A0B428DB*(step+1)) + 0x8EBC6AF09C88C6E3*(n+1)) ^ floor(c / 4))     (mix as for the schedule)
+ * are at least cut, so the mask is nowhere stored: the backward pass is this call on the gradient, without a residual.
+ * step: the device's *step_dev when the call runs (a captured graph that is replayed with another step draws anew), 0 where
+ * step_dev is NULL.  Different places in a model take different seeds.  out may take the place of x or of the residual (same
+ * row stride). */
+int moshpit_dropout(moshpit_ctx *h, const void *x_dev, int32_t dtype, int64_t x_row_stride, const void *residual_dev, int64_t residual_row_stride,
+                    int64_t n_tokens, int64_t width, double p, uint64_t seed, const uint64_t *step_dev, void *out_dev, int64_t out_row_stride);
+
 /* Measurement aids (no counterpart in the paper).
  *
  * moshpit_set_tuning overrides the launch shape of the averaging kernel:

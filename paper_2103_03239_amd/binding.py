@@ -25,7 +25,7 @@ EXPORTS = [
     "moshpit_run", "moshpit_dist_to_mean", "moshpit_dist_to_mean_static", "moshpit_dist_to_mean_subset", "moshpit_group_keys", "moshpit_schedule_mask",
     "moshpit_dynamic_reset", "moshpit_dynamic_round", "moshpit_dynamic_keys", "moshpit_local_step", "moshpit_sgd_round", "moshpit_sgd_run", "moshpit_random_groups_round", "moshpit_random_permutation", "moshpit_refresh", "moshpit_refresh_donors", "moshpit_grouped_round", "moshpit_set_tuning", "moshpit_copy_probe", "moshpit_check_bf16_rounding", "moshpit_sync", "moshpit_last_error",
     "moshpit_embed", "moshpit_embed_grad", "moshpit_checkpoint", "moshpit_checkpoint_restore", "moshpit_weight_grad", "moshpit_token_logp",
-    "moshpit_policy_loss",
+    "moshpit_policy_loss", "moshpit_norm", "moshpit_norm_grad", "moshpit_dropout",
 ]
 
 
@@ -111,6 +111,9 @@ def load_library() -> ctypes.CDLL:
     lib.moshpit_weight_grad.argtypes = [vp, vp, i32, i64, vp, vp, i64, i64, i64, i32, vp, i64, i64]
     lib.moshpit_token_logp.argtypes = [vp, vp, i32, i64, vp, i64, i64, vp]
     lib.moshpit_policy_loss.argtypes = [vp, vp, i32, i64, vp, i64, i64, vp, vp, vp, vp, f32, f32, f32, vp, i64, vp, vp]
+    lib.moshpit_norm.argtypes = [vp, vp, i32, i64, vp, i64, i64, i64, i64, f32, vp, i64, vp, i64, vp, vp]
+    lib.moshpit_norm_grad.argtypes = [vp, vp, i32, i64, vp, i64, vp, i64, i64, i64, i64, f32, vp, i64, i32, vp, i64]
+    lib.moshpit_dropout.argtypes = [vp, vp, i32, i64, vp, i64, i64, i64, ctypes.c_double, ctypes.c_uint64, vp, vp, i64]
     lib.moshpit_sync.argtypes = [vp]
     lib.moshpit_last_error.argtypes = [vp]
     lib.moshpit_last_error.restype = ctypes.c_char_p
@@ -509,6 +512,71 @@ class Moshpit:
         self._check(self._lib.moshpit_policy_loss(self._h, zp, code, stride, tp, T, vocab, old, ref, adv, w, clip_low, clip_high, kl_coef, dp,
                                                   dstride, logp.data_ptr(), stats.data_ptr()), "policy_loss")
         return stats, logp
+
+    def _like(self, x, code: int, T: int, width: int, name: str):
+        """Pointer and row stride of a further matrix of a call, of the type and shape of the first; None: (None, 0)."""
+        if x is None:
+            return None, 0
+        p, c, _, w, stride = self._rows(x, name, T)
+        if c != code or w != width:
+            raise ValueError(f"{name} must have the type and shape of the input")
+        return p, stride
+
+    def norm(self, x, column: int, residual=None, eps: float = 1e-6, saved: bool = False, out=None, total=None):
+        """Root-mean-square norm of h = x + residual [N, T, width] with the gain that starts at parameter `column` of every peer.
+        Returns (y, h, saved): h is x where there is no residual, saved is what checkpoint(y) gives where that is wanted, else None."""
+        torch = _torch()
+        xp, code, T, width, stride = self._rows(x, "x")
+        if residual is None:
+            if total is not None:
+                raise ValueError("without a residual x is the total itself")
+        wanted = [((self.N, T, width), x.dtype)] * ((out is None) + (total is None and residual is not None))
+        if saved:
+            wanted += [((self.N, T, width), torch.int8), ((self.N, T, -(-width // 32)), torch.uint8)]
+        rp, rs = self._like(residual, code, T, width, "residual")
+        new = self._new(x.device, *wanted) if wanted else []
+        out = new.pop(0) if out is None else out
+        if residual is not None and total is None:
+            total = new.pop(0)
+        op, os_ = self._like(out, code, T, width, "out")
+        hp, hs = self._like(total, code, T, width, "total")
+        self._lend(x, residual, out, total)
+        self._check(self._lib.moshpit_norm(self._h, xp, code, stride, rp, rs, T, column, width, eps, hp, hs, op, os_,
+                                           *([t.data_ptr() for t in new] if saved else (None, None))), "norm")
+        return out, x if residual is None else total, tuple(new) if saved else None
+
+    def norm_grad(self, dY, x, G, column: int, eps: float = 1e-6, dtotal=None, accumulate: bool = False, out=None):
+        """Backward pass of norm for dY [N, T, width]; x: the h that norm returned, dtotal: the gradient that reaches h elsewhere.  Returns
+        h's gradient (in `out` if given); the gain's goes into columns column.. of the gradient matrix G."""
+        yp, code, T, width, stride = self._rows(dY, "dY")
+        xp, xs = self._like(x, code, T, width, "x")
+        tp, ts = self._like(dtotal, code, T, width, "dtotal")
+        gp, gs = self._grad(G)
+        if out is None:
+            out, = self._new(dY.device, ((self.N, T, width), dY.dtype))
+        op, os_ = self._like(out, code, T, width, "out")
+        self._lend(dY, x, dtotal, G, out)
+        self._check(self._lib.moshpit_norm_grad(self._h, yp, code, stride, xp, xs, tp, ts, T, column, width, eps, op, os_, int(accumulate), gp, gs),
+                    "norm_grad")
+        return out
+
+    def dropout(self, x, p: float, seed: int, step=None, residual=None, out=None):
+        """residual + dropout(x) for x [N, T, width]; the mask follows from seed (0 .. 2^64 - 1), from `step` (None: 0, or one int64 on the GPU,
+        read when the call runs) and from the place of an element.  The backward pass is the same call on the gradient."""
+        torch = _torch()
+        xp, code, T, width, stride = self._rows(x, "x")
+        rp, rs = self._like(residual, code, T, width, "residual")
+        if step is not None and (step.dtype is not torch.int64 or step.numel() != 1 or not step.is_cuda):
+            raise ValueError("step must be one int64 on the GPU")
+        if not 0 <= seed < 1 << 64:
+            raise ValueError("seed must be a whole number from 0 to 2^64 - 1")
+        if out is None:
+            out, = self._new(x.device, ((self.N, T, width), x.dtype))
+        op, os_ = self._like(out, code, T, width, "out")
+        self._lend(x, residual, step, out)
+        self._check(self._lib.moshpit_dropout(self._h, xp, code, stride, rp, rs, T, width, p, seed, None if step is None else step.data_ptr(), op, os_),
+                    "dropout")
+        return out
 
     def sync(self) -> None:
         self._check(self._lib.moshpit_sync(self._h), "sync")

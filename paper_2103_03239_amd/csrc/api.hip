@@ -1501,6 +1501,75 @@ int moshpit_policy_loss(moshpit_ctx *h, const void *logits_dev, int32_t dtype, i
     return MOSHPIT_OK;
 }
 
+int moshpit_norm(moshpit_ctx *h, const void *x_dev, int32_t dtype, int64_t x_row_stride, const void *residual_dev, int64_t residual_row_stride,
+                 int64_t n_tokens, int64_t column, int64_t width, float eps, void *total_dev, int64_t total_row_stride, void *out_dev,
+                 int64_t out_row_stride, int8_t *codes_dev, uint8_t *scales_dev)
+{
+    CHECK(check_ready(h));
+    CHECK(check_params(h, column, 1, width));
+    CHECK(check_tokens(h, n_tokens));
+    CHECK(check_matrix(h, "input", x_dev, dtype, n_tokens, width, x_row_stride));
+    if (residual_dev) CHECK(check_matrix(h, "residual", residual_dev, dtype, n_tokens, width, residual_row_stride));
+    if (total_dev) CHECK(check_matrix(h, "total", total_dev, dtype, n_tokens, width, total_row_stride));
+    CHECK(check_matrix(h, "output", out_dev, dtype, n_tokens, width, out_row_stride));
+    if (n_tokens > 0 && !codes_dev != !scales_dev) return fail(h, MOSHPIT_EINVAL, "codes and scales: both or neither");
+    if (!(eps >= 0.f) || !std::isfinite(eps)) return fail(h, MOSHPIT_EINVAL, "eps must be finite and >= 0");
+    if (!norm_fits(h->N, n_tokens, width)) return fail(h, MOSHPIT_EINVAL, "%lld x %lld rows of %lld are too many for one call", (long long)h->N, (long long)n_tokens, (long long)width);
+    int compute_units = 0;
+    HIP_TRY(h, current_compute_units(&compute_units));
+    const NormArgs a{static_cast<const char *>(x_dev), static_cast<const char *>(residual_dev), static_cast<char *>(total_dev), static_cast<char *>(out_dev),
+                     codes_dev, scales_dev, static_cast<const char *>(h->X) + column * elem_bytes(h->dtype), h->N, n_tokens, width, x_row_stride,
+                     residual_row_stride, total_row_stride, out_row_stride, h->row_stride, eps};
+    HIP_TRY(h, launch_norm(a, dtype, h->dtype, compute_units, h->stream));
+    return MOSHPIT_OK;
+}
+
+int moshpit_norm_grad(moshpit_ctx *h, const void *dy_dev, int32_t dtype, int64_t dy_row_stride, const void *x_dev, int64_t x_row_stride,
+                      const void *dtotal_dev, int64_t dtotal_row_stride, int64_t n_tokens, int64_t column, int64_t width, float eps, void *dx_dev,
+                      int64_t dx_row_stride, int32_t accumulate, void *grad_dev, int64_t grad_row_stride_elems)
+{
+    CHECK(check_ready(h));
+    CHECK(check_params(h, column, 1, width));
+    CHECK(check_tokens(h, n_tokens));
+    CHECK(check_matrix(h, "output's gradient", dy_dev, dtype, n_tokens, width, dy_row_stride));
+    CHECK(check_matrix(h, "normed rows", x_dev, dtype, n_tokens, width, x_row_stride));
+    if (dtotal_dev) CHECK(check_matrix(h, "total's gradient", dtotal_dev, dtype, n_tokens, width, dtotal_row_stride));
+    CHECK(check_matrix(h, "input's gradient", dx_dev, dtype, n_tokens, width, dx_row_stride));
+    CHECK(check_grad(h, grad_dev, grad_row_stride_elems));
+    if (!(eps >= 0.f) || !std::isfinite(eps)) return fail(h, MOSHPIT_EINVAL, "eps must be finite and >= 0");
+    if (!norm_fits(h->N, n_tokens, width)) return fail(h, MOSHPIT_EINVAL, "%lld x %lld rows of %lld are too many for one call", (long long)h->N, (long long)n_tokens, (long long)width);
+    int compute_units = 0;
+    HIP_TRY(h, current_compute_units(&compute_units));
+    CHECK(reserve_work(h, norm_grad_work_bytes(h->N, n_tokens, width, compute_units)));
+    const int64_t bytes = elem_bytes(h->dtype);
+    const NormGradArgs a{static_cast<const char *>(dy_dev), static_cast<const char *>(x_dev), static_cast<const char *>(dtotal_dev), static_cast<char *>(dx_dev),
+                         static_cast<const char *>(h->X) + column * bytes, h->N, n_tokens, width, dy_row_stride, x_row_stride, dtotal_row_stride,
+                         dx_row_stride, h->row_stride, eps};
+    HIP_TRY(h, launch_norm_grad(a, dtype, h->dtype, accumulate != 0, static_cast<char *>(grad_dev) + column * bytes, grad_row_stride_elems,
+                                h->work.block(), compute_units, h->stream));
+    return MOSHPIT_OK;
+}
+
+int moshpit_dropout(moshpit_ctx *h, const void *x_dev, int32_t dtype, int64_t x_row_stride, const void *residual_dev, int64_t residual_row_stride,
+                    int64_t n_tokens, int64_t width, double p, uint64_t seed, const uint64_t *step_dev, void *out_dev, int64_t out_row_stride)
+{
+    CHECK(check_ready(h));
+    CHECK(check_tokens(h, n_tokens));
+    if (width < 1 || width > kMostWidth) return fail(h, MOSHPIT_EINVAL, "rows of %lld: 1 .. 2^23", (long long)width);
+    CHECK(check_matrix(h, "input", x_dev, dtype, n_tokens, width, x_row_stride));
+    if (residual_dev) CHECK(check_matrix(h, "residual", residual_dev, dtype, n_tokens, width, residual_row_stride));
+    CHECK(check_matrix(h, "output", out_dev, dtype, n_tokens, width, out_row_stride));
+    if (!(p >= 0.0 && p < 1.0)) return fail(h, MOSHPIT_EINVAL, "the probability must be within [0, 1)");
+    const uint32_t cut = static_cast<uint32_t>(p * 65536.0 + 0.5);
+    if (cut > 65535) return fail(h, MOSHPIT_EINVAL, "a probability of %.9g drops everything (it is taken to the nearest multiple of 2^-16)", p);
+    if (reinterpret_cast<uintptr_t>(step_dev) % 8 != 0) return fail(h, MOSHPIT_EINVAL, "step: pointer is not aligned to 8 bytes");
+    const DropoutArgs a{static_cast<const char *>(x_dev), static_cast<const char *>(residual_dev), static_cast<char *>(out_dev), step_dev, h->N * n_tokens, width,
+                        x_row_stride, residual_row_stride, out_row_stride, seed, cut, static_cast<float>(65536.0 / (65536 - cut))};
+    if (!dropout_fits(a)) return fail(h, MOSHPIT_EINVAL, "%lld rows of %lld are too many for one call", (long long)a.rows, (long long)width);
+    HIP_TRY(h, launch_dropout(a, dtype, h->stream));
+    return MOSHPIT_OK;
+}
+
 int moshpit_sync(moshpit_ctx *h)
 {
     if (!h) return MOSHPIT_EINVAL;

@@ -1,5 +1,5 @@
 // Launch interface of the operators of a peer's local step (token embeddings, 8-bit checkpoints,
-// weight gradients, the policy loss) between api.hip and their kernels.  Types: 0 = binary32,
+// weight gradients, the policy loss, norms, dropout, attention) between api.hip and their kernels.  Types: 0 = binary32,
 // 1 = bfloat16.  Strides in elements.  All pointers are device pointers; argument checks are api.hip's.
 #pragma once
 
@@ -57,5 +57,40 @@ hipError_t launch_policy_loss(const void *logits, int dtype, int64_t N, int64_t 
                               int compute_units, hipStream_t stream);
 hipError_t launch_token_logp(const void *logits, int dtype, int64_t rows, int64_t vocab, int64_t stride, const int32_t *tokens, float *logp,
                              void *work, int compute_units, hipStream_t stream);
+
+// Root-mean-square norms: rows of `width` elements, row i * T + t for token t of peer i, gain i at `gain` + i * gain_stride elements.
+struct NormArgs {
+    const char *x, *residual;            // residual, total, codes and scales may be nullptr
+    char *total, *out;
+    int8_t *codes;
+    uint8_t *scales;
+    const char *gain;
+    int64_t N, T, width, x_stride, residual_stride, total_stride, out_stride, gain_stride;
+    float eps;
+};
+struct NormGradArgs {
+    const char *dy, *x, *dtotal;         // dtotal may be nullptr
+    char *dx;
+    const char *gain;
+    int64_t N, T, width, dy_stride, x_stride, dtotal_stride, dx_stride, gain_stride;
+    float eps;
+};
+bool norm_fits(int64_t N, int64_t T, int64_t width);
+hipError_t launch_norm(const NormArgs &a, int dtype, int state_dtype, int compute_units, hipStream_t stream);
+int64_t norm_grad_work_bytes(int64_t N, int64_t T, int64_t width, int compute_units);
+hipError_t launch_norm_grad(const NormGradArgs &a, int dtype, int state_dtype, bool accumulate, char *grad, int64_t grad_stride, void *work,
+                            int compute_units, hipStream_t stream);
+
+struct DropoutArgs {
+    const char *x, *residual;            // residual and step may be nullptr
+    char *out;
+    const uint64_t *step;
+    int64_t rows, width, x_stride, residual_stride, out_stride;
+    uint64_t seed;
+    uint32_t cut;                        // of 2^16: elements with fewer are dropped
+    float factor;
+};
+bool dropout_fits(const DropoutArgs &a);
+hipError_t launch_dropout(const DropoutArgs &a, int dtype, hipStream_t stream);
 
 }  // namespace moshpit
