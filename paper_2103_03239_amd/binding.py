@@ -26,6 +26,7 @@ EXPORTS = [
     "moshpit_dynamic_reset", "moshpit_dynamic_round", "moshpit_dynamic_keys", "moshpit_local_step", "moshpit_sgd_round", "moshpit_sgd_run", "moshpit_random_groups_round", "moshpit_random_permutation", "moshpit_refresh", "moshpit_refresh_donors", "moshpit_grouped_round", "moshpit_set_tuning", "moshpit_copy_probe", "moshpit_check_bf16_rounding", "moshpit_sync", "moshpit_last_error",
     "moshpit_embed", "moshpit_embed_grad", "moshpit_checkpoint", "moshpit_checkpoint_restore", "moshpit_weight_grad", "moshpit_token_logp",
     "moshpit_policy_loss", "moshpit_norm", "moshpit_norm_grad", "moshpit_dropout",
+    "moshpit_attention", "moshpit_attention_grad", "moshpit_attention_cached",
 ]
 
 
@@ -114,6 +115,9 @@ def load_library() -> ctypes.CDLL:
     lib.moshpit_norm.argtypes = [vp, vp, i32, i64, vp, i64, i64, i64, i64, f32, vp, i64, vp, i64, vp, vp]
     lib.moshpit_norm_grad.argtypes = [vp, vp, i32, i64, vp, i64, vp, i64, i64, i64, i64, f32, vp, i64, i32, vp, i64]
     lib.moshpit_dropout.argtypes = [vp, vp, i32, i64, vp, i64, i64, i64, ctypes.c_double, ctypes.c_uint64, vp, vp, i64]
+    lib.moshpit_attention.argtypes = [vp, vp, i64, vp, i64, vp, i64, i32, vp, i64, i32, i32, i32, f32, vp, i64, vp]
+    lib.moshpit_attention_grad.argtypes = [vp, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, i32, vp, vp, i64, i32, i32, i32, f32, vp, i64, vp, i64, vp, i64]
+    lib.moshpit_attention_cached.argtypes = [vp, vp, i64, vp, i64, vp, i64, i32, vp, i64, i64, i64, i32, i32, i32, f32, vp, i64]
     lib.moshpit_sync.argtypes = [vp]
     lib.moshpit_last_error.argtypes = [vp]
     lib.moshpit_last_error.restype = ctypes.c_char_p
@@ -576,6 +580,78 @@ class Moshpit:
         self._lend(x, residual, step, out)
         self._check(self._lib.moshpit_dropout(self._h, xp, code, stride, rp, rs, T, width, p, seed, None if step is None else step.data_ptr(), op, os_),
                     "dropout")
+        return out
+
+    def _heads(self, q, k, v, heads: int, kv_heads, scale):
+        """What attention calls begin with: (q pointer, stride, k .., v ..), type code, query rows, key rows, kv_heads, depth, scale."""
+        kv_heads = heads if kv_heads is None else kv_heads
+        qp, code, rows, width, qs = self._rows(q, "q")
+        if heads < 1 or kv_heads < 1 or width % heads:
+            raise ValueError("q must hold `heads` heads in a row")
+        depth = width // heads
+        kp, kcode, keys, kwidth, ks = self._rows(k, "k")
+        vp, vcode, _, vwidth, vs = self._rows(v, "v", keys)
+        if kcode != code or vcode != code or kwidth != kv_heads * depth or vwidth != kwidth:
+            raise ValueError("k and v must have the type of q and hold `kv_heads` heads of its depth")
+        return (qp, qs, kp, ks, vp, vs), code, rows, keys, kv_heads, depth, depth ** -0.5 if scale is None else scale
+
+    def _first(self, first, T: int):
+        if first.dtype is not _torch().int32 or first.shape != (self.N, T) or not first.is_cuda or not first.is_contiguous():
+            raise ValueError(f"first must be a contiguous int32 GPU tensor {[self.N, T]}")
+        return first.data_ptr()
+
+    def attention(self, q, k, v, first, heads: int, kv_heads: int | None = None, scale: float | None = None, out=None):
+        """Causal attention for q [N, T, heads * depth], k and v [N, T, kv_heads * depth] over packed sequences: token t sees tokens first[t] .. t
+        (int32 [N, T]; -1: no token).  scale: depth ** -0.5 if not given.  Returns (out, lse [N, heads, T])."""
+        rows, code, T, keys, kv_heads, depth, scale = self._heads(q, k, v, heads, kv_heads, scale)
+        if keys != T:
+            raise ValueError("q, k and v must have the same tokens")
+        fp, f32 = self._first(first, T), _torch().float32
+        if out is None:
+            out, lse = self._new(q.device, (q.shape, q.dtype), ((self.N, heads, T), f32))
+        else:
+            lse, = self._new(q.device, ((self.N, heads, T), f32))
+        op, os_ = self._like(out, code, T, heads * depth, "out")
+        self._lend(q, k, v, first, out)
+        self._check(self._lib.moshpit_attention(self._h, *rows, code, fp, T, heads, kv_heads, depth, scale, op, os_, lse.data_ptr()), "attention")
+        return out, lse
+
+    def attention_grad(self, dout, q, k, v, out, lse, first, heads: int, kv_heads: int | None = None, scale: float | None = None, dq=None, dk=None,
+                       dv=None):
+        """Backward pass of attention for dout [N, T, heads * depth], with the out and lse that it returned: (dq, dk, dv), in the tensors given for
+        them or in new ones."""
+        rows, code, T, keys, kv_heads, depth, scale = self._heads(q, k, v, heads, kv_heads, scale)
+        if keys != T:
+            raise ValueError("q, k and v must have the same tokens")
+        fp, (lp,) = self._first(first, T), self._per_token((self.N, heads, T), (lse, "lse"))
+        width = heads * depth
+        yp, ys = self._like(dout, code, T, width, "dout")
+        op, os_ = self._like(out, code, T, width, "out")
+        missing = [t for t, given in ((q, dq), (k, dk), (v, dv)) if given is None]
+        new = self._new(q.device, *((t.shape, t.dtype) for t in missing)) if missing else []
+        dq, dk, dv = (new.pop(0) if given is None else given for given in (dq, dk, dv))
+        into = [*self._like(dq, code, T, width, "dq"), *self._like(dk, code, T, kv_heads * depth, "dk"), *self._like(dv, code, T, kv_heads * depth, "dv")]
+        self._lend(dout, q, k, v, out, lse, first, dq, dk, dv)
+        self._check(self._lib.moshpit_attention_grad(self._h, yp, ys, *rows, op, os_, code, lp, fp, T, heads, kv_heads, depth, scale, *into),
+                    "attention_grad")
+        return dq, dk, dv
+
+    def attention_cached(self, q, k, v, spans, heads: int, kv_heads: int | None = None, scale: float | None = None, out=None):
+        """Attention of the new tokens of S sequences a peer, q [N, S * new, heads * depth], over the rows spans[i, s, 0] .. spans[i, s, 1] - 1 (int32
+        [N, S, 2]) of the caches k and v [N, keys, kv_heads * depth], whose last ones are the new tokens' own."""
+        rows, code, T, keys, kv_heads, depth, scale = self._heads(q, k, v, heads, kv_heads, scale)
+        if spans.dtype is not _torch().int32 or spans.dim() != 3 or spans.shape[0] != self.N or spans.shape[2] != 2 or not spans.is_cuda or \
+                not spans.is_contiguous():
+            raise ValueError("spans must be a contiguous int32 GPU tensor [N, S, 2]")
+        seqs = spans.shape[1]
+        if (T % seqs if seqs else T) or (seqs and not T):
+            raise ValueError("q must hold the same number of new tokens, 1 or more, for every sequence")
+        if out is None:
+            out, = self._new(q.device, (q.shape, q.dtype))
+        op, os_ = self._like(out, code, T, heads * depth, "out")
+        self._lend(q, k, v, spans, out)
+        self._check(self._lib.moshpit_attention_cached(self._h, *rows, code, spans.data_ptr(), seqs, T // seqs if seqs else 1, keys, heads, kv_heads, depth,
+                                                       scale, op, os_), "attention_cached")
         return out
 
     def sync(self) -> None:

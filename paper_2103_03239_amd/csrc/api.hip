@@ -1570,6 +1570,97 @@ int moshpit_dropout(moshpit_ctx *h, const void *x_dev, int32_t dtype, int64_t x_
     return MOSHPIT_OK;
 }
 
+namespace {
+int check_heads(moshpit_ctx *h, int32_t heads, int32_t kv_heads, int32_t depth, float scale)
+{
+    if (heads < 1 || kv_heads < 1 || heads % kv_heads != 0 || heads > 65536)
+        return fail(h, MOSHPIT_EINVAL, "%d heads over %d heads of keys: a multiple, at most 2^16", heads, kv_heads);
+    if (depth < 1 || depth > 256) return fail(h, MOSHPIT_EINVAL, "a head of %d: 1 .. 256", depth);
+    if (!(scale > 0.f) || !std::isfinite(scale)) return fail(h, MOSHPIT_EINVAL, "the scale must be finite and > 0");
+    return MOSHPIT_OK;
+}
+}  // namespace
+
+int moshpit_attention(moshpit_ctx *h, const void *q_dev, int64_t q_row_stride, const void *k_dev, int64_t k_row_stride, const void *v_dev,
+                      int64_t v_row_stride, int32_t dtype, const int32_t *first_dev, int64_t n_tokens, int32_t heads, int32_t kv_heads,
+                      int32_t depth, float scale, void *out_dev, int64_t out_row_stride, float *lse_dev)
+{
+    CHECK(check_ready(h));
+    CHECK(check_heads(h, heads, kv_heads, depth, scale));
+    CHECK(check_tokens(h, n_tokens));
+    CHECK(check_words(h, "first tokens", first_dev, n_tokens));
+    CHECK(check_words(h, "log-sums", lse_dev, 0));
+    const int64_t width = int64_t(heads) * depth, kv_width = int64_t(kv_heads) * depth;
+    CHECK(check_matrix(h, "queries", q_dev, dtype, n_tokens, width, q_row_stride));
+    CHECK(check_matrix(h, "keys", k_dev, dtype, n_tokens, kv_width, k_row_stride));
+    CHECK(check_matrix(h, "values", v_dev, dtype, n_tokens, kv_width, v_row_stride));
+    CHECK(check_matrix(h, "output", out_dev, dtype, n_tokens, width, out_row_stride));
+    const AttentionArgs a{static_cast<const char *>(q_dev), static_cast<const char *>(k_dev), static_cast<const char *>(v_dev), static_cast<char *>(out_dev), lse_dev,
+                          first_dev, h->N, n_tokens, q_row_stride, k_row_stride, v_row_stride, out_row_stride, heads, kv_heads, depth, scale, 0};
+    if (!attention_fits(a)) return fail(h, MOSHPIT_EINVAL, "%lld x %lld tokens of %d heads are too many for one call", (long long)h->N, (long long)n_tokens, heads);
+    HIP_TRY(h, launch_attention(a, dtype, h->stream));
+    return MOSHPIT_OK;
+}
+
+int moshpit_attention_grad(moshpit_ctx *h, const void *dout_dev, int64_t dout_row_stride, const void *q_dev, int64_t q_row_stride, const void *k_dev,
+                           int64_t k_row_stride, const void *v_dev, int64_t v_row_stride, const void *out_dev, int64_t out_row_stride, int32_t dtype,
+                           const float *lse_dev, const int32_t *first_dev, int64_t n_tokens, int32_t heads, int32_t kv_heads, int32_t depth, float scale,
+                           void *dq_dev, int64_t dq_row_stride, void *dk_dev, int64_t dk_row_stride, void *dv_dev, int64_t dv_row_stride)
+{
+    CHECK(check_ready(h));
+    CHECK(check_heads(h, heads, kv_heads, depth, scale));
+    CHECK(check_tokens(h, n_tokens));
+    CHECK(check_words(h, "first tokens", first_dev, n_tokens));
+    CHECK(check_words(h, "log-sums", lse_dev, n_tokens));
+    const int64_t width = int64_t(heads) * depth, kv_width = int64_t(kv_heads) * depth;
+    CHECK(check_matrix(h, "output's gradient", dout_dev, dtype, n_tokens, width, dout_row_stride));
+    CHECK(check_matrix(h, "queries", q_dev, dtype, n_tokens, width, q_row_stride));
+    CHECK(check_matrix(h, "keys", k_dev, dtype, n_tokens, kv_width, k_row_stride));
+    CHECK(check_matrix(h, "values", v_dev, dtype, n_tokens, kv_width, v_row_stride));
+    CHECK(check_matrix(h, "output", out_dev, dtype, n_tokens, width, out_row_stride));
+    CHECK(check_matrix(h, "queries' gradient", dq_dev, dtype, n_tokens, width, dq_row_stride));
+    CHECK(check_matrix(h, "keys' gradient", dk_dev, dtype, n_tokens, kv_width, dk_row_stride));
+    CHECK(check_matrix(h, "values' gradient", dv_dev, dtype, n_tokens, kv_width, dv_row_stride));
+    const AttentionGradArgs a{static_cast<const char *>(q_dev), static_cast<const char *>(k_dev), static_cast<const char *>(v_dev), static_cast<const char *>(out_dev),
+                              static_cast<const char *>(dout_dev), static_cast<char *>(dq_dev), static_cast<char *>(dk_dev), static_cast<char *>(dv_dev), lse_dev,
+                              first_dev, h->N, n_tokens, q_row_stride, k_row_stride, v_row_stride, out_row_stride, dout_row_stride, dq_row_stride,
+                              dk_row_stride, dv_row_stride, heads, kv_heads, depth, scale};
+    if (!attention_grad_fits(a, dtype)) return fail(h, MOSHPIT_EINVAL, "%lld x %lld tokens of %d heads are too many for one call", (long long)h->N, (long long)n_tokens, heads);
+    int compute_units = 0;
+    HIP_TRY(h, current_compute_units(&compute_units));
+    CHECK(reserve_work(h, attention_grad_work_bytes(a, dtype, compute_units)));
+    HIP_TRY(h, launch_attention_grad(a, dtype, h->work.block(), compute_units, h->stream));
+    return MOSHPIT_OK;
+}
+
+int moshpit_attention_cached(moshpit_ctx *h, const void *q_dev, int64_t q_row_stride, const void *k_dev, int64_t k_row_stride, const void *v_dev,
+                             int64_t v_row_stride, int32_t dtype, const int32_t *spans_dev, int64_t sequences, int64_t n_new, int64_t n_keys, int32_t heads,
+                             int32_t kv_heads, int32_t depth, float scale, void *out_dev, int64_t out_row_stride)
+{
+    CHECK(check_ready(h));
+    CHECK(check_heads(h, heads, kv_heads, depth, scale));
+    if (sequences < 0 || n_new < 1 || n_new > 4096 || sequences > kMostTokens)
+        return fail(h, MOSHPIT_EINVAL, "%lld new tokens of %lld sequences: 1 .. 4096 of at most 2^30", (long long)n_new, (long long)sequences);
+    CHECK(check_tokens(h, sequences * n_new));
+    CHECK(check_tokens(h, n_keys));
+    CHECK(check_words(h, "spans", spans_dev, sequences));
+    const int64_t width = int64_t(heads) * depth, kv_width = int64_t(kv_heads) * depth;
+    CHECK(check_matrix(h, "queries", q_dev, dtype, sequences, width, q_row_stride));
+    CHECK(check_matrix(h, "keys", k_dev, dtype, n_keys, kv_width, k_row_stride));
+    CHECK(check_matrix(h, "values", v_dev, dtype, n_keys, kv_width, v_row_stride));
+    CHECK(check_matrix(h, "output", out_dev, dtype, sequences, width, out_row_stride));
+    int compute_units = 0;
+    HIP_TRY(h, current_compute_units(&compute_units));
+    const CachedArgs a{static_cast<const char *>(q_dev), static_cast<const char *>(k_dev), static_cast<const char *>(v_dev), static_cast<char *>(out_dev), spans_dev, h->N,
+                       n_keys, q_row_stride, k_row_stride, v_row_stride, out_row_stride, static_cast<int32_t>(sequences), static_cast<int32_t>(n_new), heads, kv_heads,
+                       depth, scale, 0, 0};
+    const CachedPlan p = cached_plan(a, compute_units);
+    if (!p.fits) return fail(h, MOSHPIT_EINVAL, "%lld new tokens of %lld x %lld sequences are too many for one call", (long long)n_new, (long long)h->N, (long long)sequences);
+    CHECK(reserve_work(h, p.work_bytes));
+    HIP_TRY(h, launch_cached(a, dtype, p, h->work.block(), h->stream));
+    return MOSHPIT_OK;
+}
+
 int moshpit_sync(moshpit_ctx *h)
 {
     if (!h) return MOSHPIT_EINVAL;

@@ -93,4 +93,51 @@ struct DropoutArgs {
 bool dropout_fits(const DropoutArgs &a);
 hipError_t launch_dropout(const DropoutArgs &a, int dtype, hipStream_t stream);
 
+// Causal attention: query rows of heads * depth elements, key and value rows of kv_heads * depth, row i * T + t for token t of peer i.
+// first: [N][T], the first token that a token sees (a token outside 0 .. its own number: no token).
+struct AttentionArgs {
+    const char *q, *k, *v;
+    char *out;
+    float *lse;                          // [N][heads][T]; may be nullptr
+    const int32_t *first;
+    int64_t N, T, q_stride, k_stride, v_stride, out_stride;
+    int32_t heads, kv_heads, depth;
+    float scale;
+    uint32_t tiles;                      // (launch's own)
+};
+bool attention_fits(const AttentionArgs &a);
+hipError_t launch_attention(AttentionArgs a, int dtype, hipStream_t stream);
+
+// Its backward pass, into dq, dk and dv.
+struct AttentionGradArgs {
+    const char *q, *k, *v, *out, *dout;
+    char *dq, *dk, *dv;
+    const float *lse;
+    const int32_t *first;
+    int64_t N, T, q_stride, k_stride, v_stride, out_stride, dout_stride, dq_stride, dk_stride, dv_stride;
+    int32_t heads, kv_heads, depth;
+    float scale;
+};
+bool attention_grad_fits(const AttentionGradArgs &a, int dtype);
+int64_t attention_grad_work_bytes(const AttentionGradArgs &a, int dtype, int compute_units);
+hipError_t launch_attention_grad(const AttentionGradArgs &a, int dtype, void *work, int compute_units, hipStream_t stream);
+
+// `fresh` new tokens of each of `seqs` sequences a peer against rows spans[..][0] .. spans[..][1] - 1 of its n_keys keys and values.
+struct CachedArgs {
+    const char *q, *k, *v;
+    char *out;
+    const int32_t *spans;                // [N][seqs][2]
+    int64_t N, n_keys, q_stride, k_stride, v_stride, out_stride;
+    int32_t seqs, fresh, heads, kv_heads, depth;
+    float scale;
+    int32_t col_tiles, splits;           // (launch's own)
+};
+struct CachedPlan {
+    int32_t col_tiles, splits;
+    int64_t work_bytes;
+    bool fits;
+};
+CachedPlan cached_plan(const CachedArgs &a, int compute_units);
+hipError_t launch_cached(CachedArgs a, int dtype, const CachedPlan &p, void *work, hipStream_t stream);
+
 }  // namespace moshpit
