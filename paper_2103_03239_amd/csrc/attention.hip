@@ -8,8 +8,8 @@
 // Sums are rescaled only where a query's largest score has grown by more than 2^8 (weights stay below 2^8, in binary32).
 //
 // A weight of 0 times a value that is no number is no number, so a sequence's infinities would reach others that share its tiles.  Rows
-// of places without a token are never read.  For the rest the block looks at its results: where they are not finite, it goes over its
-// keys again with such values taken out of the tiles, and adds each to the queries that see its row.
+// of places without a token are zeros in the tiles.  For the rest a wave looks at its results: a query whose weights are numbers and whose sums are
+// not is taken again, key by key over those that it sees.
 #include <hip/hip_runtime.h>
 
 #include "attention_tile.h"
@@ -18,19 +18,16 @@
 namespace moshpit {
 namespace {
 
-constexpr int kThreads = 256, kWaves = 4;
+constexpr int kThreads = 256, kWaves = 4, kQueries = 32 * kWaves;     // of a block
 constexpr float kSlack = 8.f;                            // by how many powers of two weights may pass 1
 
-// Rows of a tile: 64 where four tiles of them fit 64 KiB.
-template <int DT, int DP> constexpr int tile_rows() { return 4 * 64 * row_elems_of(DP) * Num<DT>::ES <= 65536 ? 64 : 32; }
-
 // Waves of a block of cached_kernel: four where their tiles fit 64 KiB.
-template <int DT, int DP> constexpr int cached_waves() { return 4 * 2 * 32 * row_elems_of(DP) * Num<DT>::ES <= 65536 ? 4 : 2; }
+template <Form F, int DP> constexpr int cached_waves() { return 4 * 2 * tile_bytes<F, DP>(32) <= 65536 ? 4 : 2; }
 
-// A wave's queries (columns) and their sums so far.
-template <int DT, int DP> struct Queries {
+// A wave's 32 queries (columns) and their sums so far.
+template <Form F, int DP> struct Queries {
     static constexpr int BLOCKS = DP / 32;
-    Held<DT, DP> q;
+    Held<F, DP> q;
     f32x16 sum[BLOCKS];
     float top, total;                    // top: what scores * scale log2 e are taken from (-inf: none yet); total: of this half's weights
 
@@ -42,60 +39,57 @@ template <int DT, int DP> struct Queries {
         for (int m = 0; m < BLOCKS; ++m) sum[m] = f32x16{};
     }
 
-    // Scores of ROWS keys to weights; `largest` of them (this half's).
-    template <int N> __device__ __forceinline__ void weigh(f32x16 (&s)[N], float scale)
+    // Scores of 32 * N keys, from the tile's first row on.
+    template <int ROWS, int N> __device__ __forceinline__ void score(const typename Num<F>::lds_t *keys, f32x16 (&s)[N]) const
+    {
+#pragma unroll
+        for (int n = 0; n < N; ++n) s[n] = rows_times<F, DP, ROWS>(keys, 32 * n, q);
+    }
+    template <int N> __device__ __forceinline__ static float largest(const f32x16 (&s)[N])
     {
         float most = s[0][0];
 #pragma unroll
         for (int n = 0; n < N; ++n)
 #pragma unroll
             for (int r = 0; r < 16; ++r) most = fmaxf(most, s[n][r]);
+        return most;
+    }
+    // Before weights are taken from scores of which `most` is the largest (of this half's).
+    __device__ __forceinline__ void rescale(float most, float scale)
+    {
         most = halves_max(most) * scale;
-        if (__any(most > top + kSlack)) {
-            const float now = fmaxf(top, most), factor = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top - now);
-            top = now;
-            total *= factor;
+        if (!__any(most > top + kSlack)) return;
+        const float now = fmaxf(top, most), factor = now == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top - now);
+        top = now;
+        total *= factor;
 #pragma unroll
-            for (int m = 0; m < BLOCKS; ++m)
+        for (int m = 0; m < BLOCKS; ++m)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) sum[m][r] *= factor;
-        }
+            for (int r = 0; r < 16; ++r) sum[m][r] *= factor;
+    }
+    __device__ __forceinline__ void weigh(f32x16 &s, float scale, Weights<F> &w)
+    {
         const float from = top == -INFINITY ? 0.f : top;
 #pragma unroll
-        for (int n = 0; n < N; ++n)
+        for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], scale, -from));
+        w.take(s);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                s[n][r] = __builtin_amdgcn_exp2f(fmaf(s[n][r], scale, -from));
-                total += s[n][r];
-            }
+        for (int r = 0; r < 16; ++r) total += s[r];                   // (not as rounded for the product: the log-sum is a binary32 result)
     }
-
-    // Values that are no numbers of the rows in `odd` (bits: rows of the tile), which are zeros in the tile, from memory.
-    template <int N>
-    __device__ void add_odd(const f32x16 (&weight)[N], uint64_t odd, const char *values, int64_t row_bytes, int depth)
+    // sum += rows row0 .. + 31 of the tile of values (ROWS rows) times their weights
+    template <int ROWS> __device__ __forceinline__ void add(const typename Num<F>::lds_t *values, int row0, const Weights<F> &w)
     {
-        const int half = threadIdx.x >> 5 & 1;
-        while (odd) {
-            const int row = __builtin_ctzll(odd);
-            odd &= odd - 1;
-            float w = 0.f;
 #pragma unroll
-            for (int n = 0; n < N; ++n)
+        for (int m = 0; m < BLOCKS; ++m) columns_times<F, DP, ROWS>(values, row0, 32 * m, w, sum[m]);
+    }
+    // What scores of 32 * N keys bring, whose values the tile holds.
+    template <int ROWS, int N> __device__ __forceinline__ void take(f32x16 (&s)[N], float scale, const typename Num<F>::lds_t *values)
+    {
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (row / 32 == n && (row >> 3 & 3) == r / 4 && (row & 3) == r % 4) w = weight[n][r];
-            const LanePair both = swap32(w, w);
-            w = (row & 4) ? both.second : both.first;
-            const char *value = values + row * row_bytes;
-#pragma unroll
-            for (int m = 0; m < BLOCKS; ++m)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int at = 32 * m + 8 * (r >> 2) + 4 * half + (r & 3);
-                    if (at >= depth) continue;
-                    const float v = load_one<DT>(value + at * Num<DT>::ES);
-                    if (!(fabsf(v) < INFINITY) && w != 0.f) sum[m][r] += w * v;
-                }
+        for (int n = 0; n < N; ++n) {
+            Weights<F> w;
+            weigh(s[n], scale, w);
+            add<ROWS>(values, 32 * n, w);
         }
     }
 
@@ -110,31 +104,69 @@ template <int DT, int DP> struct Queries {
     }
 };
 
-template <int DT, int DP, int WAVES_A_SIMD>
-__global__ __launch_bounds__(kThreads, WAVES_A_SIMD)
+// One query's result by a wave, key by key over those that it sees, where values that are no numbers have come into its sums.  lse: its log2-sum.
+template <int DT>
+__device__ __forceinline__ void attend_alone(const AttentionArgs &a, int64_t peer, int32_t head, int32_t i, int32_t lo, float lse, char *out)
+{
+    constexpr int ES = DT == 0 ? 4 : 2, MOST = 256 / 64;
+    const int32_t lane = threadIdx.x & 63, kv_head = head / (a.heads / a.kv_heads);
+    const int64_t row0 = peer * a.T;
+    const char *q = a.q + ((row0 + i) * a.q_stride + int64_t(head) * a.depth) * ES;
+    float sum[MOST] = {};
+    for (int32_t j0 = lo; j0 <= i; j0 += 64) {
+        const int32_t j = j0 + lane, f = j <= i ? a.first[row0 + j] : -1;
+        float w = 0.f;
+        if (f >= 0 && f <= j) {
+            const char *k = a.k + ((row0 + j) * a.k_stride + int64_t(kv_head) * a.depth) * ES;
+            float s = 0.f;
+            for (int32_t d = 0; d < a.depth; ++d) s = fmaf(load_one<DT>(q + d * ES), load_one<DT>(k + d * ES), s);
+            w = __builtin_amdgcn_exp2f(fmaf(s, a.scale, -lse));
+        }
+        for (uint64_t left = __ballot(w != 0.f); left; left &= left - 1) {
+            const int32_t n = __builtin_ctzll(left);
+            const float one = __shfl(w, n, 64);
+            const char *v = a.v + ((row0 + j0 + n) * a.v_stride + int64_t(kv_head) * a.depth) * ES;
+#pragma unroll
+            for (int t = 0; t < MOST; ++t)
+                if (lane + 64 * t < a.depth) sum[t] = fmaf(one, load_one<DT>(v + (lane + 64 * t) * ES), sum[t]);
+        }
+    }
+#pragma unroll
+    for (int t = 0; t < MOST; ++t)
+        if (lane + 64 * t < a.depth) store_one<DT>(out + (lane + 64 * t) * ES, sum[t]);
+}
+
+// ROWS keys a tile, JOINT blocks of 32 keys at a time, SIMD waves a SIMD, DIRECT: rows go straight into LDS.
+template <Form F, int DP, int ROWS, int JOINT, int SIMD, bool DIRECT>
+__global__ __launch_bounds__(kThreads, SIMD)
 void attention_kernel(AttentionArgs a)
 {
-    constexpr int ES = Num<DT>::ES, ROWS = tile_rows<DT, DP>(), N = ROWS / 32, LP = row_elems_of(DP), BLOCKS = DP / 32;
-    typedef typename Num<DT>::lds_t lds_t;
-    __shared__ __attribute__((aligned(16))) lds_t keys[2][ROWS * LP], values[2][ROWS * LP];
+    constexpr int ES = Num<F>::ES, DT = Num<F>::DT, BLOCKS = DP / 32, N = JOINT, ELEMS = tile_elems<F, DP>(ROWS);
+    constexpr uint64_t ALL = ROWS == 64 ? ~uint64_t(0) : 0xffffffffull;
+    typedef Direct<(DIRECT ? DP : 128), (DIRECT ? ROWS : 64), kThreads> Straight;
+    typedef typename Num<F>::lds_t lds_t;
+    // (four variables: an access to one does not wait for what is on its way into another)
+    __shared__ __attribute__((aligned(16))) lds_t k_even[ELEMS], k_odd[ELEMS], v_even[ELEMS], v_odd[ELEMS];
     __shared__ int32_t ends[2][kWaves];
-    __shared__ unsigned long long odd_rows[2];
 
-    uint32_t b = die_run(blockIdx.x, gridDim.x);
-    const uint32_t tile = a.tiles - 1 - b % a.tiles;                   // (the last ones, which see the most keys, first)
-    b /= a.tiles;
-    const int32_t head = b % a.heads, kv_head = head / (a.heads / a.kv_heads), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t peer = b / a.heads, row0 = peer * a.T;
-    const int32_t T = static_cast<int32_t>(a.T), i = static_cast<int32_t>(tile * (32 * kWaves) + wave * 32 + (lane & 31));
+    const int32_t group = a.heads / a.kv_heads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
+    const Place p = place_of(blockIdx.x, a.N, a.kv_heads, group);
+    const uint32_t tile = a.tiles - 1 - p.tile;                        // (the last ones see the most keys)
+    const int32_t kv_head = p.kv_head, head = kv_head * group + p.member;
+    const int64_t peer = p.peer, row0 = peer * a.T;
+    const int32_t T = static_cast<int32_t>(a.T), wave_first = static_cast<int32_t>(tile * kQueries) + wave * 32, i = wave_first + (lane & 31);
     const int32_t *first = a.first + row0;
     auto begin_of = [&](int32_t j) {                                   // -1: no token
         const int32_t f = j < T ? first[j] : -1;
         return f <= j ? f : -1;
     };
-    const int32_t mine = begin_of(i);
-    const bool there = mine >= 0;
-    const int32_t lo = there ? mine : INT32_MAX, hi = there ? i : -1;
-    const int32_t wave_lo = wave_min(lo), wave_hi = wave_max(hi), all_from = wave_max(there ? mine : -1), all_to = wave_min(there ? i : INT32_MAX);
+    const int32_t lo = begin_of(i);
+    const bool there = lo >= 0;
+    Queries<F, DP> x;
+    x.q.load(a.q + ((row0 + i) * a.q_stride + int64_t(head) * a.depth) * ES, there, a.depth);
+    // keys wave_lo .. wave_hi are seen by some query, all_from .. all_to by all of them that hold a token
+    const int32_t wave_lo = __builtin_amdgcn_readfirstlane(wave_min(there ? lo : INT32_MAX)), wave_hi = __builtin_amdgcn_readfirstlane(wave_max(there ? i : -1));
+    const int32_t all_from = __builtin_amdgcn_readfirstlane(wave_max(there ? lo : -1)), all_to = __builtin_amdgcn_readfirstlane(wave_min(there ? i : INT32_MAX));
     if (lane == 0) {
         ends[0][wave] = wave_lo;
         ends[1][wave] = wave_hi;
@@ -146,98 +178,114 @@ void attention_kernel(AttentionArgs a)
         from = ends[0][w] < from ? ends[0][w] : from;
         to = ends[1][w] > to ? ends[1][w] : to;
     }
+    from = __builtin_amdgcn_readfirstlane(from);
+    to = __builtin_amdgcn_readfirstlane(to);
 
-    Queries<DT, DP> x;
-    x.q.load(a.q + ((row0 + i) * a.q_stride + int64_t(head) * a.depth) * ES, there, a.depth);
     const char *k_rows = a.k + (row0 * a.k_stride + int64_t(kv_head) * a.depth) * ES, *v_rows = a.v + (row0 * a.v_stride + int64_t(kv_head) * a.depth) * ES;
     const int64_t k_bytes = a.k_stride * ES, v_bytes = a.v_stride * ES;
-    auto live_of = [&](int32_t begin) { return __ballot(begin >= 0) & (ROWS == 64 ? ~uint64_t(0) : 0xffffffffull); };
+    auto begins_at = [&](int32_t at) { return at <= to ? begin_of(at + lane) : -1; };
+    auto live_of = [&](int32_t begin) { return __ballot(begin >= 0) & ALL; };
 
-    auto pass = [&](auto careful) {
-        constexpr bool CAREFUL = decltype(careful)::value;
-        x.clear();
-        if (to < from) return;
-        Staged<DT, DP, ROWS, kThreads> k_next, v_next;
-        uint64_t live = live_of(begin_of(from + lane)), live_next = 0;
-        int32_t begin_next = from + ROWS <= to ? begin_of(from + ROWS + lane) : -1;
-        int now = 0;
-        auto fill = [&](int into) {
-            if constexpr (CAREFUL) {
-                if (threadIdx.x == 0) odd_rows[into] = 0;
-                __syncthreads();
-                const uint64_t odd = v_next.clean(threadIdx.x);
-                if (odd) atomicOr(&odd_rows[into], static_cast<unsigned long long>(odd));
-            }
-            k_next.store(keys[into], threadIdx.x);
-            v_next.store(values[into], threadIdx.x);
+    x.clear();
+    if (from <= to) {
+        typename std::conditional<DIRECT, char, Staged<F, DP, ROWS, kThreads>>::type k_next, v_next;
+        auto request = [&](auto &next, const char *rows, int64_t bytes, int32_t at, uint64_t live, lds_t *into) __attribute__((always_inline)) {
+            if constexpr (DIRECT) Straight::request(rows + at * bytes, static_cast<uint32_t>(bytes), T - 1 - at, into);
+            else next.load(rows + at * bytes, bytes, live, a.depth, threadIdx.x);
         };
-        k_next.load(k_rows + from * k_bytes, k_bytes, live, a.depth, threadIdx.x);
-        v_next.load(v_rows + from * v_bytes, v_bytes, live, a.depth, threadIdx.x);
-        fill(0);
-        for (int32_t at = from; at <= to; at += ROWS, now ^= 1, live = live_next) {
+        auto put = [&](auto &next, lds_t *into) __attribute__((always_inline)) {
+            if constexpr (!DIRECT) next.store(into, threadIdx.x);
+        };
+        auto landed = [&](uint64_t v_live, lds_t *v_into) __attribute__((always_inline)) {      // (keys without a token get no weight, their values are zeros)
+            if constexpr (DIRECT) {
+                Straight::wait();
+                if (v_live != ALL) Straight::trim(v_live, v_into);
+            }
+        };
+        uint64_t live = live_of(begins_at(from)), live_next = 0;
+        int32_t begin_next = begins_at(from + ROWS), at = from;
+        request(k_next, k_rows, k_bytes, from, live, k_even);
+        request(v_next, v_rows, v_bytes, from, live, v_even);
+        put(k_next, k_even);
+        put(v_next, v_even);
+        landed(live, v_even);
+        // The tile that begins at `at`; the next one goes into the other two.  False: it was the last.
+        auto step = [&](const lds_t *keys, const lds_t *values, lds_t *k_into, lds_t *v_into) __attribute__((always_inline)) {
             __syncthreads();
             const bool more = at + ROWS <= to;
             if (more) {
                 live_next = live_of(begin_next);
-                k_next.load(k_rows + (at + ROWS) * k_bytes, k_bytes, live_next, a.depth, threadIdx.x);
-                v_next.load(v_rows + (at + ROWS) * v_bytes, v_bytes, live_next, a.depth, threadIdx.x);
-                begin_next = at + 2 * ROWS <= to ? begin_of(at + 2 * ROWS + lane) : -1;
+                request(k_next, k_rows, k_bytes, at + ROWS, live_next, k_into);
+                request(v_next, v_rows, v_bytes, at + ROWS, live_next, v_into);
+                begin_next = begins_at(at + 2 * ROWS);
+                if constexpr (DIRECT) __builtin_amdgcn_sched_barrier(0);
             }
-            if (at <= wave_hi && at + ROWS > wave_lo) {
-                f32x16 s[N];
 #pragma unroll
-                for (int n = 0; n < N; ++n) s[n] = rows_times<DT, DP>(keys[now], 32 * n, x.q);
-                const bool whole = at >= all_from && at + ROWS - 1 <= all_to && live == (ROWS == 64 ? ~uint64_t(0) : 0xffffffffull);
-                if (!whole) {
-                    const int half = lane >> 5;
-                    const int32_t low = there ? lo - at - 4 * half : INT32_MAX / 2;
-                    const uint32_t span = there ? static_cast<uint32_t>(hi - lo) : 0u;
-                    const uint64_t seen = live >> (4 * half);
+            for (int n0 = 0; n0 < ROWS / 32; n0 += N) {
+                const int32_t j0 = at + 32 * n0;
+                if (j0 > wave_hi || j0 + 32 * N <= wave_lo) continue;
+                f32x16 s[N];
+                x.template score<ROWS>(keys + 32 * n0 * row_elems_of(DP), s);
+                const uint64_t seen = live >> (32 * n0), all = N == 2 ? ~uint64_t(0) : 0xffffffffull;
+                if (j0 < all_from || j0 + 32 * N - 1 > all_to || (seen & all) != all) {
+                    const int32_t low = there ? lo - j0 - 4 * half : INT32_MAX / 2;
+                    const uint32_t span = there ? static_cast<uint32_t>(i - lo) : 0u;
+                    const uint64_t mine = seen >> (4 * half);
 #pragma unroll
                     for (int n = 0; n < N; ++n)
 #pragma unroll
                         for (int r = 0; r < 16; ++r) {
                             const int32_t j = 32 * n + 8 * (r >> 2) + (r & 3);
-                            const bool sees = static_cast<uint32_t>(j - low) <= span && (seen >> j & 1) != 0;
-                            s[n][r] = sees ? s[n][r] : -INFINITY;
+                            s[n][r] = static_cast<uint32_t>(j - low) <= span && (mine >> j & 1) != 0 ? s[n][r] : -INFINITY;
                         }
                 }
-                x.weigh(s, a.scale);
-#pragma unroll
-                for (int n = 0; n < N; ++n) {
-                    const Weights<DT> w(s[n]);
-#pragma unroll
-                    for (int m = 0; m < BLOCKS; ++m) x.sum[m] = columns_times<DT, LP>(values[now], 32 * n, 32 * m, w, x.sum[m]);
-                }
-                if constexpr (CAREFUL) x.add_odd(s, odd_rows[now], v_rows + at * v_bytes, v_bytes, a.depth);
+                x.rescale(x.largest(s), a.scale);
+                x.template take<ROWS>(s, a.scale, values + 32 * n0 * row_elems_of(DP));
             }
-            if (more) fill(now ^ 1);
+            if (more) {
+                put(k_next, k_into);
+                put(v_next, v_into);
+                landed(live_next, v_into);
+            }
+            live = live_next;
+            at += ROWS;
+            return more;
+        };
+        for (;;) {
+            if (!step(k_even, v_even, k_odd, v_odd)) break;
+            if (!step(k_odd, v_odd, k_even, v_even)) break;
         }
-    };
-    pass(std::false_type{});
-    if (__syncthreads_or(there && !x.finite())) pass(std::true_type{});
+    }
 
-    if (i >= T) return;
-    const float total = halves_sum(x.total);
+    const float total = halves_sum(x.total), share = 1.f / total, lse = x.top + __builtin_amdgcn_logf(total);
     char *out = a.out + ((row0 + i) * a.out_stride + int64_t(head) * a.depth) * ES;
-    if (lane < 32 && a.lse) a.lse[(peer * a.heads + head) * a.T + i] = there ? (x.top + __builtin_amdgcn_logf(total)) * kLn2 : 0.f;
-    const float share = 1.f / total;
+    // weights that are numbers, but sums that are not
+    const uint64_t halves = __ballot(there && fabsf(lse) < INFINITY && !x.finite());
+    const uint32_t spoilt = static_cast<uint32_t>(halves) | static_cast<uint32_t>(halves >> 32);
+    if (i < T) {
+        if (half == 0 && a.lse) a.lse[(peer * a.heads + head) * a.T + i] = there ? lse * kLn2 : 0.f;
+        if ((spoilt >> (lane & 31) & 1) == 0)
 #pragma unroll
-    for (int m = 0; m < BLOCKS; ++m) {
-        if (!there) x.sum[m] = f32x16{};
-        store_column<DT>(out, 32 * m, a.depth, x.sum[m], there ? share : 0.f);
+            for (int m = 0; m < BLOCKS; ++m) {
+                if (!there) x.sum[m] = f32x16{};
+                store_column<DT>(out, 32 * m, a.depth, x.sum[m], there ? share : 0.f);
+            }
+    }
+    for (uint32_t left = spoilt; left; left &= left - 1) {
+        const int32_t n = __builtin_ctz(left), row = wave_first + n;
+        attend_alone<DT>(a, peer, head, row, __shfl(lo, n, 64), __shfl(lse, n, 64), a.out + ((row0 + row) * a.out_stride + int64_t(head) * a.depth) * ES);
     }
 }
 
 // Tokens' queries against a span of keys.  A block has one sequence, one head of keys and a share of the span; its waves take tiles of 32 keys in turn,
 // each its own in LDS, for the same 32 columns: the queries of the heads that share the keys, of the new tokens one after the other.
-template <int DT, int DP, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, DT == 0 && DP > 128 ? 1 : 2)
+template <Form F, int DP, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, F != kBf16 && DP > 64 ? 1 : 2)
 void cached_kernel(CachedArgs a, float *__restrict__ partials)
 {
-    constexpr int ES = Num<DT>::ES, LP = row_elems_of(DP), BLOCKS = DP / 32;
-    typedef typename Num<DT>::lds_t lds_t;
-    __shared__ __attribute__((aligned(16))) lds_t all[WAVES][2 * 32 * LP];
+    constexpr int ES = Num<F>::ES, DT = Num<F>::DT, BLOCKS = DP / 32, ELEMS = tile_elems<F, DP>(32);
+    typedef typename Num<F>::lds_t lds_t;
+    __shared__ __attribute__((aligned(16))) lds_t all[WAVES][2 * ELEMS];
     __shared__ float tops[WAVES][32], totals[WAVES][32];
 
     uint32_t b = die_run(blockIdx.x, gridDim.x);
@@ -261,17 +309,17 @@ void cached_kernel(CachedArgs a, float *__restrict__ partials)
     const int32_t sees = there ? count - (a.fresh - 1 - token) : 0;                       // how many of them this query does
     const int32_t all_see = count - (a.fresh - 1);
 
-    Queries<DT, DP> x;
+    Queries<F, DP> x;
     const int64_t row = (peer * a.seqs + seq) * a.fresh + token;
     x.q.load(a.q + (row * a.q_stride + int64_t(head) * a.depth) * ES, there, a.depth);
     x.clear();
     const char *k_rows = a.k + ((peer * a.n_keys + begin) * a.k_stride + int64_t(kv_head) * a.depth) * ES;
     const char *v_rows = a.v + ((peer * a.n_keys + begin) * a.v_stride + int64_t(kv_head) * a.depth) * ES;
     const int64_t k_bytes = a.k_stride * ES, v_bytes = a.v_stride * ES;
-    lds_t *keys = all[wave], *values = keys + 32 * LP;
+    lds_t *keys = all[wave], *values = keys + ELEMS;
     auto live_of = [&](int32_t at) { return at + 32 <= to ? 0xffffffffull : (uint64_t(1) << (to - at)) - 1; };
     int32_t at = split * each + 32 * wave;
-    Staged<DT, DP, 32, 64> k_next, v_next;
+    Staged<F, DP, 32, 64> k_next, v_next;
     if (at < to) {
         k_next.load(k_rows + at * k_bytes, k_bytes, live_of(at), a.depth, lane);
         v_next.load(v_rows + at * v_bytes, v_bytes, live_of(at), a.depth, lane);
@@ -290,16 +338,15 @@ void cached_kernel(CachedArgs a, float *__restrict__ partials)
             k_next.load(k_rows + next * k_bytes, k_bytes, live_of(next), a.depth, lane);
             v_next.load(v_rows + next * v_bytes, v_bytes, live_of(next), a.depth, lane);
         }
-        f32x16 s[1] = {rows_times<DT, DP>(keys, 0, x.q)};
+        f32x16 s[1];
+        x.template score<32>(keys, s);
         if (at + 32 > to || at + 32 > all_see) {
             const int32_t seen = (sees < to ? sees : to) - at - 4 * half;
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[0][r] = 8 * (r >> 2) + (r & 3) < seen ? s[0][r] : -INFINITY;
         }
-        x.weigh(s, a.scale);
-        const Weights<DT> w(s[0]);
-#pragma unroll
-        for (int m = 0; m < BLOCKS; ++m) x.sum[m] = columns_times<DT, LP>(values, 0, 32 * m, w, x.sum[m]);
+        x.rescale(x.largest(s), a.scale);
+        x.template take<32>(s, a.scale, values);
     }
 
     // the waves' sums, in order
@@ -358,7 +405,7 @@ void cached_kernel(CachedArgs a, float *__restrict__ partials)
 template <int DT>
 __global__ __launch_bounds__(kThreads) void cached_join_kernel(CachedArgs a, const float *__restrict__ partials, int64_t rows)
 {
-    constexpr int ES = Num<DT>::ES;
+    constexpr int ES = DT == 0 ? 4 : 2;
     const int64_t n = int64_t(blockIdx.x) * kWaves + (threadIdx.x >> 6);
     if (n >= rows * a.heads) return;
     const int64_t row = n / a.heads, head = n % a.heads;
@@ -380,20 +427,13 @@ __global__ __launch_bounds__(kThreads) void cached_join_kernel(CachedArgs a, con
     }
 }
 
-template <typename Go> hipError_t by_depth(int dtype, int depth, Go go)
-{
-    using std::integral_constant;
-    auto of_type = [&](auto dt) {
-        if (depth <= 32) return go(dt, integral_constant<int, 32>{});
-        if (depth <= 64) return go(dt, integral_constant<int, 64>{});
-        if (depth <= 128) return go(dt, integral_constant<int, 128>{});
-        return go(dt, integral_constant<int, 256>{});
-    };
-    return dtype == 0 ? of_type(integral_constant<int, 0>{}) : of_type(integral_constant<int, 1>{});
-}
+int64_t attention_blocks(const AttentionArgs &a) { return a.N * a.heads * ((a.T + kQueries - 1) / kQueries); }
 
-int64_t attention_blocks(const AttentionArgs &a) { return a.N * a.heads * ((a.T + 32 * kWaves - 1) / (32 * kWaves)); }
-
+#ifndef P_ROWS
+#define P_ROWS 64
+#define P_SIMD 2
+#define P_J 2
+#endif
 }  // namespace
 
 bool attention_fits(const AttentionArgs &a) { return launchable(attention_blocks(a), kThreads); }
@@ -401,11 +441,17 @@ bool attention_fits(const AttentionArgs &a) { return launchable(attention_blocks
 hipError_t launch_attention(AttentionArgs a, int dtype, hipStream_t stream)
 {
     if (a.T == 0) return hipSuccess;
-    a.tiles = static_cast<uint32_t>((a.T + 32 * kWaves - 1) / (32 * kWaves));
     a.scale *= kLog2e;
-    return by_depth(dtype, a.depth, [&](auto dt, auto dp) {
-        constexpr int DT = decltype(dt)::value, DP = decltype(dp)::value;
-        attention_kernel<DT, DP, (DP > 128 ? 1 : 2)><<<static_cast<uint32_t>(attention_blocks(a)), kThreads, 0, stream>>>(a);
+    a.tiles = static_cast<uint32_t>((a.T + kQueries - 1) / kQueries);
+    const uint32_t blocks = static_cast<uint32_t>(attention_blocks(a));
+    return by_depth(dtype, a.depth, [&](auto form, auto dp) {
+        constexpr Form F = decltype(form)::value;
+        constexpr int DP = decltype(dp)::value;
+        if constexpr (F != kBf16) attention_kernel<F, DP, 32, 1, (DP > 64 ? 1 : 2), false><<<blocks, kThreads, 0, stream>>>(a);
+        else if constexpr (DP > 128) attention_kernel<F, DP, 32, 1, 1, false><<<blocks, kThreads, 0, stream>>>(a);
+        else if (a.depth == DP && direct_rows(a.k, a.k_stride) && direct_rows(a.v, a.v_stride))
+            attention_kernel<F, DP, (DP <= 32 ? 64 : P_ROWS), P_J, P_SIMD, true><<<blocks, kThreads, 0, stream>>>(a);
+        else attention_kernel<F, DP, 64, 1, 2, false><<<blocks, kThreads, 0, stream>>>(a);
         return hipGetLastError();
     });
 }
@@ -432,10 +478,10 @@ hipError_t launch_cached(CachedArgs a, int dtype, const CachedPlan &p, void *wor
     a.splits = p.splits;
     a.scale *= kLog2e;
     float *partials = static_cast<float *>(work);
-    const hipError_t e = by_depth(dtype, a.depth, [&](auto dt, auto dp) {
-        constexpr int DT = decltype(dt)::value, DP = decltype(dp)::value;
-        constexpr int WAVES = cached_waves<DT, DP>();
-        cached_kernel<DT, DP, WAVES><<<static_cast<uint32_t>(a.N * a.seqs * a.kv_heads * p.col_tiles * p.splits), 64 * WAVES, 0, stream>>>(a, partials);
+    const hipError_t e = by_depth(dtype, a.depth, [&](auto form, auto dp) {
+        constexpr Form F = decltype(form)::value;
+        constexpr int DP = decltype(dp)::value, WAVES = cached_waves<F, DP>();
+        cached_kernel<F, DP, WAVES><<<static_cast<uint32_t>(a.N * a.seqs * a.kv_heads * p.col_tiles * p.splits), 64 * WAVES, 0, stream>>>(a, partials);
         return hipGetLastError();
     });
     if (e != hipSuccess || p.splits == 1) return e;

@@ -16,7 +16,7 @@
 namespace moshpit {
 namespace {
 
-constexpr int kThreads = 256, kWaves = 4;
+constexpr int kThreads = 256, kWaves = 4, kColumns = 32 * kWaves;     // columns of a block: keys or queries
 constexpr int kStat = 32;                                // queries of a tile whose range of `first` is kept
 
 struct Range {
@@ -27,7 +27,7 @@ struct Range {
 template <int DT>
 __global__ __launch_bounds__(kThreads) void delta_kernel(AttentionGradArgs a, float *__restrict__ delta, Range *__restrict__ ranges, int64_t delta_blocks)
 {
-    constexpr int ES = Num<DT>::ES;
+    constexpr int ES = DT == 0 ? 4 : 2;
     const int lane = threadIdx.x & 15;
     if (blockIdx.x >= delta_blocks) {
         const int64_t stats = (a.T + kStat - 1) / kStat, n = (blockIdx.x - delta_blocks) * (kThreads / 16) + threadIdx.x / 16;
@@ -74,35 +74,33 @@ __global__ __launch_bounds__(kThreads) void delta_kernel(AttentionGradArgs a, fl
 }
 
 // How a launch of the kernel for keys is cut: `parts` of the queries and heads that a block of keys meets, sums of a part apart, and
-// `slices` of DA depths of dk and dv.
+// `slices` of sum_depths() depths of dk and dv.
 struct KeysPlan {
     uint32_t tiles;
     int32_t parts;
 };
 
 // Depths of dk and dv that a block's sums have: all up to 128, as registers allow.
-template <int DT, int DP> constexpr int sum_depths() { return DP <= 128 ? DP : DT == 0 ? 64 : 128; }
+template <Form F, int DP> constexpr int sum_depths() { return DP <= 128 ? DP : F == kF32 ? 64 : DP == 192 ? 96 : 128; }
 
-template <int DT, int DP>
-__global__ __launch_bounds__(kThreads, DP > 128 || (DT == 0 && DP > 64) ? 1 : 2)
+// SIMD waves a SIMD; ASIDE: the values stay in LDS (registers do not hold them beside the keys and the sums); DIRECT: rows go straight into LDS.
+template <Form F, int DP, int SIMD, bool ASIDE, bool DIRECT>
+__global__ __launch_bounds__(kThreads, SIMD)
 void keys_grad_kernel(AttentionGradArgs a, KeysPlan plan, const float *__restrict__ delta, const Range *__restrict__ ranges, float *__restrict__ partials)
 {
-    constexpr int ES = Num<DT>::ES, ROWS = kStat, LP = row_elems_of(DP), DA = sum_depths<DT, DP>(), BLOCKS = DA / 32, SLICES = DP / DA;
-    typedef typename Num<DT>::lds_t lds_t;
-    __shared__ __attribute__((aligned(16))) lds_t queries[2][ROWS * LP], douts[2][ROWS * LP];
+    constexpr int ES = Num<F>::ES, DT = Num<F>::DT, ROWS = kStat, DA = sum_depths<F, DP>(), BLOCKS = DA / 32, SLICES = DP / DA, ELEMS = tile_elems<F, DP>(ROWS);
+    typedef Direct<(DIRECT ? DP : 128), ROWS, kThreads> Straight;
+    typedef typename Num<F>::lds_t lds_t;
+    __shared__ __attribute__((aligned(16))) lds_t q_even[ELEMS], q_odd[ELEMS], d_even[ELEMS], d_odd[ELEMS], aside[ASIDE ? tile_elems<F, DP>(kColumns) : 8];
     __shared__ __attribute__((aligned(16))) float lses[2][ROWS], deltas[2][ROWS];
     __shared__ __attribute__((aligned(16))) int32_t firsts[2][ROWS];
 
-    uint32_t b = die_run(blockIdx.x, gridDim.x);
-    const int32_t slice = b % SLICES;
-    b /= SLICES;
-    const uint32_t tile = b % plan.tiles;                              // (the first ones, which the most queries see, first)
-    b /= plan.tiles;
-    const int32_t part = b % plan.parts;
-    b /= plan.parts;
-    const int32_t kv_head = b % a.kv_heads, group = a.heads / a.kv_heads, lane = threadIdx.x & 63, half = lane >> 5, wave = threadIdx.x >> 6;
-    const int64_t peer = b / a.kv_heads, row0 = peer * a.T;
-    const int32_t T = static_cast<int32_t>(a.T), begin = static_cast<int32_t>(tile * (32 * kWaves)), wave_begin = begin + 32 * wave, j = wave_begin + (lane & 31);
+    const int32_t group = a.heads / a.kv_heads, lane = threadIdx.x & 63, half = lane >> 5, wave = threadIdx.x >> 6;
+    const Place place = place_of(blockIdx.x, a.N, a.kv_heads, plan.parts * SLICES);    // (the first tiles are seen by the most queries)
+    const int32_t part = place.member / SLICES, slice = place.member % SLICES, kv_head = place.kv_head;
+    const int64_t peer = place.peer, row0 = peer * a.T;
+    const int32_t T = static_cast<int32_t>(a.T), begin = static_cast<int32_t>(place.tile * kColumns), j = begin + 32 * wave + (lane & 31);
+    const int32_t wave_begin = __builtin_amdgcn_readfirstlane(begin + 32 * wave);
     const int32_t *first = a.first + row0;
     auto begin_of = [&](int32_t i) {
         const int32_t f = i < T ? first[i] : -1;
@@ -110,15 +108,19 @@ void keys_grad_kernel(AttentionGradArgs a, KeysPlan plan, const float *__restric
     };
     const bool there = begin_of(j) >= 0;
 
-    Held<DT, DP> k, v;
+    Held<F, DP> k, v;
     k.load(a.k + ((row0 + j) * a.k_stride + int64_t(kv_head) * a.depth) * ES, there, a.depth);
     v.load(a.v + ((row0 + j) * a.v_stride + int64_t(kv_head) * a.depth) * ES, there, a.depth);
+    if constexpr (ASIDE) Aside<F, DP>::put(v, aside + 32 * wave * row_elems_of(DP));
     f32x16 dk[BLOCKS] = {}, dv[BLOCKS] = {};
 
     // The tiles of queries that see one of the block's keys, each for the heads of the group: numbers part, part + parts, ... of them.
-    const int32_t last = begin + 32 * kWaves - 1, stats = (T + ROWS - 1) / ROWS;
+    struct Item {
+        int32_t tile, member, lo, hi;
+    };
+    const int32_t last = begin + kColumns - 1, stats = (T + ROWS - 1) / ROWS;
     const Range *range = ranges + peer * stats;
-    int32_t base = begin / ROWS, turn = 0, at = -1, head = 0;          // the tiles looked at from, the item's tile and head
+    int32_t base = begin / ROWS, turn = 0;                             // the tiles looked at from
     uint64_t left = 0;
     Range r{};
     auto look = [&] {
@@ -127,10 +129,11 @@ void keys_grad_kernel(AttentionGradArgs a, KeysPlan plan, const float *__restric
         left = __ballot(r.lo <= last);
     };
     look();
+    Item item{-1, 0, 0, 0};
     auto advance = [&]() -> bool {                                     // to the next item of this part; false: there is none
         for (;;) {
-            if (at >= 0 && ++head < group) {
-                if (turn++ % plan.parts == part) return true;
+            if (item.tile >= 0 && ++item.member < group) {
+                if (plan.parts == 1 || turn++ % plan.parts == part) return true;
                 continue;
             }
             while (left == 0) {
@@ -138,49 +141,60 @@ void keys_grad_kernel(AttentionGradArgs a, KeysPlan plan, const float *__restric
                 if (base >= stats) return false;
                 look();
             }
-            at = base + __builtin_ctzll(left);
+            const int32_t n = __builtin_ctzll(left);
             left &= left - 1;
-            head = -1;
+            item = Item{base + n, -1, __builtin_amdgcn_readlane(r.lo, n), __builtin_amdgcn_readlane(r.hi, n)};
         }
     };
-    Staged<DT, DP, ROWS, kThreads> q_next, d_next;
+    typename std::conditional<DIRECT, char, Staged<F, DP, ROWS, kThreads>>::type q_next, d_next;
     float lse_next = 0.f, delta_next = 0.f;
     int32_t first_next = -1;
-    auto request = [&] {
-        const int32_t i = at * ROWS + (threadIdx.x & (ROWS - 1)), h = kv_head * group + head;
+    uint64_t live_next = 0;
+    auto request = [&](lds_t *q_into, lds_t *d_into) __attribute__((always_inline)) {
+        const int32_t i0 = item.tile * ROWS, i = i0 + (threadIdx.x & (ROWS - 1)), h = kv_head * group + item.member;
+        const char *q = a.q + ((row0 + i0) * a.q_stride + int64_t(h) * a.depth) * ES, *d = a.dout + ((row0 + i0) * a.dout_stride + int64_t(h) * a.depth) * ES;
         first_next = begin_of(i);
-        const uint64_t live = __ballot(first_next >= 0) & 0xffffffffull;
-        q_next.load(a.q + ((row0 + at * ROWS) * a.q_stride + int64_t(h) * a.depth) * ES, a.q_stride * ES, live, a.depth, threadIdx.x);
-        d_next.load(a.dout + ((row0 + at * ROWS) * a.dout_stride + int64_t(h) * a.depth) * ES, a.dout_stride * ES, live, a.depth, threadIdx.x);
-        const int64_t n = (peer * a.heads + h) * a.T + i;
-        lse_next = first_next >= 0 ? a.lse[n] * kLog2e : INFINITY;    // (a query without a token: weights of 0)
-        delta_next = first_next >= 0 ? delta[n] : 0.f;
+        const int64_t n = (peer * a.heads + h) * a.T + (i < T ? i : T - 1);
+        lse_next = a.lse[n] * kLog2e;
+        delta_next = delta[n];
+        if constexpr (DIRECT) {
+            Straight::request(q, static_cast<uint32_t>(a.q_stride * ES), T - 1 - i0, q_into);
+            Straight::request(d, static_cast<uint32_t>(a.dout_stride * ES), T - 1 - i0, d_into);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        live_next = __ballot(first_next >= 0) & 0xffffffffull;
+        if constexpr (!DIRECT) {
+            q_next.load(q, a.q_stride * ES, live_next, a.depth, threadIdx.x);
+            d_next.load(d, a.dout_stride * ES, live_next, a.depth, threadIdx.x);
+        }
     };
-    auto fill = [&](int into) {
-        q_next.store(queries[into], threadIdx.x);
-        d_next.store(douts[into], threadIdx.x);
+    auto fill = [&](lds_t *q_into, lds_t *d_into, int into) __attribute__((always_inline)) {
+        if constexpr (DIRECT) {
+            Straight::wait();
+            if (live_next != 0xffffffffull) {
+                Straight::trim(live_next, q_into);
+                Straight::trim(live_next, d_into);
+            }
+        } else {
+            q_next.store(q_into, threadIdx.x);
+            d_next.store(d_into, threadIdx.x);
+        }
         if (threadIdx.x < ROWS) {
-            lses[into][threadIdx.x] = lse_next;
-            deltas[into][threadIdx.x] = delta_next;
+            lses[into][threadIdx.x] = first_next >= 0 ? lse_next : INFINITY;       // (a query without a token: weights of 0)
+            deltas[into][threadIdx.x] = first_next >= 0 ? delta_next : 0.f;
             firsts[into][threadIdx.x] = first_next;
         }
     };
-    int now = 0;
-    bool more = advance();
-    if (more) {
-        request();
-        fill(0);
-    }
-    while (more) {
-        const int32_t i0 = at * ROWS;
-        const int32_t lo = __shfl(r.lo, at - base, 64), hi = __shfl(r.hi, at - base, 64);
-        more = advance();
+    auto step = [&](const lds_t *queries, const lds_t *douts, int now, lds_t *q_into, lds_t *d_into) __attribute__((always_inline)) {
+        const Item it = item;
+        const bool more = advance();
         __syncthreads();
-        if (more) request();
-        if (lo <= wave_begin + 31 && i0 + ROWS > wave_begin) {
-            f32x16 p = rows_times<DT, DP>(queries[now], 0, k);
-            f32x16 ds = rows_times<DT, DP>(douts[now], 0, v);
-            const bool whole = i0 >= wave_begin + 31 && hi <= wave_begin;
+        if (more) request(q_into, d_into);
+        const int32_t i0 = it.tile * ROWS;
+        if (it.lo <= wave_begin + 31 && i0 + ROWS > wave_begin) {
+            f32x16 p = rows_times<F, DP, ROWS>(queries, 0, k), ds;
+            if constexpr (ASIDE) ds = rows_times<F, DP, ROWS>(douts, 0, Aside<F, DP>{aside + 32 * wave * row_elems_of(DP)});
+            else ds = rows_times<F, DP, ROWS>(douts, 0, v);
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
                 const f32x4 l = *reinterpret_cast<const f32x4 *>(&lses[now][8 * g + 4 * half]), d = *reinterpret_cast<const f32x4 *>(&deltas[now][8 * g + 4 * half]);
@@ -190,7 +204,7 @@ void keys_grad_kernel(AttentionGradArgs a, KeysPlan plan, const float *__restric
                     ds[4 * g + e] = p[4 * g + e] * (ds[4 * g + e] - d[e]);
                 }
             }
-            if (!whole) {
+            if (i0 < wave_begin + 31 || it.hi > wave_begin) {
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
                     const u32x4 f = *reinterpret_cast<const u32x4 *>(&firsts[now][8 * g + 4 * half]);
@@ -203,34 +217,39 @@ void keys_grad_kernel(AttentionGradArgs a, KeysPlan plan, const float *__restric
                     }
                 }
             }
-            const Weights<DT> wp(p), ws(ds);
+            Weights<F> w;
+            w.take(p);
 #pragma unroll
-            for (int m = 0; m < BLOCKS; ++m) {
-                dv[m] = columns_times<DT, LP>(douts[now], 0, slice * DA + 32 * m, wp, dv[m]);
-                dk[m] = columns_times<DT, LP>(queries[now], 0, slice * DA + 32 * m, ws, dk[m]);
-            }
+            for (int m = 0; m < BLOCKS; ++m) columns_times<F, DP, ROWS>(douts, 0, slice * DA + 32 * m, w, dv[m]);
+            w.take(ds);
+#pragma unroll
+            for (int m = 0; m < BLOCKS; ++m) columns_times<F, DP, ROWS>(queries, 0, slice * DA + 32 * m, w, dk[m]);
         }
-        now ^= 1;
-        if (more) fill(now);
+        if (more) fill(q_into, d_into, now ^ 1);
+        return more;
+    };
+    if (advance()) {
+        request(q_even, d_even);
+        fill(q_even, d_even, 0);
+        for (;;) {
+            if (!step(q_even, d_even, 0, q_odd, d_odd)) break;
+            if (!step(q_odd, d_odd, 1, q_even, d_even)) break;
+        }
     }
     if (j >= T) return;
-    const float factor = a.scale * kLn2;                               // (a.scale: times log2 e)
+    const float factor = there ? a.scale * kLn2 : 0.f;                 // (a.scale: times log2 e)
     const int64_t width = int64_t(a.kv_heads) * a.depth, column = int64_t(kv_head) * a.depth;
-    if (!there)
 #pragma unroll
-        for (int m = 0; m < BLOCKS; ++m) dk[m] = dv[m] = f32x16{};
-    if (plan.parts == 1) {
-#pragma unroll
-        for (int m = 0; m < BLOCKS; ++m) {
-            store_column<DT>(a.dk + ((row0 + j) * a.dk_stride + column) * ES, slice * DA + 32 * m, a.depth, dk[m], factor);
-            store_column<DT>(a.dv + ((row0 + j) * a.dv_stride + column) * ES, slice * DA + 32 * m, a.depth, dv[m], 1.f);
-        }
-    } else {
-        char *to = reinterpret_cast<char *>(partials + ((int64_t(part) * a.N * a.T + row0 + j) * 2 * width + column));
-#pragma unroll
-        for (int m = 0; m < BLOCKS; ++m) {
-            store_column<0>(to, slice * DA + 32 * m, a.depth, dk[m], factor);
-            store_column<0>(to + width * 4, slice * DA + 32 * m, a.depth, dv[m], 1.f);
+    for (int m = 0; m < BLOCKS; ++m) {
+        if (!there) dk[m] = dv[m] = f32x16{};
+        const int at = slice * DA + 32 * m;
+        if (plan.parts == 1) {
+            store_column<DT>(a.dk + ((row0 + j) * a.dk_stride + column) * ES, at, a.depth, dk[m], factor);
+            store_column<DT>(a.dv + ((row0 + j) * a.dv_stride + column) * ES, at, a.depth, dv[m], 1.f);
+        } else {
+            char *to = reinterpret_cast<char *>(partials + ((int64_t(part) * a.N * a.T + row0 + j) * 2 * width + column));
+            store_column<0>(to, at, a.depth, dk[m], factor);
+            store_column<0>(to + width * 4, at, a.depth, dv[m], 1.f);
         }
     }
 }
@@ -239,7 +258,7 @@ void keys_grad_kernel(AttentionGradArgs a, KeysPlan plan, const float *__restric
 template <int DT>
 __global__ __launch_bounds__(kThreads) void keys_join_kernel(AttentionGradArgs a, int32_t parts, const float *__restrict__ partials)
 {
-    constexpr int ES = Num<DT>::ES;
+    constexpr int ES = DT == 0 ? 4 : 2;
     const int64_t width = int64_t(a.kv_heads) * a.depth, all = a.N * a.T * 2 * width;
     for (int64_t n = int64_t(blockIdx.x) * kThreads + threadIdx.x; n < all; n += int64_t(gridDim.x) * kThreads) {
         float sum = 0.f;
@@ -256,30 +275,33 @@ __global__ __launch_bounds__(kThreads) void keys_join_kernel(AttentionGradArgs a
     }
 }
 
-template <int DT, int DP>
-__global__ __launch_bounds__(kThreads, DP > 128 || (DT == 0 && DP > 64) ? 1 : 2)
+// ROWS keys a tile; SIMD, DIRECT as above.
+template <Form F, int DP, int ROWS, int SIMD, bool DIRECT>
+__global__ __launch_bounds__(kThreads, SIMD)
 void queries_grad_kernel(AttentionGradArgs a, uint32_t tiles, const float *__restrict__ delta)
 {
-    constexpr int ES = Num<DT>::ES, ROWS = 32, LP = row_elems_of(DP), BLOCKS = DP / 32;
-    typedef typename Num<DT>::lds_t lds_t;
-    __shared__ __attribute__((aligned(16))) lds_t keys[2][ROWS * LP], values[2][ROWS * LP];
+    constexpr int ES = Num<F>::ES, DT = Num<F>::DT, BLOCKS = DP / 32, ELEMS = tile_elems<F, DP>(ROWS);
+    constexpr uint64_t ALL = ROWS == 64 ? ~uint64_t(0) : 0xffffffffull;
+    typedef Direct<(DIRECT ? DP : 128), (DIRECT ? ROWS : 64), kThreads> Straight;
+    typedef typename Num<F>::lds_t lds_t;
+    __shared__ __attribute__((aligned(16))) lds_t k_even[ELEMS], k_odd[ELEMS], v_even[ELEMS], v_odd[ELEMS];
     __shared__ int32_t ends[2][kWaves];
 
-    uint32_t b = die_run(blockIdx.x, gridDim.x);
-    const uint32_t tile = tiles - 1 - b % tiles;
-    b /= tiles;
-    const int32_t head = b % a.heads, kv_head = head / (a.heads / a.kv_heads), lane = threadIdx.x & 63, half = lane >> 5, wave = threadIdx.x >> 6;
-    const int64_t peer = b / a.heads, row0 = peer * a.T;
-    const int32_t T = static_cast<int32_t>(a.T), i = static_cast<int32_t>(tile * (32 * kWaves) + wave * 32 + (lane & 31));
+    const int32_t group = a.heads / a.kv_heads, lane = threadIdx.x & 63, half = lane >> 5, wave = threadIdx.x >> 6;
+    const Place place = place_of(blockIdx.x, a.N, a.kv_heads, group);
+    const uint32_t tile = tiles - 1 - place.tile;
+    const int32_t kv_head = place.kv_head, head = kv_head * group + place.member;
+    const int64_t peer = place.peer, row0 = peer * a.T;
+    const int32_t T = static_cast<int32_t>(a.T), i = static_cast<int32_t>(tile * kColumns) + wave * 32 + (lane & 31);
     const int32_t *first = a.first + row0;
     auto begin_of = [&](int32_t n) {
         const int32_t f = n < T ? first[n] : -1;
         return f <= n ? f : -1;
     };
-    const int32_t mine = begin_of(i);
-    const bool there = mine >= 0;
-    const int32_t lo = there ? mine : INT32_MAX, hi = there ? i : -1;
-    const int32_t wave_lo = wave_min(lo), wave_hi = wave_max(hi), all_from = wave_max(there ? mine : -1), all_to = wave_min(there ? i : INT32_MAX);
+    const int32_t lo = begin_of(i);
+    const bool there = lo >= 0;
+    const int32_t wave_lo = __builtin_amdgcn_readfirstlane(wave_min(there ? lo : INT32_MAX)), wave_hi = __builtin_amdgcn_readfirstlane(wave_max(there ? i : -1));
+    const int32_t all_from = __builtin_amdgcn_readfirstlane(wave_max(there ? lo : -1)), all_to = __builtin_amdgcn_readfirstlane(wave_min(there ? i : INT32_MAX));
     if (lane == 0) {
         ends[0][wave] = wave_lo;
         ends[1][wave] = wave_hi;
@@ -291,7 +313,9 @@ void queries_grad_kernel(AttentionGradArgs a, uint32_t tiles, const float *__res
         from = ends[0][w] < from ? ends[0][w] : from;
         to = ends[1][w] > to ? ends[1][w] : to;
     }
-    Held<DT, DP> q, d;
+    from = __builtin_amdgcn_readfirstlane(from);
+    to = __builtin_amdgcn_readfirstlane(to);
+    Held<F, DP> q, d;
     q.load(a.q + ((row0 + i) * a.q_stride + int64_t(head) * a.depth) * ES, there, a.depth);
     d.load(a.dout + ((row0 + i) * a.dout_stride + int64_t(head) * a.depth) * ES, there, a.depth);
     const int64_t n = (peer * a.heads + head) * a.T + i;
@@ -299,49 +323,72 @@ void queries_grad_kernel(AttentionGradArgs a, uint32_t tiles, const float *__res
     f32x16 dq[BLOCKS] = {};
     const char *k_rows = a.k + (row0 * a.k_stride + int64_t(kv_head) * a.depth) * ES, *v_rows = a.v + (row0 * a.v_stride + int64_t(kv_head) * a.depth) * ES;
     const int64_t k_bytes = a.k_stride * ES, v_bytes = a.v_stride * ES;
-    auto live_of = [&](int32_t f) { return __ballot(f >= 0) & 0xffffffffull; };
+    auto begins_at = [&](int32_t at) { return at <= to ? begin_of(at + lane) : -1; };
+    auto live_of = [&](int32_t f) { return __ballot(f >= 0) & ALL; };
     if (from <= to) {
-        Staged<DT, DP, ROWS, kThreads> k_next, v_next;
-        uint64_t live = live_of(begin_of(from + (lane & 31))), live_next = 0;
-        int32_t begin_next = from + ROWS <= to ? begin_of(from + ROWS + (lane & 31)) : -1;
-        int now = 0;
-        k_next.load(k_rows + from * k_bytes, k_bytes, live, a.depth, threadIdx.x);
-        v_next.load(v_rows + from * v_bytes, v_bytes, live, a.depth, threadIdx.x);
-        k_next.store(keys[0], threadIdx.x);
-        v_next.store(values[0], threadIdx.x);
-        for (int32_t at = from; at <= to; at += ROWS, now ^= 1, live = live_next) {
+        typename std::conditional<DIRECT, char, Staged<F, DP, ROWS, kThreads>>::type k_next, v_next;
+        auto request = [&](int32_t at, uint64_t live, lds_t *k_into, lds_t *v_into) __attribute__((always_inline)) {
+            if constexpr (DIRECT) {
+                Straight::request(k_rows + at * k_bytes, static_cast<uint32_t>(k_bytes), T - 1 - at, k_into);
+                Straight::request(v_rows + at * v_bytes, static_cast<uint32_t>(v_bytes), T - 1 - at, v_into);
+            } else {
+                k_next.load(k_rows + at * k_bytes, k_bytes, live, a.depth, threadIdx.x);
+                v_next.load(v_rows + at * v_bytes, v_bytes, live, a.depth, threadIdx.x);
+            }
+        };
+        auto fill = [&](uint64_t live, lds_t *k_into, lds_t *v_into) __attribute__((always_inline)) {
+            if constexpr (DIRECT) {
+                Straight::wait();
+                if (live != ALL) Straight::trim(live, k_into);         // (values without a token meet a weight that is taken as 0)
+            } else {
+                k_next.store(k_into, threadIdx.x);
+                v_next.store(v_into, threadIdx.x);
+            }
+        };
+        uint64_t live = live_of(begins_at(from)), live_next = 0;
+        int32_t begin_next = begins_at(from + ROWS), at = from;
+        request(from, live, k_even, v_even);
+        fill(live, k_even, v_even);
+        auto step = [&](const lds_t *keys, const lds_t *values, lds_t *k_into, lds_t *v_into) __attribute__((always_inline)) {
             __syncthreads();
             const bool more = at + ROWS <= to;
             if (more) {
                 live_next = live_of(begin_next);
-                k_next.load(k_rows + (at + ROWS) * k_bytes, k_bytes, live_next, a.depth, threadIdx.x);
-                v_next.load(v_rows + (at + ROWS) * v_bytes, v_bytes, live_next, a.depth, threadIdx.x);
-                begin_next = at + 2 * ROWS <= to ? begin_of(at + 2 * ROWS + (lane & 31)) : -1;
+                request(at + ROWS, live_next, k_into, v_into);
+                begin_next = begins_at(at + 2 * ROWS);
+                if constexpr (DIRECT) __builtin_amdgcn_sched_barrier(0);
             }
-            if (at <= wave_hi && at + ROWS > wave_lo) {
-                const f32x16 s = rows_times<DT, DP>(keys[now], 0, q);
-                f32x16 ds = rows_times<DT, DP>(values[now], 0, d);
+#pragma unroll
+            for (int n = 0; n < ROWS / 32; ++n) {
+                const int32_t j0 = at + 32 * n;
+                if (j0 > wave_hi || j0 + 32 <= wave_lo) continue;
+                const f32x16 s = rows_times<F, DP, ROWS>(keys, 32 * n, q);
+                f32x16 ds = rows_times<F, DP, ROWS>(values, 32 * n, d);
 #pragma unroll
                 for (int r = 0; r < 16; ++r) ds[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale, -lse)) * (ds[r] - off);
-                const bool whole = at >= all_from && at + ROWS - 1 <= all_to && live == 0xffffffffull;
-                if (!whole) {
-                    const int32_t low = there ? lo - at - 4 * half : INT32_MAX / 2;
-                    const uint32_t span = there ? static_cast<uint32_t>(hi - lo) : 0u;
-                    const uint32_t seen = static_cast<uint32_t>(live) >> (4 * half);
+                const uint32_t seen = static_cast<uint32_t>(live >> (32 * n));
+                if (j0 < all_from || j0 + 31 > all_to || seen != 0xffffffffu) {
+                    const int32_t low = there ? lo - j0 - 4 * half : INT32_MAX / 2;
+                    const uint32_t span = there ? static_cast<uint32_t>(i - lo) : 0u, mine = seen >> (4 * half);
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         const int32_t j = 8 * (r >> 2) + (r & 3);
-                        ds[r] = static_cast<uint32_t>(j - low) <= span && (seen >> j & 1) != 0 ? ds[r] : 0.f;
+                        ds[r] = static_cast<uint32_t>(j - low) <= span && (mine >> j & 1) != 0 ? ds[r] : 0.f;
                     }
                 }
-                const Weights<DT> w(ds);
+                Weights<F> w;
+                w.take(ds);
 #pragma unroll
-                for (int m = 0; m < BLOCKS; ++m) dq[m] = columns_times<DT, LP>(keys[now], 0, 32 * m, w, dq[m]);
+                for (int m = 0; m < BLOCKS; ++m) columns_times<F, DP, ROWS>(keys, 32 * n, 32 * m, w, dq[m]);
             }
-            if (more) {
-                k_next.store(keys[now ^ 1], threadIdx.x);
-                v_next.store(values[now ^ 1], threadIdx.x);
-            }
+            if (more) fill(live_next, k_into, v_into);
+            live = live_next;
+            at += ROWS;
+            return more;
+        };
+        for (;;) {
+            if (!step(k_even, v_even, k_odd, v_odd)) break;
+            if (!step(k_odd, v_odd, k_even, v_even)) break;
         }
     }
     if (i >= T) return;
@@ -353,11 +400,9 @@ void queries_grad_kernel(AttentionGradArgs a, uint32_t tiles, const float *__res
     }
 }
 
-int depth_of(int depth) { return depth <= 32 ? 32 : depth <= 64 ? 64 : depth <= 128 ? 128 : 256; }
+int slices_of(int dtype, int depth) { return depth <= 128 ? 1 : dtype != 0 ? 2 : depth <= 192 ? 3 : 4; }
 
-int slices_of(int dtype, int depth) { return depth_of(depth) <= 128 ? 1 : dtype == 0 ? 4 : 2; }
-
-int64_t tiles_of(const AttentionGradArgs &a) { return (a.T + 32 * kWaves - 1) / (32 * kWaves); }
+int64_t tiles_of(const AttentionGradArgs &a) { return (a.T + kColumns - 1) / kColumns; }
 int64_t stats_of(const AttentionGradArgs &a) { return (a.T + kStat - 1) / kStat; }
 
 KeysPlan keys_plan(const AttentionGradArgs &a, int dtype, int compute_units)
@@ -401,27 +446,24 @@ hipError_t launch_attention_grad(const AttentionGradArgs &given, int dtype, void
     float *partials = reinterpret_cast<float *>(reinterpret_cast<char *>(ranges) + round_up(int64_t(sizeof(Range)) * a.N * stats_of(a)));
     const int64_t delta_blocks = (a.N * a.T * a.heads + 15) / 16, range_blocks = (a.N * stats_of(a) + 15) / 16;
     (dtype == 0 ? delta_kernel<0> : delta_kernel<1>)<<<static_cast<uint32_t>(delta_blocks + range_blocks), kThreads, 0, stream>>>(a, delta, ranges, delta_blocks);
-    auto of = [&](auto dt, auto dp) {
-        constexpr int DT = decltype(dt)::value, DP = decltype(dp)::value;
-        const uint32_t slices = DP / sum_depths<DT, DP>();
-        keys_grad_kernel<DT, DP><<<static_cast<uint32_t>(a.N * a.kv_heads * p.tiles * p.parts) * slices, kThreads, 0, stream>>>(a, p, delta, ranges, partials);
+    const bool q_direct = direct_rows(a.q, a.q_stride) && direct_rows(a.dout, a.dout_stride), k_direct = direct_rows(a.k, a.k_stride) && direct_rows(a.v, a.v_stride);
+    auto of = [&](auto form, auto dp) {
+        constexpr Form F = decltype(form)::value;
+        constexpr int DP = decltype(dp)::value, DT = Num<F>::DT, SIMD = DP > 128 || F == kParts ? 1 : 2;
+        constexpr bool ASIDE = F == kBf16 && DP == 128, STRAIGHT = F == kBf16 && DP > 32 && DP <= 128;
+        const uint32_t key_blocks = static_cast<uint32_t>(a.N * a.kv_heads * p.tiles * p.parts) * (DP / sum_depths<F, DP>()), query_blocks = static_cast<uint32_t>(a.N * a.heads * p.tiles);
+        if (STRAIGHT && a.depth == DP && q_direct) keys_grad_kernel<F, DP, SIMD, ASIDE, STRAIGHT><<<key_blocks, kThreads, 0, stream>>>(a, p, delta, ranges, partials);
+        else keys_grad_kernel<F, DP, SIMD, ASIDE, false><<<key_blocks, kThreads, 0, stream>>>(a, p, delta, ranges, partials);
         if (p.parts > 1) {
             const int64_t blocks = (a.N * a.T * 2 * a.kv_heads * a.depth + kThreads - 1) / kThreads;
             keys_join_kernel<DT><<<static_cast<uint32_t>(blocks < 4096 ? blocks : 4096), kThreads, 0, stream>>>(a, p.parts, partials);
         }
-        queries_grad_kernel<DT, DP><<<static_cast<uint32_t>(a.N * a.heads * p.tiles), kThreads, 0, stream>>>(a, p.tiles, delta);
+        constexpr int ROWS = F == kBf16 && DP <= 128 ? 64 : 32;
+        if (STRAIGHT && a.depth == DP && k_direct) queries_grad_kernel<F, DP, ROWS, SIMD, STRAIGHT><<<query_blocks, kThreads, 0, stream>>>(a, p.tiles, delta);
+        else queries_grad_kernel<F, DP, ROWS, SIMD, false><<<query_blocks, kThreads, 0, stream>>>(a, p.tiles, delta);
         return hipGetLastError();
     };
-    using std::integral_constant;
-    auto of_type = [&](auto dt) {
-        switch (depth_of(a.depth)) {
-        case 32: return of(dt, integral_constant<int, 32>{});
-        case 64: return of(dt, integral_constant<int, 64>{});
-        case 128: return of(dt, integral_constant<int, 128>{});
-        default: return of(dt, integral_constant<int, 256>{});
-        }
-    };
-    return dtype == 0 ? of_type(integral_constant<int, 0>{}) : of_type(integral_constant<int, 1>{});
+    return by_depth(dtype, a.depth, of);
 }
 
 }  // namespace moshpit

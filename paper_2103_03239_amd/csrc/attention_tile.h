@@ -8,8 +8,12 @@
 // The weights of the second are blocks of the first as they lie in the lanes: the order of the summed index may be any, as
 // long as the tile is read in the same one, so weights never move between lanes.
 //
-// DT: 0 = binary32, by the binary32 matrix instructions; 1 = bfloat16, weights rounded to bfloat16 for the product.  DP: the depth, rounded up
-// to a multiple of 32 (zeros behind it).
+// Forms:
+//   kBf16   bfloat16 matrices; weights are rounded to bfloat16 for their product, the rest is exact before the binary32 sums
+//   kParts  binary32 matrices as three bfloat16 parts of 8 significant bits each, six products in place of one: what is left out is 2^-24 of
+//           a product and less.  At sixteen times the rate of the binary32 matrix instructions, so 2.7 times as fast
+//   kF32    binary32 matrices by the binary32 matrix instructions, where the parts of deep heads do not fit the registers
+// DP: the depth, rounded up to a multiple of 32 (zeros behind it).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -27,47 +31,101 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
 
-template <int DT> struct Num;
-template <> struct Num<0> {
-    typedef float lds_t;
-    static constexpr int ES = 4, CE = 4;                              // bytes of an element, elements of 16 bytes
-};
-template <> struct Num<1> {
-    typedef uint16_t lds_t;
-    static constexpr int ES = 2, CE = 8;
+enum Form { kF32 = 0, kBf16 = 1, kParts = 2 };
+
+template <Form F> struct Num {
+    static constexpr int DT = F == kBf16 ? 1 : 0;                     // type of the matrices, as in row_elems.h
+    static constexpr int ES = F == kBf16 ? 2 : 4;                     // bytes of their elements
+    static constexpr int PARTS = F == kParts ? 3 : 1;
+    static constexpr int LS = F == kF32 ? 4 : 2, CE = 16 / LS;        // bytes of an element in LDS, elements of 16 bytes there
+    typedef typename std::conditional<F == kF32, float, uint16_t>::type lds_t;
 };
 
+// Elements of a tile's row in LDS, and of a tile of `rows` rows, all its parts.
 constexpr int row_elems_of(int DP) { return DP <= 32 ? 32 : DP <= 64 ? 64 : DP <= 128 ? 128 : 256; }
+template <Form F, int DP> constexpr int tile_elems(int rows) { return Num<F>::PARTS * rows * row_elems_of(DP); }
+template <Form F, int DP> constexpr int tile_bytes(int rows) { return tile_elems<F, DP>(rows) * Num<F>::LS; }
 
 // Where 16-byte chunk `chunk` of row `row` of a tile with LP elements a row lies, in elements.  Rows are a power of two long, so the chunks
 // of a row are stored with their numbers xor a number of the row: 16 consecutive rows' same chunks then lie in different banks (for
 // rows_times), and so do 4 consecutive rows' same 64 bytes (for the transposing reads of columns_times).
-template <int DT, int LP> __device__ __forceinline__ int chunk_at(int row, int chunk)
+template <int CH> __device__ __forceinline__ int chunk_shift(int row)
 {
-    constexpr int CE = Num<DT>::CE, CH = LP / CE;
-    const int moved = CH >= 16 ? ((row & 3) << 2 | (row >> 2 & 3)) : CH == 8 ? ((row >> 1 & 1) << 2 | (row >> 2 & 3)) : (row >> 2 & 3);
-    return row * LP + (chunk ^ moved) * CE;
+    return CH >= 16 ? ((row & 3) << 2 | (row >> 2 & 3)) : CH == 8 ? ((row >> 1 & 1) << 2 | (row >> 2 & 3)) : (row >> 2 & 3);
+}
+template <Form F, int LP> __device__ __forceinline__ int chunk_at(int row, int chunk)
+{
+    constexpr int CE = Num<F>::CE;
+    return row * LP + (chunk ^ chunk_shift<LP / CE>(row)) * CE;
 }
 
-// 16 bytes of a row from p on, of which `left` elements are the row's; zeros behind them.
-template <int DT> __device__ __forceinline__ u32x4 load_chunk(const char *p, int left)
+// `count` elements of 4 or 2 bytes from p on that end after `left` of them; zeros behind.
+template <int DT, int WORDS> __device__ __forceinline__ void load_words(const char *p, int left, u32x4 (&v)[WORDS])
 {
-    constexpr int ES = Num<DT>::ES, CE = Num<DT>::CE;
-    if (left >= CE) return load_vec<false, u32x4>(p);
-    u32x4 v = {0, 0, 0, 0};
+    constexpr int ES = DT == 0 ? 4 : 2, EACH = 16 / ES;
+    if (left >= EACH * WORDS) {
 #pragma unroll
-    for (int k = 0; k < CE; ++k)
-        if (k < left) {
-            if constexpr (DT == 0) v[k] = *reinterpret_cast<const uint32_t *>(p + k * ES);
-            else v[k / 2] |= static_cast<uint32_t>(*reinterpret_cast<const uint16_t *>(p + k * ES)) << (16 * (k & 1));
-        }
-    return v;
+        for (int q = 0; q < WORDS; ++q) v[q] = load_vec<false, u32x4>(p + 16 * q);
+        return;
+    }
+#pragma unroll
+    for (int q = 0; q < WORDS; ++q) {
+        v[q] = u32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int k = 0; k < EACH; ++k)
+            if (q * EACH + k < left) {
+                if constexpr (DT == 0) v[q][k] = *reinterpret_cast<const uint32_t *>(p + 16 * q + k * ES);
+                else v[q][k / 2] |= static_cast<uint32_t>(*reinterpret_cast<const uint16_t *>(p + 16 * q + k * ES)) << (16 * (k & 1));
+            }
+    }
 }
 
-// 32 columns held by a wave: lane l has chunks l / 32, 2 + l / 32, ... of column l % 32.
-template <int DT, int DP> struct Held {
-    static constexpr int CE = Num<DT>::CE, COUNT = DP / (2 * CE);
-    u32x4 v[COUNT];
+// A unit: the elements of a row that are 16 bytes of a tile's (of each of its parts).
+template <Form F> struct Unit {
+    static constexpr int WORDS = Num<F>::CE * Num<F>::ES / 16;
+    u32x4 v[WORDS];
+
+    __device__ __forceinline__ void load(const char *p, int left) { load_words<Num<F>::DT, WORDS>(p, left, v); }
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int q = 0; q < WORDS; ++q) v[q] = u32x4{0, 0, 0, 0};
+    }
+};
+
+// Upper halves of two words, a's in the lower half.
+__device__ __forceinline__ uint32_t upper_halves(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
+
+// Two binary32 values as pairs of bfloat16 parts, 8 significant bits each, cut off (so the largest do not round up to infinity).
+__device__ __forceinline__ void split_pair(float a, float b, uint32_t (&part)[3])
+{
+#pragma unroll
+    for (int q = 0; q < 3; ++q) {
+        const uint32_t u = __float_as_uint(a), w = __float_as_uint(b);
+        part[q] = upper_halves(u, w);
+        a -= __uint_as_float(u & 0xffff0000u);
+        b -= __uint_as_float(w & 0xffff0000u);
+    }
+}
+
+// A unit's 16 bytes of every part.
+template <Form F> __device__ __forceinline__ void parts_of(const Unit<F> &u, u32x4 (&part)[Num<F>::PARTS])
+{
+    if constexpr (F != kParts) part[0] = u.v[0];
+    else
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            uint32_t p[3];
+            split_pair(__uint_as_float(u.v[k / 2][2 * (k & 1)]), __uint_as_float(u.v[k / 2][2 * (k & 1) + 1]), p);
+#pragma unroll
+            for (int q = 0; q < 3; ++q) part[q][k] = p[q];
+        }
+}
+
+// 32 columns held by a wave: lane l has units l / 32, 2 + l / 32, ... of column l % 32.
+template <Form F, int DP> struct Held {
+    static constexpr int CE = Num<F>::CE, COUNT = DP / (2 * CE), PARTS = Num<F>::PARTS;
+    u32x4 v[PARTS][COUNT];
 
     // column: this lane's, from its first element on; `depth` elements, none where it is not `there`.
     __device__ __forceinline__ void load(const char *column, bool there, int depth)
@@ -76,76 +134,135 @@ template <int DT, int DP> struct Held {
 #pragma unroll
         for (int s = 0; s < COUNT; ++s) {
             const int at = (2 * s + half) * CE;
-            v[s] = there && at < depth ? load_chunk<DT>(column + at * Num<DT>::ES, depth - at) : u32x4{0, 0, 0, 0};
+            Unit<F> u;
+            u.clear();
+            if (there && at < depth) u.load(column + at * Num<F>::ES, depth - at);
+            u32x4 part[PARTS];
+            parts_of<F>(u, part);
+#pragma unroll
+            for (int q = 0; q < PARTS; ++q) v[q][s] = part[q];
         }
     }
 };
 
-// Rows row0 .. row0 + 31 of the tile times the columns.
-template <int DT, int DP> __device__ __forceinline__ f32x16 rows_times(const typename Num<DT>::lds_t *tile, int row0, const Held<DT, DP> &held)
+// The same out of LDS: the columns are rows 0 .. 31 of a tile.
+template <Form F, int DP> struct Aside {
+    const uint16_t *tile;                // (of one part: bfloat16)
+
+    __device__ __forceinline__ static void put(const Held<F, DP> &held, uint16_t *into)
+    {
+#pragma unroll
+        for (int s = 0; s < DP / 16; ++s) *reinterpret_cast<u32x4 *>(into + chunk_at<F, row_elems_of(DP)>(threadIdx.x & 31, 2 * s + (threadIdx.x >> 5 & 1))) = held.v[0][s];
+    }
+};
+
+__device__ __forceinline__ f32x16 mfma_bf16(const u32x4 &a, const u32x4 &b, const f32x16 &c)
 {
-    constexpr int LP = row_elems_of(DP);
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// Products of parts, the smallest first; 2^-24 of a product and less is left out.
+constexpr int kTileParts[6] = {2, 1, 0, 1, 0, 0}, kHeldParts[6] = {0, 1, 2, 0, 1, 0};
+
+// Rows row0 .. row0 + 31 of the tile (ROWS rows a part) times the columns.
+template <Form F, int DP, int ROWS>
+__device__ __forceinline__ f32x16 rows_times(const typename Num<F>::lds_t *tile, int row0, const Held<F, DP> &held)
+{
+    constexpr int LP = row_elems_of(DP), PARTS = Num<F>::PARTS;
     const int row = row0 + (threadIdx.x & 31), half = threadIdx.x >> 5 & 1;
     f32x16 sum = {};
 #pragma unroll
-    for (int s = 0; s < Held<DT, DP>::COUNT; ++s) {
-        const u32x4 a = *reinterpret_cast<const u32x4 *>(tile + chunk_at<DT, LP>(row, 2 * s + half));
-        if constexpr (DT == 1) sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, held.v[s]), sum, 0, 0, 0);
+    for (int s = 0; s < Held<F, DP>::COUNT; ++s) {
+        u32x4 a[PARTS];
+#pragma unroll
+        for (int q = 0; q < PARTS; ++q) a[q] = *reinterpret_cast<const u32x4 *>(tile + q * ROWS * LP + chunk_at<F, LP>(row, 2 * s + half));
+        if constexpr (F == kBf16) sum = mfma_bf16(a[0], held.v[0][s], sum);
+        else if constexpr (F == kParts)
+#pragma unroll
+            for (int n = 0; n < 6; ++n) sum = mfma_bf16(a[kTileParts[n]], held.v[kHeldParts[n]][s], sum);
         else
 #pragma unroll
-            for (int e = 0; e < 4; ++e) sum = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[e]), __uint_as_float(held.v[s][e]), sum, 0, 0, 0);
+            for (int e = 0; e < 4; ++e) sum = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[0][e]), __uint_as_float(held.v[0][s][e]), sum, 0, 0, 0);
     }
     return sum;
 }
 
+template <Form F, int DP, int ROWS>
+__device__ __forceinline__ f32x16 rows_times(const uint16_t *tile, int row0, const Aside<F, DP> &aside)
+{
+    constexpr int LP = row_elems_of(DP);
+    const int lane_row = threadIdx.x & 31, half = threadIdx.x >> 5 & 1;
+    f32x16 sum = {};
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s)
+        sum = mfma_bf16(*reinterpret_cast<const u32x4 *>(tile + chunk_at<F, LP>(row0 + lane_row, 2 * s + half)),
+                        *reinterpret_cast<const u32x4 *>(aside.tile + chunk_at<F, LP>(lane_row, 2 * s + half)), sum);
+    return sum;
+}
+
 // Weights of 32 rows as the matrix instructions take them.
-template <int DT> struct Weights;
-template <> struct Weights<0> {
-    f32x16 w;
-    __device__ __forceinline__ explicit Weights(const f32x16 &p) : w(p) {}
-};
-template <> struct Weights<1> {
-    u32x4 w[2];
-    __device__ __forceinline__ explicit Weights(const f32x16 &p)
+template <Form F> struct Weights {
+    u32x4 w[Num<F>::PARTS][2];
+    __device__ __forceinline__ void take(const f32x16 &p)
     {
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) w[t][k] = bf16_pair(p[8 * t + 2 * k], p[8 * t + 2 * k + 1]);
+            for (int k = 0; k < 4; ++k) {
+                if constexpr (F == kBf16) w[0][t][k] = bf16_pair(p[8 * t + 2 * k], p[8 * t + 2 * k + 1]);
+                else {
+                    uint32_t part[3];
+                    split_pair(p[8 * t + 2 * k], p[8 * t + 2 * k + 1], part);
+#pragma unroll
+                    for (int q = 0; q < 3; ++q) w[q][t][k] = part[q];
+                }
+            }
     }
 };
+template <> struct Weights<kF32> {
+    f32x16 w;
+    __device__ __forceinline__ void take(const f32x16 &p) { w = p; }
+};
 
-// sum + columns col0 .. col0 + 31 of the tile's rows row0 .. row0 + 31, each row times its weight.
-template <int DT, int LP>
-__device__ __forceinline__ f32x16 columns_times(const typename Num<DT>::lds_t *tile, int row0, int col0, const Weights<DT> &weights, f32x16 sum)
+// sum += columns col0 .. col0 + 31 of the tile's rows row0 .. row0 + 31, each row times its weight.
+template <Form F, int DP, int ROWS>
+__device__ __forceinline__ void columns_times(const typename Num<F>::lds_t *tile, int row0, int col0, const Weights<F> &weights, f32x16 &sum)
 {
+    constexpr int LP = row_elems_of(DP), PARTS = Num<F>::PARTS;
     const int lane = threadIdx.x & 63, half = lane >> 5;
-    if constexpr (DT == 1) {
+    if constexpr (F != kF32) {
         typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
         const int j = lane & 15, row = row0 + 4 * half + (j >> 2), chunk = col0 / 8 + 2 * (lane >> 4 & 1) + (j >> 1 & 1), in = 4 * (j & 1);
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const s16x4 low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + chunk_at<DT, LP>(row + 16 * t, chunk) + in));
-            const s16x4 high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(tile + chunk_at<DT, LP>(row + 16 * t + 8, chunk) + in));
-            const s16x8 a = __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7);
-            sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, weights.w[t]), sum, 0, 0, 0);
+            u32x4 a[PARTS];
+#pragma unroll
+            for (int q = 0; q < PARTS; ++q) {
+                const uint16_t *part = tile + q * ROWS * LP;
+                const s16x4 low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(part + chunk_at<F, LP>(row + 16 * t, chunk) + in));
+                const s16x4 high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(part + chunk_at<F, LP>(row + 16 * t + 8, chunk) + in));
+                a[q] = __builtin_bit_cast(u32x4, __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7));
+            }
+            if constexpr (F == kBf16) sum = mfma_bf16(a[0], weights.w[0][t], sum);
+            else
+#pragma unroll
+                for (int n = 0; n < 6; ++n) sum = mfma_bf16(a[kTileParts[n]], weights.w[kHeldParts[n]][t], sum);
         }
     } else {
         const int col = col0 + (lane & 31);
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
             const int row = row0 + 8 * (r >> 2) + 4 * half + (r & 3);
-            sum = __builtin_amdgcn_mfma_f32_32x32x2f32(tile[chunk_at<DT, LP>(row, col >> 2) + (col & 3)], weights.w[r], sum, 0, 0, 0);
+            sum = __builtin_amdgcn_mfma_f32_32x32x2f32(tile[chunk_at<F, LP>(row, col >> 2) + (col & 3)], weights.w[r], sum, 0, 0, 0);
         }
     }
-    return sum;
 }
 
 // ROWS rows on their way into a tile by THREADS threads, number `thread` of which this is.
-template <int DT, int DP, int ROWS, int THREADS> struct Staged {
-    static constexpr int CE = Num<DT>::CE, LP = row_elems_of(DP), CH = LP / CE, COUNT = (ROWS * CH + THREADS - 1) / THREADS;
+template <Form F, int DP, int ROWS, int THREADS> struct Staged {
+    static constexpr int CE = Num<F>::CE, LP = row_elems_of(DP), CH = LP / CE, COUNT = (ROWS * CH + THREADS - 1) / THREADS;
     static_assert(ROWS * CH % THREADS == 0 || COUNT == 1);            // (of a small tile some threads have nothing)
-    u32x4 v[COUNT];
+    Unit<F> unit[COUNT];
 
     // rows: the tile's first row, from its first element on; row r is read where bit r of `live` is set and is zeros elsewhere.
     __device__ __forceinline__ void load(const char *rows, int64_t row_bytes, uint64_t live, int depth, int thread)
@@ -153,42 +270,80 @@ template <int DT, int DP, int ROWS, int THREADS> struct Staged {
 #pragma unroll
         for (int n = 0; n < COUNT; ++n) {
             const int row = (thread + n * THREADS) / CH, at = (thread + n * THREADS) % CH * CE;
-            v[n] = row < ROWS && (live >> row & 1) != 0 && at < depth ? load_chunk<DT>(rows + row * row_bytes + at * Num<DT>::ES, depth - at) : u32x4{0, 0, 0, 0};
+            unit[n].clear();
+            if (row < ROWS && (live >> row & 1) != 0 && at < depth) unit[n].load(rows + row * row_bytes + at * Num<F>::ES, depth - at);
         }
     }
-    __device__ __forceinline__ void store(typename Num<DT>::lds_t *tile, int thread) const
+    __device__ __forceinline__ void store(typename Num<F>::lds_t *tile, int thread) const
     {
-#pragma unroll
-        for (int n = 0; n < COUNT; ++n)
-            if (ROWS * CH % THREADS == 0 || thread < ROWS * CH)
-                *reinterpret_cast<u32x4 *>(tile + chunk_at<DT, LP>((thread + n * THREADS) / CH, (thread + n * THREADS) % CH)) = v[n];
-    }
-    // Infinities and NaN to zeros; bit r of what is returned: row r had some among this thread's.
-    __device__ __forceinline__ uint64_t clean(int thread)
-    {
-        uint64_t found = 0;
 #pragma unroll
         for (int n = 0; n < COUNT; ++n) {
-            bool any = false;
+            if (ROWS * CH % THREADS != 0 && thread >= ROWS * CH) continue;
+            u32x4 part[Num<F>::PARTS];
+            parts_of<F>(unit[n], part);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                uint32_t w = v[n][k];
-                if constexpr (DT == 0) {
-                    if ((w & 0x7f800000u) == 0x7f800000u) w = 0;
-                } else {
-                    if ((w & 0x7f800000u) == 0x7f800000u) w &= 0xffffu;
-                    if ((w & 0x7f80u) == 0x7f80u) w &= 0xffff0000u;
-                }
-                any = any || w != v[n][k];
-                v[n][k] = w;
-            }
-            if (any) found |= uint64_t(1) << ((thread + n * THREADS) / CH);
+            for (int q = 0; q < Num<F>::PARTS; ++q)
+                *reinterpret_cast<u32x4 *>(tile + q * ROWS * LP + chunk_at<F, LP>((thread + n * THREADS) / CH, (thread + n * THREADS) % CH)) = part[q];
         }
-        return found;
     }
 };
 
-// The column's sums of both halves of the wave.
+// The same for bfloat16 rows of DP elements that are whole 16-byte vectors: from memory into LDS without passing through registers, a wave 1
+// KiB at a time: lane l's 16 bytes to where the wave's begin + 16 * l, so the lane reads the chunk that chunk_at() puts there.
+template <int DP, int ROWS, int THREADS> struct Direct {
+    static constexpr int LP = row_elems_of(DP), CH = LP / 8, WAVES = THREADS / 64, EACH = 64 / CH, COUNT = ROWS / EACH / WAVES;      // rows of 1 KiB; KiB of a wave
+    static_assert(COUNT >= 1 && ROWS % (EACH * WAVES) == 0);
+
+    // Rows 0 .. last of the tile are there to be read; what is in the place of further ones is any row.
+    __device__ __forceinline__ static void request(const char *rows, uint32_t row_bytes, int32_t last, uint16_t *tile)
+    {
+        typedef __attribute__((address_space(3))) uint16_t lds_u16;
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(rows), 0, 0xffffffffu, 0x00027000);
+#pragma unroll
+        for (int n = 0; n < COUNT; ++n) {
+            const int begin = (wave * COUNT + n) * EACH, row = begin + lane / CH, chunk = (lane % CH) ^ chunk_shift<CH>(row);
+            const uint32_t at = static_cast<uint32_t>(row < last ? row : last) * row_bytes + (DP == LP || chunk < DP / 8 ? chunk * 16 : 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_u16 *)(tile + begin * LP), 16, at, 0, 0, 0);
+        }
+    }
+    // Behind a wait for all that was requested: rows whose bit in `live` is not set become zeros.
+    __device__ __forceinline__ static void trim(uint64_t live, uint16_t *tile)
+    {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+        for (int n = 0; n < COUNT; ++n) {
+            const int begin = (wave * COUNT + n) * EACH;
+            if ((live >> (begin + lane / CH) & 1) == 0) *reinterpret_cast<u32x4 *>(tile + begin * LP + lane * 8) = u32x4{0, 0, 0, 0};
+        }
+    }
+    __device__ __forceinline__ static void wait() { __builtin_amdgcn_s_waitcnt(0x0f70); }              // vmcnt(0)
+};
+// Whether a matrix's rows can be read so: whole vectors, and a tile's offsets below 2^31.
+inline bool direct_rows(const void *p, int64_t stride) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0 && stride <= (int64_t(1) << 23); }
+
+// Which tile of which peer's head block number `block` takes.  Tiles with the most work come first for all peers and heads (a peer's sequences may
+// be longer than another's, so none is left to a single die), and a tile's blocks of the query heads that share keys go to the
+// same die where the peers' heads of keys are a multiple of 8 (block b runs on die b % 8), another one for each tile.
+struct Place {
+    uint32_t tile;                       // 0: the one with the most work
+    int64_t peer;
+    int32_t kv_head, member;             // the head of keys, and the query head among those that share it
+};
+__device__ __forceinline__ Place place_of(uint32_t block, int64_t N, int32_t kv_heads, int32_t members)
+{
+    const uint32_t units = static_cast<uint32_t>(N) * kv_heads, turn = block / units;
+    Place p;
+    p.tile = turn / members;
+    p.member = static_cast<int32_t>(turn % members);
+    uint32_t unit = block % units + p.tile % units;
+    unit = unit >= units ? unit - units : unit;
+    p.peer = unit / kv_heads;
+    p.kv_head = static_cast<int32_t>(unit % kv_heads);
+    return p;
+}
+
+// Of both halves of the wave, which hold the same columns.
 __device__ __forceinline__ float halves_sum(float v)
 {
     const LanePair p = swap32(v, v);
@@ -214,7 +369,7 @@ __device__ __forceinline__ int32_t wave_max(int32_t v) { return -wave_min(-v); }
 // Writes a column's rows (depths col0 .. + 31 of the block) to `to`, its place for depth 0; `depth` elements in all.
 template <int DT> __device__ __forceinline__ void store_column(char *to, int col0, int depth, const f32x16 &block, float factor)
 {
-    constexpr int ES = Num<DT>::ES;
+    constexpr int ES = DT == 0 ? 4 : 2;
     const int half = threadIdx.x >> 5 & 1;
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
@@ -228,6 +383,21 @@ template <int DT> __device__ __forceinline__ void store_column(char *to, int col
             for (int k = 0; k < 4; ++k)
                 if (k < left) store_one<DT>(to + (at + k) * ES, f[k]);
     }
+}
+
+// go(form, depth) with the kernels' form and their rounded depth for `depth` elements of type dtype.
+template <typename Go> hipError_t by_depth(int dtype, int depth, Go go)
+{
+    using std::integral_constant;
+    auto of_form = [&](auto form, auto deep) {
+        if (depth <= 32) return go(form, integral_constant<int, 32>{});
+        if (depth <= 64) return go(form, integral_constant<int, 64>{});
+        if (depth <= 96) return go(form, integral_constant<int, 96>{});
+        if (depth <= 128) return go(form, integral_constant<int, 128>{});
+        if (depth <= 192) return go(deep, integral_constant<int, 192>{});
+        return go(deep, integral_constant<int, 256>{});
+    };
+    return dtype == 0 ? of_form(integral_constant<Form, kParts>{}, integral_constant<Form, kF32>{}) : of_form(integral_constant<Form, kBf16>{}, integral_constant<Form, kBf16>{});
 }
 
 }  // namespace moshpit
