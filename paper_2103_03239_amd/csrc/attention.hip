@@ -79,8 +79,7 @@ template <Form F, int DP> struct Queries {
     // sum += rows row0 .. + 31 of the tile of values (ROWS rows) times their weights
     template <int ROWS> __device__ __forceinline__ void add(const typename Num<F>::lds_t *values, int row0, const Weights<F> &w)
     {
-#pragma unroll
-        for (int m = 0; m < BLOCKS; ++m) columns_times<F, DP, ROWS>(values, row0, 32 * m, w, sum[m]);
+        columns_times<F, DP, ROWS>(values, row0, 0, w, sum);
     }
     // What scores of 32 * N keys bring, whose values the tile holds.
     template <int ROWS, int N> __device__ __forceinline__ void take(f32x16 (&s)[N], float scale, const typename Num<F>::lds_t *values)

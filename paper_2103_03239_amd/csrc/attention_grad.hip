@@ -219,11 +219,9 @@ void keys_grad_kernel(AttentionGradArgs a, KeysPlan plan, const float *__restric
             }
             Weights<F> w;
             w.take(p);
-#pragma unroll
-            for (int m = 0; m < BLOCKS; ++m) columns_times<F, DP, ROWS>(douts, 0, slice * DA + 32 * m, w, dv[m]);
+            columns_times<F, DP, ROWS>(douts, 0, slice * DA, w, dv);
             w.take(ds);
-#pragma unroll
-            for (int m = 0; m < BLOCKS; ++m) columns_times<F, DP, ROWS>(queries, 0, slice * DA + 32 * m, w, dk[m]);
+            columns_times<F, DP, ROWS>(queries, 0, slice * DA, w, dk);
         }
         if (more) fill(q_into, d_into, now ^ 1);
         return more;
@@ -378,8 +376,7 @@ void queries_grad_kernel(AttentionGradArgs a, uint32_t tiles, const float *__res
                 }
                 Weights<F> w;
                 w.take(ds);
-#pragma unroll
-                for (int m = 0; m < BLOCKS; ++m) columns_times<F, DP, ROWS>(keys, 32 * n, 32 * m, w, dq[m]);
+                columns_times<F, DP, ROWS>(keys, 32 * n, 0, w, dq);
             }
             if (more) fill(live_next, k_into, v_into);
             live = live_next;

@@ -164,18 +164,34 @@ __device__ __forceinline__ f32x16 mfma_bf16(const u32x4 &a, const u32x4 &b, cons
 // Products of parts, the smallest first; 2^-24 of a product and less is left out.
 constexpr int kTileParts[6] = {2, 1, 0, 1, 0, 0}, kHeldParts[6] = {0, 1, 2, 0, 1, 0};
 
+// v, as a number that the compiler knows nothing of: addresses made of it are made anew where they are used, in an instruction or none, and do not
+// take registers from one step to the next (there are dozens, for each of a kernel's tiles).
+__device__ __forceinline__ uint32_t afresh(uint32_t v)
+{
+    asm volatile("" : "+v"(v));
+    return v;
+}
+template <typename T> __device__ __forceinline__ T from_lds(const void *base, uint32_t bytes) { return *reinterpret_cast<const T *>(static_cast<const char *>(base) + bytes); }
+
+// Where row lane % 32 of a tile has chunk lane / 32, in bytes; xor 32 s: chunk 2 s + lane / 32.
+template <Form F, int DP> __device__ __forceinline__ uint32_t lane_row()
+{
+    const int row = threadIdx.x & 31, half = threadIdx.x >> 5 & 1;
+    return afresh(static_cast<uint32_t>(chunk_at<F, row_elems_of(DP)>(row, half) * Num<F>::LS));
+}
+
 // Rows row0 .. row0 + 31 of the tile (ROWS rows a part) times the columns.
 template <Form F, int DP, int ROWS>
 __device__ __forceinline__ f32x16 rows_times(const typename Num<F>::lds_t *tile, int row0, const Held<F, DP> &held)
 {
-    constexpr int LP = row_elems_of(DP), PARTS = Num<F>::PARTS;
-    const int row = row0 + (threadIdx.x & 31), half = threadIdx.x >> 5 & 1;
+    constexpr int PARTS = Num<F>::PARTS, ROW_BYTES = row_elems_of(DP) * Num<F>::LS;
+    const uint32_t at = lane_row<F, DP>();
     f32x16 sum = {};
 #pragma unroll
     for (int s = 0; s < Held<F, DP>::COUNT; ++s) {
         u32x4 a[PARTS];
 #pragma unroll
-        for (int q = 0; q < PARTS; ++q) a[q] = *reinterpret_cast<const u32x4 *>(tile + q * ROWS * LP + chunk_at<F, LP>(row, 2 * s + half));
+        for (int q = 0; q < PARTS; ++q) a[q] = from_lds<u32x4>(tile, (at ^ (32 * s)) + (q * ROWS + row0) * ROW_BYTES);
         if constexpr (F == kBf16) sum = mfma_bf16(a[0], held.v[0][s], sum);
         else if constexpr (F == kParts)
 #pragma unroll
@@ -186,17 +202,14 @@ __device__ __forceinline__ f32x16 rows_times(const typename Num<F>::lds_t *tile,
     }
     return sum;
 }
-
 template <Form F, int DP, int ROWS>
 __device__ __forceinline__ f32x16 rows_times(const uint16_t *tile, int row0, const Aside<F, DP> &aside)
 {
-    constexpr int LP = row_elems_of(DP);
-    const int lane_row = threadIdx.x & 31, half = threadIdx.x >> 5 & 1;
+    constexpr int ROW_BYTES = row_elems_of(DP) * 2;
+    const uint32_t at = lane_row<F, DP>();
     f32x16 sum = {};
 #pragma unroll
-    for (int s = 0; s < DP / 16; ++s)
-        sum = mfma_bf16(*reinterpret_cast<const u32x4 *>(tile + chunk_at<F, LP>(row0 + lane_row, 2 * s + half)),
-                        *reinterpret_cast<const u32x4 *>(aside.tile + chunk_at<F, LP>(lane_row, 2 * s + half)), sum);
+    for (int s = 0; s < DP / 16; ++s) sum = mfma_bf16(from_lds<u32x4>(tile, (at ^ (32 * s)) + row0 * ROW_BYTES), from_lds<u32x4>(aside.tile, at ^ (32 * s)), sum);
     return sum;
 }
 
@@ -224,37 +237,48 @@ template <> struct Weights<kF32> {
     __device__ __forceinline__ void take(const f32x16 &p) { w = p; }
 };
 
-// sum += columns col0 .. col0 + 31 of the tile's rows row0 .. row0 + 31, each row times its weight.
-template <Form F, int DP, int ROWS>
-__device__ __forceinline__ void columns_times(const typename Num<F>::lds_t *tile, int row0, int col0, const Weights<F> &weights, f32x16 &sum)
+// sum[m] += columns col0 + 32 m .. + 31 of the tile's rows row0 .. row0 + 31, each row times its weight.
+template <Form F, int DP, int ROWS, int BLOCKS>
+__device__ __forceinline__ void columns_times(const typename Num<F>::lds_t *tile, int row0, int col0, const Weights<F> &weights, f32x16 (&sum)[BLOCKS])
 {
-    constexpr int LP = row_elems_of(DP), PARTS = Num<F>::PARTS;
+    constexpr int LP = row_elems_of(DP), PARTS = Num<F>::PARTS, ROW_BYTES = LP * Num<F>::LS;
     const int lane = threadIdx.x & 63, half = lane >> 5;
     if constexpr (F != kF32) {
+        // A transposing read of 16 lanes takes 4 rows' 16 columns, 8 bytes a lane, and gives lane j column j of all 4.  Two make the 8 rows
+        // of a lane; the second's are 8 rows on, where chunks lie xor 2.
         typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-        const int j = lane & 15, row = row0 + 4 * half + (j >> 2), chunk = col0 / 8 + 2 * (lane >> 4 & 1) + (j >> 1 & 1), in = 4 * (j & 1);
+        const int j = lane & 15;
+        const uint32_t at = afresh(static_cast<uint32_t>((chunk_at<F, LP>(4 * half + (j >> 2), 2 * (lane >> 4 & 1) + (j >> 1 & 1)) + 4 * (j & 1)) * 2));
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            u32x4 a[PARTS];
+        for (int m = 0; m < BLOCKS; ++m) {
+            const uint32_t low_at = at ^ static_cast<uint32_t>(2 * (col0 + 32 * m)), high_at = low_at ^ 32;
 #pragma unroll
-            for (int q = 0; q < PARTS; ++q) {
-                const uint16_t *part = tile + q * ROWS * LP;
-                const s16x4 low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(part + chunk_at<F, LP>(row + 16 * t, chunk) + in));
-                const s16x4 high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(part + chunk_at<F, LP>(row + 16 * t + 8, chunk) + in));
-                a[q] = __builtin_bit_cast(u32x4, __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7));
+            for (int t = 0; t < 2; ++t) {
+                u32x4 a[PARTS];
+#pragma unroll
+                for (int q = 0; q < PARTS; ++q) {
+                    const char *part = reinterpret_cast<const char *>(tile) + (q * ROWS + row0 + 16 * t) * ROW_BYTES;
+                    const s16x4 low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(part + low_at));
+                    const s16x4 high = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(part + 8 * ROW_BYTES + high_at));
+                    a[q] = __builtin_bit_cast(u32x4, __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7));
+                }
+                if constexpr (F == kBf16) sum[m] = mfma_bf16(a[0], weights.w[0][t], sum[m]);
+                else
+#pragma unroll
+                    for (int n = 0; n < 6; ++n) sum[m] = mfma_bf16(a[kTileParts[n]], weights.w[kHeldParts[n]][t], sum[m]);
             }
-            if constexpr (F == kBf16) sum = mfma_bf16(a[0], weights.w[0][t], sum);
-            else
-#pragma unroll
-                for (int n = 0; n < 6; ++n) sum = mfma_bf16(a[kTileParts[n]], weights.w[kHeldParts[n]][t], sum);
         }
     } else {
-        const int col = col0 + (lane & 31);
+        // (row 8 g + 4 half + e: chunks lie xor (4 e + 2 g + half) % 16)
+        const uint32_t at = afresh(static_cast<uint32_t>(4 * half * ROW_BYTES + (((lane >> 2 & 7) ^ half) * 16) + (lane & 3) * 4));
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int row = row0 + 8 * (r >> 2) + 4 * half + (r & 3);
-            sum = __builtin_amdgcn_mfma_f32_32x32x2f32(tile[chunk_at<F, LP>(row, col >> 2) + (col & 3)], weights.w[r], sum, 0, 0, 0);
-        }
+        for (int m = 0; m < BLOCKS; ++m)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const int g = r >> 2, e = r & 3;
+                sum[m] = __builtin_amdgcn_mfma_f32_32x32x2f32(from_lds<float>(tile, (at ^ static_cast<uint32_t>(4 * (col0 + 32 * m)) ^ (16 * (4 * e + 2 * (g & 1)))) + (row0 + 8 * g + e) * ROW_BYTES),
+                                                              weights.w[r], sum[m], 0, 0, 0);
+            }
     }
 }
 
