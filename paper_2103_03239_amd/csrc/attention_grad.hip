@@ -17,7 +17,9 @@ namespace moshpit {
 namespace {
 
 constexpr int kThreads = 256, kWaves = 4, kColumns = 32 * kWaves;     // columns of a block: keys or queries
-constexpr int kStat = 32;                                // queries of a tile whose range of `first` is kept
+// Queries of a tile of keys_grad_kernel, whose range of `first` is kept.
+template <Form F, int DP> constexpr int query_rows() { return F == kBf16 && DP <= 64 ? 64 : 32; }
+int query_rows_of(int dtype, int depth) { return dtype != 0 && depth <= 64 ? 64 : 32; }
 
 struct Range {
     int32_t lo, hi;                      // smallest and largest `first` of the queries that hold a token; lo = INT32_MAX: none does
@@ -25,17 +27,17 @@ struct Range {
 
 // delta of a row's heads by 16 lanes each, 4 rows and heads a wave; the ranges by the blocks behind them.
 template <int DT>
-__global__ __launch_bounds__(kThreads) void delta_kernel(AttentionGradArgs a, float *__restrict__ delta, Range *__restrict__ ranges, int64_t delta_blocks)
+__global__ __launch_bounds__(kThreads) void delta_kernel(AttentionGradArgs a, float *__restrict__ delta, Range *__restrict__ ranges, int64_t delta_blocks, int32_t rows)
 {
     constexpr int ES = DT == 0 ? 4 : 2;
     const int lane = threadIdx.x & 15;
     if (blockIdx.x >= delta_blocks) {
-        const int64_t stats = (a.T + kStat - 1) / kStat, n = (blockIdx.x - delta_blocks) * (kThreads / 16) + threadIdx.x / 16;
+        const int64_t stats = (a.T + rows - 1) / rows, n = (blockIdx.x - delta_blocks) * (kThreads / 16) + threadIdx.x / 16;
         if (n >= a.N * stats) return;
         const int64_t peer = n / stats;
-        const int32_t begin = static_cast<int32_t>(n % stats) * kStat;
+        const int32_t begin = static_cast<int32_t>(n % stats) * rows;
         Range r{INT32_MAX, -1};
-        for (int k = lane; k < kStat; k += 16) {
+        for (int k = lane; k < rows; k += 16) {
             const int32_t i = begin + k, f = i < a.T ? a.first[peer * a.T + i] : -1;
             if (f < 0 || f > i) continue;
             r.lo = f < r.lo ? f : r.lo;
@@ -88,7 +90,8 @@ template <Form F, int DP, int SIMD, bool ASIDE, bool DIRECT>
 __global__ __launch_bounds__(kThreads, SIMD)
 void keys_grad_kernel(AttentionGradArgs a, KeysPlan plan, const float *__restrict__ delta, const Range *__restrict__ ranges, float *__restrict__ partials)
 {
-    constexpr int ES = Num<F>::ES, DT = Num<F>::DT, ROWS = kStat, DA = sum_depths<F, DP>(), BLOCKS = DA / 32, SLICES = DP / DA, ELEMS = tile_elems<F, DP>(ROWS);
+    constexpr int ES = Num<F>::ES, DT = Num<F>::DT, ROWS = query_rows<F, DP>(), DA = sum_depths<F, DP>(), BLOCKS = DA / 32, SLICES = DP / DA, ELEMS = tile_elems<F, DP>(ROWS);
+    constexpr uint64_t ALL = ROWS == 64 ? ~uint64_t(0) : 0xffffffffull;
     typedef Direct<(DIRECT ? DP : 128), ROWS, kThreads> Straight;
     typedef typename Num<F>::lds_t lds_t;
     __shared__ __attribute__((aligned(16))) lds_t q_even[ELEMS], q_odd[ELEMS], d_even[ELEMS], d_odd[ELEMS], aside[ASIDE ? tile_elems<F, DP>(kColumns) : 8];
@@ -133,7 +136,9 @@ void keys_grad_kernel(AttentionGradArgs a, KeysPlan plan, const float *__restric
     auto advance = [&]() -> bool {                                     // to the next item of this part; false: there is none
         for (;;) {
             if (item.tile >= 0 && ++item.member < group) {
-                if (plan.parts == 1 || turn++ % plan.parts == part) return true;
+                const bool mine = turn == part;
+                turn = turn + 1 == plan.parts ? 0 : turn + 1;
+                if (mine) return true;
                 continue;
             }
             while (left == 0) {
@@ -162,7 +167,7 @@ void keys_grad_kernel(AttentionGradArgs a, KeysPlan plan, const float *__restric
             Straight::request(d, static_cast<uint32_t>(a.dout_stride * ES), T - 1 - i0, d_into);
             __builtin_amdgcn_sched_barrier(0);
         }
-        live_next = __ballot(first_next >= 0) & 0xffffffffull;
+        live_next = __ballot(first_next >= 0) & ALL;
         if constexpr (!DIRECT) {
             q_next.load(q, a.q_stride * ES, live_next, a.depth, threadIdx.x);
             d_next.load(d, a.dout_stride * ES, live_next, a.depth, threadIdx.x);
@@ -171,7 +176,7 @@ void keys_grad_kernel(AttentionGradArgs a, KeysPlan plan, const float *__restric
     auto fill = [&](lds_t *q_into, lds_t *d_into, int into) __attribute__((always_inline)) {
         if constexpr (DIRECT) {
             Straight::wait();
-            if (live_next != 0xffffffffull) {
+            if (live_next != ALL) {
                 Straight::trim(live_next, q_into);
                 Straight::trim(live_next, d_into);
             }
@@ -190,14 +195,16 @@ void keys_grad_kernel(AttentionGradArgs a, KeysPlan plan, const float *__restric
         const bool more = advance();
         __syncthreads();
         if (more) request(q_into, d_into);
-        const int32_t i0 = it.tile * ROWS;
-        if (it.lo <= wave_begin + 31 && i0 + ROWS > wave_begin) {
-            f32x16 p = rows_times<F, DP, ROWS>(queries, 0, k), ds;
-            if constexpr (ASIDE) ds = rows_times<F, DP, ROWS>(douts, 0, Aside<F, DP>{aside + 32 * wave * row_elems_of(DP)});
-            else ds = rows_times<F, DP, ROWS>(douts, 0, v);
+#pragma unroll
+        for (int n = 0; n < ROWS / 32; ++n) {
+            const int32_t i0 = it.tile * ROWS + 32 * n;
+            if (it.lo > wave_begin + 31 || i0 + 32 <= wave_begin) continue;
+            f32x16 p = rows_times<F, DP, ROWS>(queries, 32 * n, k), ds;
+            if constexpr (ASIDE) ds = rows_times<F, DP, ROWS>(douts, 32 * n, Aside<F, DP>{aside + 32 * wave * row_elems_of(DP)});
+            else ds = rows_times<F, DP, ROWS>(douts, 32 * n, v);
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const f32x4 l = *reinterpret_cast<const f32x4 *>(&lses[now][8 * g + 4 * half]), d = *reinterpret_cast<const f32x4 *>(&deltas[now][8 * g + 4 * half]);
+                const f32x4 l = *reinterpret_cast<const f32x4 *>(&lses[now][32 * n + 8 * g + 4 * half]), d = *reinterpret_cast<const f32x4 *>(&deltas[now][32 * n + 8 * g + 4 * half]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     p[4 * g + e] = __builtin_amdgcn_exp2f(fmaf(p[4 * g + e], a.scale, -l[e]));
@@ -207,7 +214,7 @@ void keys_grad_kernel(AttentionGradArgs a, KeysPlan plan, const float *__restric
             if (i0 < wave_begin + 31 || it.hi > wave_begin) {
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
-                    const u32x4 f = *reinterpret_cast<const u32x4 *>(&firsts[now][8 * g + 4 * half]);
+                    const u32x4 f = *reinterpret_cast<const u32x4 *>(&firsts[now][32 * n + 8 * g + 4 * half]);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
                         const int32_t i = i0 + 8 * g + 4 * half + e, from = static_cast<int32_t>(f[e]);
@@ -219,9 +226,9 @@ void keys_grad_kernel(AttentionGradArgs a, KeysPlan plan, const float *__restric
             }
             Weights<F> w;
             w.take(p);
-            columns_times<F, DP, ROWS>(douts, 0, slice * DA, w, dv);
+            columns_times<F, DP, ROWS>(douts, 32 * n, slice * DA, w, dv);
             w.take(ds);
-            columns_times<F, DP, ROWS>(queries, 0, slice * DA, w, dk);
+            columns_times<F, DP, ROWS>(queries, 32 * n, slice * DA, w, dk);
         }
         if (more) fill(q_into, d_into, now ^ 1);
         return more;
@@ -400,17 +407,23 @@ void queries_grad_kernel(AttentionGradArgs a, uint32_t tiles, const float *__res
 int slices_of(int dtype, int depth) { return depth <= 128 ? 1 : dtype != 0 ? 2 : depth <= 192 ? 3 : 4; }
 
 int64_t tiles_of(const AttentionGradArgs &a) { return (a.T + kColumns - 1) / kColumns; }
-int64_t stats_of(const AttentionGradArgs &a) { return (a.T + kStat - 1) / kStat; }
+int64_t stats_of(const AttentionGradArgs &a, int dtype) { return (a.T + query_rows_of(dtype, a.depth) - 1) / query_rows_of(dtype, a.depth); }
+
+// Blocks of the kernels a compute unit, as their registers allow.
+int waves_of(int dtype, int depth) { return dtype == 0 || depth > 128 ? 1 : 2; }
 
 KeysPlan keys_plan(const AttentionGradArgs &a, int dtype, int compute_units)
 {
     KeysPlan p;
     p.tiles = static_cast<uint32_t>(tiles_of(a));
     const int64_t blocks = a.N * a.kv_heads * tiles_of(a) * slices_of(dtype, a.depth), group = a.heads / a.kv_heads;
-    // the parts that fill the chip, at least a tile of queries for all heads of the group, and 8 parts at most
-    int64_t parts = blocks > 0 ? 2 * int64_t(compute_units) / blocks : 1;
+    // A block goes over all queries that see its keys, the first keys' over the most, so there are to be twice as many as run at once, in up to 8
+    // parts of at least a tile of queries: 2 x 2 x 64 tiles of 128 keys, groups of 4 heads of 64, 8192 tokens: the backward pass in 657 us, with half as
+    // many parts in 816, with twice as many in 689; 4 x 4 x 32 of 128, groups of 2: 564, 710, 582.
+    const int64_t at_once = int64_t(compute_units) * (waves_of(dtype, a.depth));
+    int64_t parts = blocks > 0 ? (2 * at_once + blocks - 1) / blocks : 1;
     if (parts > 8) parts = 8;
-    if (parts > group * stats_of(a)) parts = group * stats_of(a);
+    if (parts > group * stats_of(a, dtype)) parts = group * stats_of(a, dtype);
     p.parts = static_cast<int32_t>(parts < 1 ? 1 : parts);
     return p;
 }
@@ -421,7 +434,7 @@ int64_t round_up(int64_t n) { return (n + 255) / 256 * 256; }
 
 bool attention_grad_fits(const AttentionGradArgs &a, int dtype)
 {
-    const int64_t delta_blocks = (a.N * a.T * a.heads + 15) / 16 + (a.N * stats_of(a) + 15) / 16;
+    const int64_t delta_blocks = (a.N * a.T * a.heads + 15) / 16 + (a.N * stats_of(a, dtype) + 15) / 16;
     return launchable(delta_blocks, kThreads) && launchable(a.N * a.heads * tiles_of(a) * slices_of(dtype, a.depth), kThreads);
 }
 
@@ -429,7 +442,7 @@ int64_t attention_grad_work_bytes(const AttentionGradArgs &a, int dtype, int com
 {
     const KeysPlan p = keys_plan(a, dtype, compute_units);
     const int64_t sums = p.parts > 1 ? 4 * p.parts * a.N * a.T * 2 * a.kv_heads * a.depth : 0;
-    return round_up(4 * a.N * a.heads * a.T) + round_up(int64_t(sizeof(Range)) * a.N * stats_of(a)) + sums;
+    return round_up(4 * a.N * a.heads * a.T) + round_up(int64_t(sizeof(Range)) * a.N * stats_of(a, dtype)) + sums;
 }
 
 hipError_t launch_attention_grad(const AttentionGradArgs &given, int dtype, void *work, int compute_units, hipStream_t stream)
@@ -440,9 +453,9 @@ hipError_t launch_attention_grad(const AttentionGradArgs &given, int dtype, void
     a.scale *= kLog2e;
     float *delta = static_cast<float *>(work);
     Range *ranges = reinterpret_cast<Range *>(static_cast<char *>(work) + round_up(4 * a.N * a.heads * a.T));
-    float *partials = reinterpret_cast<float *>(reinterpret_cast<char *>(ranges) + round_up(int64_t(sizeof(Range)) * a.N * stats_of(a)));
-    const int64_t delta_blocks = (a.N * a.T * a.heads + 15) / 16, range_blocks = (a.N * stats_of(a) + 15) / 16;
-    (dtype == 0 ? delta_kernel<0> : delta_kernel<1>)<<<static_cast<uint32_t>(delta_blocks + range_blocks), kThreads, 0, stream>>>(a, delta, ranges, delta_blocks);
+    float *partials = reinterpret_cast<float *>(reinterpret_cast<char *>(ranges) + round_up(int64_t(sizeof(Range)) * a.N * stats_of(a, dtype)));
+    const int64_t delta_blocks = (a.N * a.T * a.heads + 15) / 16, range_blocks = (a.N * stats_of(a, dtype) + 15) / 16;
+    (dtype == 0 ? delta_kernel<0> : delta_kernel<1>)<<<static_cast<uint32_t>(delta_blocks + range_blocks), kThreads, 0, stream>>>(a, delta, ranges, delta_blocks, query_rows_of(dtype, a.depth));
     const bool q_direct = direct_rows(a.q, a.q_stride) && direct_rows(a.dout, a.dout_stride), k_direct = direct_rows(a.k, a.k_stride) && direct_rows(a.v, a.v_stride);
     auto of = [&](auto form, auto dp) {
         constexpr Form F = decltype(form)::value;
