@@ -1654,7 +1654,7 @@ int moshpit_attention_cached(moshpit_ctx *h, const void *q_dev, int64_t q_row_st
     const CachedArgs a{static_cast<const char *>(q_dev), static_cast<const char *>(k_dev), static_cast<const char *>(v_dev), static_cast<char *>(out_dev), spans_dev, h->N,
                        n_keys, q_row_stride, k_row_stride, v_row_stride, out_row_stride, static_cast<int32_t>(sequences), static_cast<int32_t>(n_new), heads, kv_heads,
                        depth, scale, 0, 0};
-    const CachedPlan p = cached_plan(a, compute_units);
+    const CachedPlan p = cached_plan(a, dtype, compute_units);
     if (!p.fits) return fail(h, MOSHPIT_EINVAL, "%lld new tokens of %lld x %lld sequences are too many for one call", (long long)n_new, (long long)h->N, (long long)sequences);
     CHECK(reserve_work(h, p.work_bytes));
     HIP_TRY(h, launch_cached(a, dtype, p, h->work.block(), h->stream));

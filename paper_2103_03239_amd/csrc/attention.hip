@@ -21,9 +21,6 @@ namespace {
 constexpr int kThreads = 256, kWaves = 4, kQueries = 32 * kWaves;     // of a block
 constexpr float kSlack = 8.f;                            // by how many powers of two weights may pass 1
 
-// Waves of a block of cached_kernel: four where their tiles fit 64 KiB.
-template <Form F, int DP> constexpr int cached_waves() { return 4 * 2 * tile_bytes<F, DP>(32) <= 65536 ? 4 : 2; }
-
 // A wave's 32 queries (columns) and their sums so far.
 template <Form F, int DP> struct Queries {
     static constexpr int BLOCKS = DP / 32;
@@ -277,162 +274,194 @@ void attention_kernel(AttentionArgs a)
 }
 
 // Tokens' queries against a span of keys.  A block has one sequence, one head of keys and a share of the span; its waves take tiles of 32 keys in turn,
-// each its own in LDS, for the same 32 columns: the queries of the heads that share the keys, of the new tokens one after the other.
-template <Form F, int DP, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, F != kBf16 && DP > 64 ? 1 : 2)
+// for the same 32 columns: the queries of the heads that share the keys, of the new tokens one after the other.  Nobody waits for
+// anybody before the end.
+struct Share {
+    int64_t peer, row;                   // row: of this lane's query
+    int32_t split, kv_head, col_tile, seq, group, head, from, to, sees, all_see;      // keys of the share, by their number in the span
+    bool there;
+    const char *k_rows, *v_rows;         // key 0
+
+    __device__ __forceinline__ Share(const CachedArgs &a, int es)
+    {
+        uint32_t b = blockIdx.x;
+        kv_head = b % a.kv_heads;                                      // (neighbours in memory run at the same time)
+        b /= a.kv_heads;
+        col_tile = b % a.col_tiles;
+        b /= a.col_tiles;
+        seq = b % a.seqs;
+        b /= a.seqs;
+        peer = b % static_cast<uint32_t>(a.N);
+        split = static_cast<int32_t>(b / static_cast<uint32_t>(a.N));
+        group = a.heads / a.kv_heads;
+        const int32_t column = col_tile * 32 + (threadIdx.x & 31), token = column / group, n_keys = static_cast<int32_t>(a.n_keys);
+        head = kv_head * group + column - token * group;
+        there = token < a.fresh;
+        row = (peer * a.seqs + seq) * a.fresh + token;
+        int32_t begin = a.spans[2 * (peer * a.seqs + seq)], end = a.spans[2 * (peer * a.seqs + seq) + 1];
+        begin = begin < 0 ? 0 : begin > n_keys ? n_keys : begin;
+        end = end > n_keys ? n_keys : end;
+        const int32_t count = end > begin ? end - begin : 0;
+        const int32_t each = static_cast<int32_t>((count + 32u * kWaves * a.splits - 1) / (32u * kWaves * a.splits)) * (32 * kWaves);
+        from = split * each;
+        to = int64_t(split + 1) * each < count ? (split + 1) * each : count;
+        sees = there ? count - (a.fresh - 1 - token) : 0;             // how many of the span's keys this query does
+        all_see = count - (a.fresh - 1);
+        k_rows = a.k + ((peer * a.n_keys + begin) * a.k_stride + int64_t(kv_head) * a.depth) * es;
+        v_rows = a.v + ((peer * a.n_keys + begin) * a.v_stride + int64_t(kv_head) * a.depth) * es;
+    }
+    // Scores of keys j0 .. j0 + 31 that the queries do not see become -inf.
+    __device__ __forceinline__ void mask(f32x16 &s, int32_t j0) const
+    {
+        if (j0 + 32 <= to && j0 + 32 <= all_see) return;
+        const int32_t seen = (sees < to ? sees : to) - j0 - 4 * (threadIdx.x >> 5 & 1);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = 8 * (r >> 2) + (r & 3) < seen ? s[r] : -INFINITY;
+    }
+};
+
+// A wave has one tile in LDS, keys and values by turns, and the one after it on its way in registers.  (Four tiles a wave, straight into LDS, bring
+// nothing: 4 x 8 sequences of up to 16384, 4 heads of keys of 128 in bfloat16, in 155 us against 147.  Nor do equal shares of all sequences' keys, whatever
+// their lengths: 141 us, and 33 against 23 for two sequences of 16000 and one head of keys.)
+template <Form F, int DP, int SIMD>
+__global__ __launch_bounds__(kThreads, SIMD)
 void cached_kernel(CachedArgs a, float *__restrict__ partials)
 {
     constexpr int ES = Num<F>::ES, DT = Num<F>::DT, BLOCKS = DP / 32, ELEMS = tile_elems<F, DP>(32);
     typedef typename Num<F>::lds_t lds_t;
-    __shared__ __attribute__((aligned(16))) lds_t all[WAVES][2 * ELEMS];
-    __shared__ float tops[WAVES][32], totals[WAVES][32];
-
-    uint32_t b = die_run(blockIdx.x, gridDim.x);
-    const int32_t split = b % a.splits;
-    b /= a.splits;
-    const int32_t col_tile = b % a.col_tiles;
-    b /= a.col_tiles;
-    const int32_t kv_head = b % a.kv_heads;
-    b /= a.kv_heads;
-    const int32_t seq = b % a.seqs, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
-    const int64_t peer = b / a.seqs;
-    const int32_t group = a.heads / a.kv_heads, column = col_tile * 32 + (lane & 31), token = column / group, head = kv_head * group + column % group;
-    const bool there = token < a.fresh;
-    const int32_t n_keys = static_cast<int32_t>(a.n_keys);
-    int32_t begin = a.spans[2 * (peer * a.seqs + seq)], end = a.spans[2 * (peer * a.seqs + seq) + 1];
-    begin = begin < 0 ? 0 : begin > n_keys ? n_keys : begin;
-    end = end > n_keys ? n_keys : end;
-    const int32_t count = end > begin ? end - begin : 0;
-    const int32_t each = static_cast<int32_t>((count + 32u * WAVES * a.splits - 1) / (32u * WAVES * a.splits)) * (32 * WAVES);
-    const int32_t to = int64_t(split + 1) * each < count ? (split + 1) * each : count;    // (keys by their number in the span)
-    const int32_t sees = there ? count - (a.fresh - 1 - token) : 0;                       // how many of them this query does
-    const int32_t all_see = count - (a.fresh - 1);
-
-    Queries<F, DP> x;
-    const int64_t row = (peer * a.seqs + seq) * a.fresh + token;
-    x.q.load(a.q + (row * a.q_stride + int64_t(head) * a.depth) * ES, there, a.depth);
-    x.clear();
-    const char *k_rows = a.k + ((peer * a.n_keys + begin) * a.k_stride + int64_t(kv_head) * a.depth) * ES;
-    const char *v_rows = a.v + ((peer * a.n_keys + begin) * a.v_stride + int64_t(kv_head) * a.depth) * ES;
+    __shared__ __attribute__((aligned(16))) lds_t tiles[kWaves][ELEMS];
+    __shared__ float tops[kWaves][32], totals[kWaves][32], block_top[32], block_total[32];
+    const Share share(a, ES);
+    const int32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int64_t k_bytes = a.k_stride * ES, v_bytes = a.v_stride * ES;
-    lds_t *keys = all[wave], *values = keys + ELEMS;
-    auto live_of = [&](int32_t at) { return at + 32 <= to ? 0xffffffffull : (uint64_t(1) << (to - at)) - 1; };
-    int32_t at = split * each + 32 * wave;
-    Staged<F, DP, 32, 64> k_next, v_next;
-    if (at < to) {
-        k_next.load(k_rows + at * k_bytes, k_bytes, live_of(at), a.depth, lane);
-        v_next.load(v_rows + at * v_bytes, v_bytes, live_of(at), a.depth, lane);
-    }
-    auto settle = [] {                                                 // LDS of a wave: what was written before is read behind it
+    lds_t *tile = tiles[wave];
+    auto live_of = [&](int32_t at) { return at + 32 <= share.to ? 0xffffffffull : (uint64_t(1) << (share.to - at)) - 1; };
+    Queries<F, DP> x;
+    int32_t at = share.from + 32 * wave;
+    Staged<F, DP, 32, 64> next;
+    if (at < share.to) next.load(share.k_rows + at * k_bytes, k_bytes, live_of(at), a.depth, lane);
+    x.q.load(a.q + (share.row * a.q_stride + int64_t(share.head) * a.depth) * ES, share.there, a.depth);
+    x.clear();
+    auto put = [&] {                                                   // into the wave's own tile: written behind what was read, read behind what is written
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        next.store(tile, lane);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
     };
-    for (; at < to; at += 32 * WAVES) {
-        settle();
-        k_next.store(keys, lane);
-        v_next.store(values, lane);
-        settle();
-        const int32_t next = at + 32 * WAVES;
-        if (next < to) {
-            k_next.load(k_rows + next * k_bytes, k_bytes, live_of(next), a.depth, lane);
-            v_next.load(v_rows + next * v_bytes, v_bytes, live_of(next), a.depth, lane);
-        }
+    for (; at < share.to; at += 32 * kWaves) {
+        put();
+        next.load(share.v_rows + at * v_bytes, v_bytes, live_of(at), a.depth, lane);
         f32x16 s[1];
-        x.template score<32>(keys, s);
-        if (at + 32 > to || at + 32 > all_see) {
-            const int32_t seen = (sees < to ? sees : to) - at - 4 * half;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[0][r] = 8 * (r >> 2) + (r & 3) < seen ? s[0][r] : -INFINITY;
-        }
+        x.template score<32>(tile, s);
+        share.mask(s[0], at);
         x.rescale(x.largest(s), a.scale);
-        x.template take<32>(s, a.scale, values);
+        Weights<F> w;
+        x.weigh(s[0], a.scale, w);
+        put();
+        const int32_t after = at + 32 * kWaves;
+        if (after < share.to) next.load(share.k_rows + after * k_bytes, k_bytes, live_of(after), a.depth, lane);
+        x.template add<32>(tile, 0, w);
     }
 
     // the waves' sums, in order
     x.total = halves_sum(x.total);
-    if (lane < 32) {
+    if (half == 0) {
         tops[wave][lane] = x.top;
         totals[wave][lane] = x.total;
     }
     __syncthreads();
     float top = tops[0][lane & 31], total = 0.f;
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) top = fmaxf(top, tops[w][lane & 31]);
+    for (int w = 1; w < kWaves; ++w) top = fmaxf(top, tops[w][lane & 31]);
     auto factor_of = [&](float t) { return t == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(t - top); };
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) total += totals[w][lane & 31] * factor_of(tops[w][lane & 31]);
+    for (int w = 0; w < kWaves; ++w) total += totals[w][lane & 31] * factor_of(tops[w][lane & 31]);
     const float factor = factor_of(x.top);
-    // a wave at a time adds its sums to block 32 * m of [depth][column] in LDS
-    float *joined = reinterpret_cast<float *>(all);
-    static_assert(sizeof(all) >= 32 * DP * sizeof(float));
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-        if (wave == w)
+    // Eight columns at a time, [wave][depth][9], in the place of the tiles (which no wave needs any more).
+    constexpr int SOME = 8, PLACE = SOME + 1;
+    float *joined = reinterpret_cast<float *>(tiles);
+    static_assert(sizeof(tiles) >= kWaves * DP * PLACE * sizeof(float));
+    const int32_t first = share.col_tile * 32, columns = a.fresh * share.group - first < 32 ? a.fresh * share.group - first : 32;
+    for (int32_t c0 = 0; c0 < columns; c0 += SOME) {
+        if (c0 > 0) __syncthreads();
+        const int32_t mine = (lane & 31) - c0;
+        if (mine >= 0 && mine < SOME)
 #pragma unroll
             for (int m = 0; m < BLOCKS; ++m)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    float *p = joined + (32 * m + 8 * (r >> 2) + 4 * half + (r & 3)) * 32 + (lane & 31);
-                    const float v = x.top == -INFINITY ? 0.f : x.sum[m][r] * factor;
-                    *p = w == 0 ? v : *p + v;
-                }
+                for (int r = 0; r < 16; ++r)
+                    joined[(wave * DP + 32 * m + 8 * (r >> 2) + 4 * half + (r & 3)) * PLACE + mine] = x.top == -INFINITY ? 0.f : x.sum[m][r] * factor;
+        if (c0 == 0 && wave == 0 && half == 0) {
+            block_top[lane] = top;
+            block_total[lane] = total;
+        }
         __syncthreads();
-    }
-        const int32_t columns = a.fresh * group - col_tile * 32 < 32 ? a.fresh * group - col_tile * 32 : 32;
-    for (int32_t n = threadIdx.x; n < columns * a.depth; n += 64 * WAVES) {
-        const int32_t c = n / a.depth, d = n % a.depth, t = (col_tile * 32 + c) / group, h = kv_head * group + (col_tile * 32 + c) % group;
-        const int64_t r = (peer * a.seqs + seq) * a.fresh + t;
-        const float v = joined[d * 32 + c];
-        if (a.splits == 1) {
-            float sum = 0.f, most = tops[0][c];
+        const int32_t some = columns - c0 < SOME ? columns - c0 : SOME;
+        for (int32_t n = threadIdx.x; n < some * a.depth; n += kThreads) {
+            const int32_t c = n / a.depth, d = n - c * a.depth, column = first + c0 + c, t = column / share.group, h = share.kv_head * share.group + column - t * share.group;
+            const int64_t r = (share.peer * a.seqs + share.seq) * a.fresh + t;
+            float v = joined[d * PLACE + c];
 #pragma unroll
-            for (int w = 1; w < WAVES; ++w) most = fmaxf(most, tops[w][c]);
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) sum += tops[w][c] == -INFINITY ? 0.f : totals[w][c] * __builtin_amdgcn_exp2f(tops[w][c] - most);
-            store_one<DT>(a.out + (r * a.out_stride + int64_t(h) * a.depth + d) * ES, most == -INFINITY ? 0.f : v / sum);
-        } else
-            partials[((r * a.heads + h) * a.splits + split) * (a.depth + 2) + 2 + d] = v;
+            for (int w = 1; w < kWaves; ++w) v += joined[(w * DP + d) * PLACE + c];
+            if (a.splits == 1) store_one<DT>(a.out + (r * a.out_stride + int64_t(h) * a.depth + d) * ES, block_top[c0 + c] == -INFINITY ? 0.f : v / block_total[c0 + c]);
+            else partials[((r * a.heads + h) * a.splits + share.split) * a.depth + d] = v;
+        }
     }
-    if (a.splits > 1 && wave == 0 && half == 0 && there) {
-        float *p = partials + ((row * a.heads + head) * a.splits + split) * (a.depth + 2);
+    if (a.splits > 1 && wave == 0 && half == 0 && share.there) {
+        const int64_t shares = a.N * a.seqs * a.fresh * a.heads * a.splits;
+        float *p = partials + shares * a.depth + (share.row * a.heads + share.head) * a.splits + share.split;
         p[0] = top;
-        p[1] = total;
+        p[shares] = total;
     }
 }
 
-// The shares of a span, in order: a wave has a query of a head.
+// The shares of a span, in order: a wave has a query of a head, a lane the top and total of one share (of several, where there are more than 64).
 template <int DT>
 __global__ __launch_bounds__(kThreads) void cached_join_kernel(CachedArgs a, const float *__restrict__ partials, int64_t rows)
 {
-    constexpr int ES = DT == 0 ? 4 : 2;
+    constexpr int ES = DT == 0 ? 4 : 2, MOST = 256 / 64;
     const int64_t n = int64_t(blockIdx.x) * kWaves + (threadIdx.x >> 6);
     if (n >= rows * a.heads) return;
-    const int64_t row = n / a.heads, head = n % a.heads;
+    const int64_t row = n / a.heads, head = n % a.heads, shares = rows * a.heads * a.splits;
     const int lane = threadIdx.x & 63;
-    const float *p = partials + n * a.splits * (a.depth + 2);
-    float top = -INFINITY;
-    for (int s = 0; s < a.splits; ++s) top = fmaxf(top, p[s * (a.depth + 2)]);
-    char *out = a.out + (row * a.out_stride + head * a.depth) * ES;
-    for (int d = lane; d < a.depth; d += 64) {
-        float sum = 0.f, total = 0.f;
-        for (int s = 0; s < a.splits; ++s) {
-            const float *q = p + s * (a.depth + 2);
-            if (q[0] == -INFINITY) continue;
-            const float f = __builtin_amdgcn_exp2f(q[0] - top);
-            total = fmaf(q[1], f, total);
-            sum = fmaf(q[2 + d], f, sum);
+    const float *tops = partials + shares * a.depth + n * a.splits, *totals = tops + shares, *sums = partials + n * a.splits * a.depth;
+    float top = -INFINITY, sum[MOST] = {}, total = 0.f;
+    for (int s = lane; s < a.splits; s += 64) top = fmaxf(top, tops[s]);
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
+    for (int s0 = 0; s0 < a.splits; s0 += 64) {
+        const int left = a.splits - s0 < 64 ? a.splits - s0 : 64;
+        float mine = -INFINITY, part = 0.f;
+        if (lane < left) {
+            mine = tops[s0 + lane];
+            part = totals[s0 + lane];
         }
-        store_one<DT>(out + d * ES, top == -INFINITY ? 0.f : sum / total);
+        const float factor = mine == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mine - top);
+        for (int s = 0; s < left; s += 4) {                            // four shares requested at a time
+            float v[4][MOST];
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int t = 0; t < MOST; ++t) v[u][t] = s + u < left && lane + 64 * t < a.depth ? sums[int64_t(s0 + s + u) * a.depth + lane + 64 * t] : 0.f;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const float f = __shfl(factor, (s + u) & 63, 64), p = __shfl(part, (s + u) & 63, 64);
+                if (s + u >= left) continue;
+                total = fmaf(p, f, total);
+#pragma unroll
+                for (int t = 0; t < MOST; ++t) sum[t] = fmaf(v[u][t], f, sum[t]);
+            }
+        }
     }
+    char *out = a.out + (row * a.out_stride + head * a.depth) * ES;
+#pragma unroll
+    for (int t = 0; t < MOST; ++t)
+        if (lane + 64 * t < a.depth) store_one<DT>(out + (lane + 64 * t) * ES, top == -INFINITY ? 0.f : sum[t] / total);
 }
 
 int64_t attention_blocks(const AttentionArgs &a) { return a.N * a.heads * ((a.T + kQueries - 1) / kQueries); }
 
-#ifndef P_ROWS
-#define P_ROWS 64
-#define P_SIMD 2
-#define P_J 2
-#endif
 }  // namespace
 
 bool attention_fits(const AttentionArgs &a) { return launchable(attention_blocks(a), kThreads); }
@@ -446,22 +475,29 @@ hipError_t launch_attention(AttentionArgs a, int dtype, hipStream_t stream)
     return by_depth(dtype, a.depth, [&](auto form, auto dp) {
         constexpr Form F = decltype(form)::value;
         constexpr int DP = decltype(dp)::value;
+        // bfloat16: two blocks of keys at a time (2 x 16 heads of 128, 8192 tokens: 430 us, one at a time 454), up to a depth of 64 one, with four waves a
+        // SIMD (16 x 8 heads of 64, 4096 tokens: 138 us, two at a time with three waves 150)
         if constexpr (F != kBf16) attention_kernel<F, DP, 32, 1, (DP > 64 ? 1 : 2), false><<<blocks, kThreads, 0, stream>>>(a);
         else if constexpr (DP > 128) attention_kernel<F, DP, 32, 1, 1, false><<<blocks, kThreads, 0, stream>>>(a);
-        else if (a.depth == DP && direct_rows(a.k, a.k_stride) && direct_rows(a.v, a.v_stride))
-            attention_kernel<F, DP, (DP <= 32 ? 64 : P_ROWS), P_J, P_SIMD, true><<<blocks, kThreads, 0, stream>>>(a);
-        else attention_kernel<F, DP, 64, 1, 2, false><<<blocks, kThreads, 0, stream>>>(a);
+        else {
+            constexpr int JOINT = DP <= 64 ? 1 : 2, SIMD = DP <= 64 ? 4 : 2;
+            if (a.depth == DP && direct_rows(a.k, a.k_stride) && direct_rows(a.v, a.v_stride)) attention_kernel<F, DP, 64, JOINT, SIMD, true><<<blocks, kThreads, 0, stream>>>(a);
+            else attention_kernel<F, DP, 64, JOINT, (DP <= 64 ? 3 : 2), false><<<blocks, kThreads, 0, stream>>>(a);
+        }
         return hipGetLastError();
     });
 }
 
-// Shares of a span: enough blocks for the chip, 512 keys each and more where the keys of a peer are even over its sequences.
-CachedPlan cached_plan(const CachedArgs &a, int compute_units)
+// Blocks of cached_kernel a compute unit, as its registers allow.
+constexpr int cached_waves(Form f, int dp) { return f == kBf16 && dp <= 128 ? 2 : 1; }
+
+// Shares of a span: twice the blocks that run at once, and 512 keys each and more where the keys of a peer are one sequence's.
+CachedPlan cached_plan(const CachedArgs &a, int dtype, int compute_units)
 {
     CachedPlan p;
     p.col_tiles = (a.fresh * (a.heads / a.kv_heads) + 31) / 32;
-    const int64_t blocks = a.N * a.seqs * a.kv_heads * p.col_tiles;
-    const int64_t most = blocks > 0 ? 4 * int64_t(compute_units) / blocks : 1, use = (a.n_keys + 511) / 512;
+    const int64_t blocks = a.N * a.seqs * a.kv_heads * p.col_tiles, at_once = int64_t(compute_units) * cached_waves(dtype == 0 ? kF32 : kBf16, a.depth);
+    const int64_t most = blocks > 0 ? 2 * at_once / blocks : 1, use = (a.n_keys + 511) / 512;
     const int64_t splits = most < use ? most : use;
     p.splits = static_cast<int32_t>(splits < 1 ? 1 : splits);
     p.work_bytes = p.splits > 1 ? 4 * a.N * a.seqs * a.fresh * a.heads * p.splits * (a.depth + 2) : 0;
@@ -479,13 +515,14 @@ hipError_t launch_cached(CachedArgs a, int dtype, const CachedPlan &p, void *wor
     float *partials = static_cast<float *>(work);
     const hipError_t e = by_depth(dtype, a.depth, [&](auto form, auto dp) {
         constexpr Form F = decltype(form)::value;
-        constexpr int DP = decltype(dp)::value, WAVES = cached_waves<F, DP>();
-        cached_kernel<F, DP, WAVES><<<static_cast<uint32_t>(a.N * a.seqs * a.kv_heads * p.col_tiles * p.splits), 64 * WAVES, 0, stream>>>(a, partials);
+        constexpr int DP = decltype(dp)::value;
+        const uint32_t blocks = static_cast<uint32_t>(a.N * a.seqs * a.kv_heads * p.col_tiles * p.splits);
+        cached_kernel<F, DP, cached_waves(F, DP)><<<blocks, kThreads, 0, stream>>>(a, partials);
         return hipGetLastError();
     });
     if (e != hipSuccess || p.splits == 1) return e;
-    const uint32_t blocks = static_cast<uint32_t>((rows * a.heads + kWaves - 1) / kWaves);
-    (dtype == 0 ? cached_join_kernel<0> : cached_join_kernel<1>)<<<blocks, kThreads, 0, stream>>>(a, partials, rows);
+    const uint32_t join_blocks = static_cast<uint32_t>((rows * a.heads + kWaves - 1) / kWaves);
+    (dtype == 0 ? cached_join_kernel<0> : cached_join_kernel<1>)<<<join_blocks, kThreads, 0, stream>>>(a, partials, rows);
     return hipGetLastError();
 }
 

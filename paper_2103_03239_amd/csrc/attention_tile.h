@@ -313,7 +313,7 @@ template <Form F, int DP, int ROWS, int THREADS> struct Staged {
 };
 
 // The same for bfloat16 rows of DP elements that are whole 16-byte vectors: from memory into LDS without passing through registers, a wave 1
-// KiB at a time: lane l's 16 bytes to where the wave's begin + 16 * l, so the lane reads the chunk that chunk_at() puts there.
+// KiB at a time (THREADS = 64: a tile of a wave's own): lane l's 16 bytes to where the wave's begin + 16 * l, so the lane reads the chunk that chunk_at() puts there.
 template <int DP, int ROWS, int THREADS> struct Direct {
     static constexpr int LP = row_elems_of(DP), CH = LP / 8, WAVES = THREADS / 64, EACH = 64 / CH, COUNT = ROWS / EACH / WAVES;      // rows of 1 KiB; KiB of a wave
     static_assert(COUNT >= 1 && ROWS % (EACH * WAVES) == 0);
@@ -322,7 +322,7 @@ template <int DP, int ROWS, int THREADS> struct Direct {
     __device__ __forceinline__ static void request(const char *rows, uint32_t row_bytes, int32_t last, uint16_t *tile)
     {
         typedef __attribute__((address_space(3))) uint16_t lds_u16;
-        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int lane = threadIdx.x & 63, wave = WAVES == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(rows), 0, 0xffffffffu, 0x00027000);
 #pragma unroll
         for (int n = 0; n < COUNT; ++n) {
@@ -334,7 +334,7 @@ template <int DP, int ROWS, int THREADS> struct Direct {
     // Behind a wait for all that was requested: rows whose bit in `live` is not set become zeros.
     __device__ __forceinline__ static void trim(uint64_t live, uint16_t *tile)
     {
-        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        const int lane = threadIdx.x & 63, wave = WAVES == 1 ? 0 : threadIdx.x >> 6;
 #pragma unroll
         for (int n = 0; n < COUNT; ++n) {
             const int begin = (wave * COUNT + n) * EACH;

@@ -137,7 +137,7 @@ struct CachedPlan {
     int64_t work_bytes;
     bool fits;
 };
-CachedPlan cached_plan(const CachedArgs &a, int compute_units);
+CachedPlan cached_plan(const CachedArgs &a, int dtype, int compute_units);
 hipError_t launch_cached(CachedArgs a, int dtype, const CachedPlan &p, void *work, hipStream_t stream);
 
 }  // namespace moshpit
