@@ -283,7 +283,7 @@ __global__ __launch_bounds__(kThreads) void keys_join_kernel(AttentionGradArgs a
 // ROWS keys a tile; SIMD, DIRECT as above.
 template <Form F, int DP, int ROWS, int SIMD, bool DIRECT>
 __global__ __launch_bounds__(kThreads, SIMD)
-void queries_grad_kernel(AttentionGradArgs a, uint32_t tiles, const float *__restrict__ delta)
+void queries_grad_kernel(AttentionGradArgs a, uint32_t tiles, float *__restrict__ delta)
 {
     constexpr int ES = Num<F>::ES, DT = Num<F>::DT, BLOCKS = DP / 32, ELEMS = tile_elems<F, DP>(ROWS);
     constexpr uint64_t ALL = ROWS == 64 ? ~uint64_t(0) : 0xffffffffull;
@@ -325,6 +325,7 @@ void queries_grad_kernel(AttentionGradArgs a, uint32_t tiles, const float *__res
     d.load(a.dout + ((row0 + i) * a.dout_stride + int64_t(head) * a.depth) * ES, there, a.depth);
     const int64_t n = (peer * a.heads + head) * a.T + i;
     const float lse = there ? a.lse[n] * kLog2e : INFINITY, off = there ? delta[n] : 0.f;
+    float drift = 0.f;
     f32x16 dq[BLOCKS] = {};
     const char *k_rows = a.k + (row0 * a.k_stride + int64_t(kv_head) * a.depth) * ES, *v_rows = a.v + (row0 * a.v_stride + int64_t(kv_head) * a.depth) * ES;
     const int64_t k_bytes = a.k_stride * ES, v_bytes = a.v_stride * ES;
@@ -384,6 +385,12 @@ void queries_grad_kernel(AttentionGradArgs a, uint32_t tiles, const float *__res
                 Weights<F> w;
                 w.take(ds);
                 columns_times<F, DP, ROWS>(keys, 32 * n, 0, w, dq);
+                if constexpr (F == kBf16) {                            // and what their rounding took off them
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) drift += ds[r];
+                    w.rest(ds);
+                    columns_times<F, DP, ROWS>(keys, 32 * n, 0, w, dq);
+                }
             }
             if (more) fill(live_next, k_into, v_into);
             live = live_next;
@@ -394,6 +401,10 @@ void queries_grad_kernel(AttentionGradArgs a, uint32_t tiles, const float *__res
             if (!step(k_even, v_even, k_odd, v_odd)) break;
             if (!step(k_odd, v_odd, k_even, v_even)) break;
         }
+    }
+    if constexpr (F == kBf16) {
+        drift = halves_sum(drift);
+        if (there && half == 0) delta[n] = off + drift;
     }
     if (i >= T) return;
     char *to_row = a.dq + ((row0 + i) * a.dq_stride + int64_t(head) * a.depth) * ES;
@@ -462,15 +473,15 @@ hipError_t launch_attention_grad(const AttentionGradArgs &given, int dtype, void
         constexpr int DP = decltype(dp)::value, DT = Num<F>::DT, SIMD = DP > 128 || F == kParts ? 1 : 2;
         constexpr bool ASIDE = F == kBf16 && DP == 128, STRAIGHT = F == kBf16 && DP > 32 && DP <= 128;
         const uint32_t key_blocks = static_cast<uint32_t>(a.N * a.kv_heads * p.tiles * p.parts) * (DP / sum_depths<F, DP>()), query_blocks = static_cast<uint32_t>(a.N * a.heads * p.tiles);
+        constexpr int ROWS = F == kBf16 && DP <= 128 ? 64 : 32;
+        if (STRAIGHT && a.depth == DP && k_direct) queries_grad_kernel<F, DP, ROWS, SIMD, STRAIGHT><<<query_blocks, kThreads, 0, stream>>>(a, p.tiles, delta);
+        else queries_grad_kernel<F, DP, ROWS, SIMD, false><<<query_blocks, kThreads, 0, stream>>>(a, p.tiles, delta);
         if (STRAIGHT && a.depth == DP && q_direct) keys_grad_kernel<F, DP, SIMD, ASIDE, STRAIGHT><<<key_blocks, kThreads, 0, stream>>>(a, p, delta, ranges, partials);
         else keys_grad_kernel<F, DP, SIMD, ASIDE, false><<<key_blocks, kThreads, 0, stream>>>(a, p, delta, ranges, partials);
         if (p.parts > 1) {
             const int64_t blocks = (a.N * a.T * 2 * a.kv_heads * a.depth + kThreads - 1) / kThreads;
             keys_join_kernel<DT><<<static_cast<uint32_t>(blocks < 4096 ? blocks : 4096), kThreads, 0, stream>>>(a, p.parts, partials);
         }
-        constexpr int ROWS = F == kBf16 && DP <= 128 ? 64 : 32;
-        if (STRAIGHT && a.depth == DP && k_direct) queries_grad_kernel<F, DP, ROWS, SIMD, STRAIGHT><<<query_blocks, kThreads, 0, stream>>>(a, p.tiles, delta);
-        else queries_grad_kernel<F, DP, ROWS, SIMD, false><<<query_blocks, kThreads, 0, stream>>>(a, p.tiles, delta);
         return hipGetLastError();
     };
     return by_depth(dtype, a.depth, of);
