@@ -139,7 +139,7 @@ void attention_kernel(AttentionArgs a)
 {
     constexpr int ES = Num<F>::ES, DT = Num<F>::DT, BLOCKS = DP / 32, N = JOINT, ELEMS = tile_elems<F, DP>(ROWS);
     constexpr uint64_t ALL = ROWS == 64 ? ~uint64_t(0) : 0xffffffffull;
-    typedef Direct<(DIRECT ? DP : 128), (DIRECT ? ROWS : 64), kThreads> Straight;
+    typedef Direct<(DIRECT ? F : kBf16), (DIRECT ? DP : 128), (DIRECT ? ROWS : 64), kThreads> Straight;
     typedef typename Num<F>::lds_t lds_t;
     // (four variables: an access to one does not wait for what is on its way into another)
     __shared__ __attribute__((aligned(16))) lds_t k_even[ELEMS], k_odd[ELEMS], v_even[ELEMS], v_odd[ELEMS];
@@ -186,15 +186,17 @@ void attention_kernel(AttentionArgs a)
     if (from <= to) {
         typename std::conditional<DIRECT, char, Staged<F, DP, ROWS, kThreads>>::type k_next, v_next;
         auto request = [&](auto &next, const char *rows, int64_t bytes, int32_t at, uint64_t live, lds_t *into) __attribute__((always_inline)) {
-            if constexpr (DIRECT) Straight::request(rows + at * bytes, static_cast<uint32_t>(bytes), T - 1 - at, into);
+            if constexpr (DIRECT) Straight::request(rows + at * bytes, static_cast<uint32_t>(bytes), T - 1 - at, a.depth / Num<F>::CE, into);
             else next.load(rows + at * bytes, bytes, live, a.depth, threadIdx.x);
         };
         auto put = [&](auto &next, lds_t *into) __attribute__((always_inline)) {
             if constexpr (!DIRECT) next.store(into, threadIdx.x);
         };
-        auto landed = [&](uint64_t v_live, lds_t *v_into) __attribute__((always_inline)) {      // (keys without a token get no weight, their values are zeros)
+        auto landed = [&](uint64_t v_live, lds_t *k_into, lds_t *v_into) __attribute__((always_inline)) {      // (keys without a token get no weight, their values are zeros)
             if constexpr (DIRECT) {
                 Straight::wait();
+                Straight::blank(a.depth / Num<F>::CE, k_into);
+                Straight::blank(a.depth / Num<F>::CE, v_into);
                 if (v_live != ALL) Straight::trim(v_live, v_into);
             }
         };
@@ -204,7 +206,7 @@ void attention_kernel(AttentionArgs a)
         request(v_next, v_rows, v_bytes, from, live, v_even);
         put(k_next, k_even);
         put(v_next, v_even);
-        landed(live, v_even);
+        landed(live, k_even, v_even);
         // The tile that begins at `at`; the next one goes into the other two.  False: it was the last.
         auto step = [&](const lds_t *keys, const lds_t *values, lds_t *k_into, lds_t *v_into) __attribute__((always_inline)) {
             __syncthreads();
@@ -241,7 +243,7 @@ void attention_kernel(AttentionArgs a)
             if (more) {
                 put(k_next, k_into);
                 put(v_next, v_into);
-                landed(live_next, v_into);
+                landed(live_next, k_into, v_into);
             }
             live = live_next;
             at += ROWS;
@@ -477,11 +479,14 @@ hipError_t launch_attention(AttentionArgs a, int dtype, hipStream_t stream)
         constexpr int DP = decltype(dp)::value;
         // bfloat16: two blocks of keys at a time (2 x 16 heads of 128, 8192 tokens: 430 us, one at a time 454), up to a depth of 64 one, with four waves a
         // SIMD (16 x 8 heads of 64, 4096 tokens: 138 us, two at a time with three waves 150)
-        if constexpr (F != kBf16) attention_kernel<F, DP, 32, 1, (DP > 64 ? 1 : 2), false><<<blocks, kThreads, 0, stream>>>(a);
-        else if constexpr (DP > 128) attention_kernel<F, DP, 32, 1, 1, false><<<blocks, kThreads, 0, stream>>>(a);
-        else {
+        const bool direct = F != kParts && direct_rows(a.k, a.k_stride, a.depth, dtype) && direct_rows(a.v, a.v_stride, a.depth, dtype);
+        if constexpr (F == kParts) attention_kernel<F, DP, 32, 1, (DP > 64 ? 1 : 2), false><<<blocks, kThreads, 0, stream>>>(a);
+        else if constexpr (DP > 128) {
+            if (direct) attention_kernel<F, DP, 32, 1, 1, true><<<blocks, kThreads, 0, stream>>>(a);
+            else attention_kernel<F, DP, 32, 1, 1, false><<<blocks, kThreads, 0, stream>>>(a);
+        } else {
             constexpr int JOINT = DP <= 64 ? 1 : 2, SIMD = DP <= 64 ? 4 : 2;
-            if (a.depth == DP && direct_rows(a.k, a.k_stride) && direct_rows(a.v, a.v_stride)) attention_kernel<F, DP, 64, JOINT, SIMD, true><<<blocks, kThreads, 0, stream>>>(a);
+            if (direct) attention_kernel<F, DP, 64, JOINT, SIMD, true><<<blocks, kThreads, 0, stream>>>(a);
             else attention_kernel<F, DP, 64, JOINT, (DP <= 64 ? 3 : 2), false><<<blocks, kThreads, 0, stream>>>(a);
         }
         return hipGetLastError();

@@ -92,7 +92,7 @@ void keys_grad_kernel(AttentionGradArgs a, KeysPlan plan, const float *__restric
 {
     constexpr int ES = Num<F>::ES, DT = Num<F>::DT, ROWS = query_rows<F, DP>(), DA = sum_depths<F, DP>(), BLOCKS = DA / 32, SLICES = DP / DA, ELEMS = tile_elems<F, DP>(ROWS);
     constexpr uint64_t ALL = ROWS == 64 ? ~uint64_t(0) : 0xffffffffull;
-    typedef Direct<(DIRECT ? DP : 128), ROWS, kThreads> Straight;
+    typedef Direct<(DIRECT ? F : kBf16), (DIRECT ? DP : 128), ROWS, kThreads> Straight;
     typedef typename Num<F>::lds_t lds_t;
     __shared__ __attribute__((aligned(16))) lds_t q_even[ELEMS], q_odd[ELEMS], d_even[ELEMS], d_odd[ELEMS], aside[ASIDE ? tile_elems<F, DP>(kColumns) : 8];
     __shared__ __attribute__((aligned(16))) float lses[2][ROWS], deltas[2][ROWS];
@@ -163,8 +163,8 @@ void keys_grad_kernel(AttentionGradArgs a, KeysPlan plan, const float *__restric
         lse_next = a.lse[n] * kLog2e;
         delta_next = delta[n];
         if constexpr (DIRECT) {
-            Straight::request(q, static_cast<uint32_t>(a.q_stride * ES), T - 1 - i0, q_into);
-            Straight::request(d, static_cast<uint32_t>(a.dout_stride * ES), T - 1 - i0, d_into);
+            Straight::request(q, static_cast<uint32_t>(a.q_stride * ES), T - 1 - i0, a.depth / Num<F>::CE, q_into);
+            Straight::request(d, static_cast<uint32_t>(a.dout_stride * ES), T - 1 - i0, a.depth / Num<F>::CE, d_into);
             __builtin_amdgcn_sched_barrier(0);
         }
         live_next = __ballot(first_next >= 0) & ALL;
@@ -176,6 +176,8 @@ void keys_grad_kernel(AttentionGradArgs a, KeysPlan plan, const float *__restric
     auto fill = [&](lds_t *q_into, lds_t *d_into, int into) __attribute__((always_inline)) {
         if constexpr (DIRECT) {
             Straight::wait();
+            Straight::blank(a.depth / Num<F>::CE, q_into);
+            Straight::blank(a.depth / Num<F>::CE, d_into);
             if (live_next != ALL) {
                 Straight::trim(live_next, q_into);
                 Straight::trim(live_next, d_into);
@@ -287,7 +289,7 @@ void queries_grad_kernel(AttentionGradArgs a, uint32_t tiles, float *__restrict_
 {
     constexpr int ES = Num<F>::ES, DT = Num<F>::DT, BLOCKS = DP / 32, ELEMS = tile_elems<F, DP>(ROWS);
     constexpr uint64_t ALL = ROWS == 64 ? ~uint64_t(0) : 0xffffffffull;
-    typedef Direct<(DIRECT ? DP : 128), (DIRECT ? ROWS : 64), kThreads> Straight;
+    typedef Direct<(DIRECT ? F : kBf16), (DIRECT ? DP : 128), (DIRECT ? ROWS : 64), kThreads> Straight;
     typedef typename Num<F>::lds_t lds_t;
     __shared__ __attribute__((aligned(16))) lds_t k_even[ELEMS], k_odd[ELEMS], v_even[ELEMS], v_odd[ELEMS];
     __shared__ int32_t ends[2][kWaves];
@@ -335,8 +337,8 @@ void queries_grad_kernel(AttentionGradArgs a, uint32_t tiles, float *__restrict_
         typename std::conditional<DIRECT, char, Staged<F, DP, ROWS, kThreads>>::type k_next, v_next;
         auto request = [&](int32_t at, uint64_t live, lds_t *k_into, lds_t *v_into) __attribute__((always_inline)) {
             if constexpr (DIRECT) {
-                Straight::request(k_rows + at * k_bytes, static_cast<uint32_t>(k_bytes), T - 1 - at, k_into);
-                Straight::request(v_rows + at * v_bytes, static_cast<uint32_t>(v_bytes), T - 1 - at, v_into);
+                Straight::request(k_rows + at * k_bytes, static_cast<uint32_t>(k_bytes), T - 1 - at, a.depth / Num<F>::CE, k_into);
+                Straight::request(v_rows + at * v_bytes, static_cast<uint32_t>(v_bytes), T - 1 - at, a.depth / Num<F>::CE, v_into);
             } else {
                 k_next.load(k_rows + at * k_bytes, k_bytes, live, a.depth, threadIdx.x);
                 v_next.load(v_rows + at * v_bytes, v_bytes, live, a.depth, threadIdx.x);
@@ -345,6 +347,8 @@ void queries_grad_kernel(AttentionGradArgs a, uint32_t tiles, float *__restrict_
         auto fill = [&](uint64_t live, lds_t *k_into, lds_t *v_into) __attribute__((always_inline)) {
             if constexpr (DIRECT) {
                 Straight::wait();
+                Straight::blank(a.depth / Num<F>::CE, k_into);
+                Straight::blank(a.depth / Num<F>::CE, v_into);
                 if (live != ALL) Straight::trim(live, k_into);         // (values without a token meet a weight that is taken as 0)
             } else {
                 k_next.store(k_into, threadIdx.x);
@@ -467,16 +471,17 @@ hipError_t launch_attention_grad(const AttentionGradArgs &given, int dtype, void
     float *partials = reinterpret_cast<float *>(reinterpret_cast<char *>(ranges) + round_up(int64_t(sizeof(Range)) * a.N * stats_of(a, dtype)));
     const int64_t delta_blocks = (a.N * a.T * a.heads + 15) / 16, range_blocks = (a.N * stats_of(a, dtype) + 15) / 16;
     (dtype == 0 ? delta_kernel<0> : delta_kernel<1>)<<<static_cast<uint32_t>(delta_blocks + range_blocks), kThreads, 0, stream>>>(a, delta, ranges, delta_blocks, query_rows_of(dtype, a.depth));
-    const bool q_direct = direct_rows(a.q, a.q_stride) && direct_rows(a.dout, a.dout_stride), k_direct = direct_rows(a.k, a.k_stride) && direct_rows(a.v, a.v_stride);
+    const bool q_direct = direct_rows(a.q, a.q_stride, a.depth, dtype) && direct_rows(a.dout, a.dout_stride, a.depth, dtype);
+    const bool k_direct = direct_rows(a.k, a.k_stride, a.depth, dtype) && direct_rows(a.v, a.v_stride, a.depth, dtype);
     auto of = [&](auto form, auto dp) {
         constexpr Form F = decltype(form)::value;
         constexpr int DP = decltype(dp)::value, DT = Num<F>::DT, SIMD = DP > 128 || F == kParts ? 1 : 2;
-        constexpr bool ASIDE = F == kBf16 && DP == 128, STRAIGHT = F == kBf16 && DP > 32 && DP <= 128;
+        constexpr bool ASIDE = F == kBf16 && DP == 128, STRAIGHT = F != kParts && DP > 32;
         const uint32_t key_blocks = static_cast<uint32_t>(a.N * a.kv_heads * p.tiles * p.parts) * (DP / sum_depths<F, DP>()), query_blocks = static_cast<uint32_t>(a.N * a.heads * p.tiles);
         constexpr int ROWS = F == kBf16 && DP <= 128 ? 64 : 32;
-        if (STRAIGHT && a.depth == DP && k_direct) queries_grad_kernel<F, DP, ROWS, SIMD, STRAIGHT><<<query_blocks, kThreads, 0, stream>>>(a, p.tiles, delta);
+        if (STRAIGHT && k_direct) queries_grad_kernel<F, DP, ROWS, SIMD, STRAIGHT><<<query_blocks, kThreads, 0, stream>>>(a, p.tiles, delta);
         else queries_grad_kernel<F, DP, ROWS, SIMD, false><<<query_blocks, kThreads, 0, stream>>>(a, p.tiles, delta);
-        if (STRAIGHT && a.depth == DP && q_direct) keys_grad_kernel<F, DP, SIMD, ASIDE, STRAIGHT><<<key_blocks, kThreads, 0, stream>>>(a, p, delta, ranges, partials);
+        if (STRAIGHT && q_direct) keys_grad_kernel<F, DP, SIMD, ASIDE, STRAIGHT><<<key_blocks, kThreads, 0, stream>>>(a, p, delta, ranges, partials);
         else keys_grad_kernel<F, DP, SIMD, ASIDE, false><<<key_blocks, kThreads, 0, stream>>>(a, p, delta, ranges, partials);
         if (p.parts > 1) {
             const int64_t blocks = (a.N * a.T * 2 * a.kv_heads * a.depth + kThreads - 1) / kThreads;

@@ -323,39 +323,57 @@ template <Form F, int DP, int ROWS, int THREADS> struct Staged {
     }
 };
 
-// The same for bfloat16 rows of DP elements that are whole 16-byte vectors: from memory into LDS without passing through registers, a wave 1
-// KiB at a time (THREADS = 64: a tile of a wave's own): lane l's 16 bytes to where the wave's begin + 16 * l, so the lane reads the chunk that chunk_at() puts there.
-template <int DP, int ROWS, int THREADS> struct Direct {
-    static constexpr int LP = row_elems_of(DP), CH = LP / 8, WAVES = THREADS / 64, EACH = 64 / CH, COUNT = ROWS / EACH / WAVES;      // rows of 1 KiB; KiB of a wave
+// The same for rows that are whole 16-byte vectors (`chunks` of them), in the type that LDS has them in: from memory into LDS without passing through
+// registers, a wave 1 KiB at a time (THREADS = 64: a tile of a wave's own): lane l's 16 bytes to where the wave's begin + 16 * l, so the lane
+// reads the chunk that chunk_at() puts there.
+template <Form F, int DP, int ROWS, int THREADS> struct Direct {
+    static_assert(F != kParts);
+    typedef typename Num<F>::lds_t lds_t;
+    static constexpr int CE = Num<F>::CE, LP = row_elems_of(DP), CH = LP / CE, WAVES = THREADS / 64, EACH = 64 / CH, COUNT = ROWS / EACH / WAVES;      // rows of 1 KiB; KiB of a wave
     static_assert(COUNT >= 1 && ROWS % (EACH * WAVES) == 0);
 
     // Rows 0 .. last of the tile are there to be read; what is in the place of further ones is any row.
-    __device__ __forceinline__ static void request(const char *rows, uint32_t row_bytes, int32_t last, uint16_t *tile)
+    __device__ __forceinline__ static void request(const char *rows, uint32_t row_bytes, int32_t last, int32_t chunks, lds_t *tile)
     {
-        typedef __attribute__((address_space(3))) uint16_t lds_u16;
+        typedef __attribute__((address_space(3))) lds_t to_lds_t;
         const int lane = threadIdx.x & 63, wave = WAVES == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(rows), 0, 0xffffffffu, 0x00027000);
 #pragma unroll
         for (int n = 0; n < COUNT; ++n) {
             const int begin = (wave * COUNT + n) * EACH, row = begin + lane / CH, chunk = (lane % CH) ^ chunk_shift<CH>(row);
-            const uint32_t at = static_cast<uint32_t>(row < last ? row : last) * row_bytes + (DP == LP || chunk < DP / 8 ? chunk * 16 : 0);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_u16 *)(tile + begin * LP), 16, at, 0, 0, 0);
+            const uint32_t at = static_cast<uint32_t>(row < last ? row : last) * row_bytes + (chunk < chunks ? chunk * 16 : 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (to_lds_t *)(tile + begin * LP), 16, at, 0, 0, 0);
         }
     }
-    // Behind a wait for all that was requested: rows whose bit in `live` is not set become zeros.
-    __device__ __forceinline__ static void trim(uint64_t live, uint16_t *tile)
+    // Behind a wait for all that was requested: what is behind the rows' chunks becomes zeros.
+    __device__ __forceinline__ static void blank(int32_t chunks, lds_t *tile)
+    {
+        if (chunks == DP / CE) return;
+        const int lane = threadIdx.x & 63, wave = WAVES == 1 ? 0 : threadIdx.x >> 6;
+#pragma unroll
+        for (int n = 0; n < COUNT; ++n) {
+            const int begin = (wave * COUNT + n) * EACH, chunk = (lane % CH) ^ chunk_shift<CH>(begin + lane / CH);
+            if (chunk >= chunks && chunk < DP / CE) *reinterpret_cast<u32x4 *>(tile + begin * LP + lane * CE) = u32x4{0, 0, 0, 0};
+        }
+    }
+    // And rows whose bit in `live` is not set.
+    __device__ __forceinline__ static void trim(uint64_t live, lds_t *tile)
     {
         const int lane = threadIdx.x & 63, wave = WAVES == 1 ? 0 : threadIdx.x >> 6;
 #pragma unroll
         for (int n = 0; n < COUNT; ++n) {
             const int begin = (wave * COUNT + n) * EACH;
-            if ((live >> (begin + lane / CH) & 1) == 0) *reinterpret_cast<u32x4 *>(tile + begin * LP + lane * 8) = u32x4{0, 0, 0, 0};
+            if ((live >> (begin + lane / CH) & 1) == 0) *reinterpret_cast<u32x4 *>(tile + begin * LP + lane * CE) = u32x4{0, 0, 0, 0};
         }
     }
     __device__ __forceinline__ static void wait() { __builtin_amdgcn_s_waitcnt(0x0f70); }              // vmcnt(0)
 };
-// Whether a matrix's rows can be read so: whole vectors, and a tile's offsets below 2^31.
-inline bool direct_rows(const void *p, int64_t stride) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % 8 == 0 && stride <= (int64_t(1) << 23); }
+// Whether a matrix's heads can be read so: whole vectors, and a tile's offsets below 2^31.
+inline bool direct_rows(const void *p, int64_t stride, int depth, int dtype)
+{
+    const int each = dtype == 0 ? 4 : 8;
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && stride % each == 0 && depth % each == 0 && stride <= (int64_t(1) << 22);
+}
 
 // Which tile of which peer's head block number `block` takes.  Tiles with the most work come first for all peers and heads (a peer's sequences may
 // be longer than another's, so none is left to a single die), and a tile's blocks of the query heads that share keys go to the

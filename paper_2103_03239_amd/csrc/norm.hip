@@ -428,12 +428,15 @@ Parts parts_of(int64_t N, int64_t T, int slots, int64_t blocks)
     return Parts{each, T > 0 ? (T + each - 1) / each : 1};
 }
 int slots_of(const Shape &s) { return s.lanes >= kBlock ? 1 : kBlock / s.lanes; }
-int64_t blocks_wanted(int compute_units, const Shape &s) { return int64_t(compute_units) * (s.lanes > kBlock ? 4 : 8); }
+// Blocks a compute unit.  A block reads its gain once: 16 x 4096 rows of 4096 in bfloat16 with a binary32 gain, residual and 8-bit output (and its
+// restoring) in 546 us, with 8 blocks in 630, with 256 in 565.  In the backward pass it leaves its sums, too: 411 us with 8, 443 with 32.
+int64_t blocks_wanted(int compute_units, const Shape &s) { return int64_t(compute_units) * (s.lanes > kBlock ? 4 : 64); }
+int64_t grad_blocks_wanted(int compute_units, const Shape &s) { return int64_t(compute_units) * (s.lanes > kBlock ? 4 : 8); }
 Parts grad_parts(int64_t N, int64_t T, int64_t width, int compute_units)
 {
     if (width > kMostHeld) return parts_of(N, T, 1, 2 * compute_units / ((width + kBlock - 1) / kBlock) + 1);
     const Shape s = shape_of(width);
-    return parts_of(N, T, slots_of(s), blocks_wanted(compute_units, s));
+    return parts_of(N, T, slots_of(s), grad_blocks_wanted(compute_units, s));
 }
 
 template <typename Go> hipError_t by_shape(const Shape &s, Go go)
