@@ -11,7 +11,7 @@ An iteration draws sequences, samples an action at every place, rewards the one 
 place only learns by attention), and takes a few steps on that sample: forward pass with the layers' inputs saved in 8 bits, clipped
 policy loss, backward pass into the rows of G, then one averaging round.
 
-    python examples/block_step.py [--iterations 40]
+    python examples/block_step.py [--iterations 80]
 """
 from __future__ import annotations
 
@@ -33,14 +33,14 @@ from paper_2103_03239_amd import binding  # noqa: E402
 class Sizes:
     M: int = 4
     d: int = 2
-    vocab: int = 32
+    vocab: int = 8
     width: int = 64
     heads: int = 4
     kv_heads: int = 2
     depth: int = 16
     hidden: int = 128
-    tokens: int = 256                  # places of a peer in an iteration
-    dropout: float = 0.05
+    tokens: int = 512                  # places of a peer in an iteration
+    dropout: float = 0.02
 
     @property
     def N(self) -> int:
@@ -148,7 +148,7 @@ def sequences(sizes: Sizes, rng, device):
     return tokens, first
 
 
-def train(sizes: Sizes, iterations: int, steps: int = 4, gamma: float = 0.1, absent: float = 0.1, seed: int = 0, say=print):
+def train(sizes: Sizes, iterations: int, steps: int = 4, gamma: float = 0.2, absent: float = 0.1, seed: int = 0, say=print):
     """Rewards per iteration (mean over the peers) and the peers' distortion at the end."""
     p = Peers(sizes, seed)
     s, dev = sizes, p.X.device
@@ -177,6 +177,6 @@ def train(sizes: Sizes, iterations: int, steps: int = 4, gamma: float = 0.1, abs
 
 if __name__ == "__main__":
     ap = argparse.ArgumentParser(description=__doc__.split("\n\n")[0])
-    ap.add_argument("--iterations", type=int, default=40)
+    ap.add_argument("--iterations", type=int, default=80)
     got, spread = train(Sizes(), ap.parse_args().iterations)
     print(f"reward {got[0]:.3f} at the start, {got[-1]:.3f} at the end; distortion of the peers {spread:.3g}")
