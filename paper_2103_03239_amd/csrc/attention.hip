@@ -139,10 +139,11 @@ void attention_kernel(AttentionArgs a)
 {
     constexpr int ES = Num<F>::ES, DT = Num<F>::DT, BLOCKS = DP / 32, N = JOINT, ELEMS = tile_elems<F, DP>(ROWS);
     constexpr uint64_t ALL = ROWS == 64 ? ~uint64_t(0) : 0xffffffffull;
+    constexpr bool TWO = F != kParts || DP <= 64;                      // two buffers of a tile; one where two blocks a compute unit are worth more
     typedef Direct<(DIRECT ? F : kBf16), (DIRECT ? DP : 128), (DIRECT ? ROWS : 64), kThreads> Straight;
     typedef typename Num<F>::lds_t lds_t;
     // (four variables: an access to one does not wait for what is on its way into another)
-    __shared__ __attribute__((aligned(16))) lds_t k_even[ELEMS], k_odd[ELEMS], v_even[ELEMS], v_odd[ELEMS];
+    __shared__ __attribute__((aligned(16))) lds_t k_even[ELEMS], k_odd[TWO ? ELEMS : 8], v_even[ELEMS], v_odd[TWO ? ELEMS : 8];
     __shared__ int32_t ends[2][kWaves];
 
     const int32_t group = a.heads / a.kv_heads, lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = lane >> 5;
@@ -241,6 +242,7 @@ void attention_kernel(AttentionArgs a)
                 x.template take<ROWS>(s, a.scale, values + 32 * n0 * row_elems_of(DP));
             }
             if (more) {
+                if constexpr (!TWO) __syncthreads();
                 put(k_next, k_into);
                 put(v_next, v_into);
                 landed(live_next, k_into, v_into);
@@ -250,8 +252,9 @@ void attention_kernel(AttentionArgs a)
             return more;
         };
         for (;;) {
-            if (!step(k_even, v_even, k_odd, v_odd)) break;
-            if (!step(k_odd, v_odd, k_even, v_even)) break;
+            if (!step(k_even, v_even, TWO ? k_odd : k_even, TWO ? v_odd : v_even)) break;
+            if constexpr (TWO)
+                if (!step(k_odd, v_odd, k_even, v_even)) break;
         }
     }
 
@@ -480,7 +483,7 @@ hipError_t launch_attention(AttentionArgs a, int dtype, hipStream_t stream)
         // bfloat16: two blocks of keys at a time (2 x 16 heads of 128, 8192 tokens: 430 us, one at a time 454), up to a depth of 64 one, with four waves a
         // SIMD (16 x 8 heads of 64, 4096 tokens: 138 us, two at a time with three waves 150)
         const bool direct = F != kParts && direct_rows(a.k, a.k_stride, a.depth, dtype) && direct_rows(a.v, a.v_stride, a.depth, dtype);
-        if constexpr (F == kParts) attention_kernel<F, DP, 32, 1, (DP > 64 ? 1 : 2), false><<<blocks, kThreads, 0, stream>>>(a);
+        if constexpr (F == kParts) attention_kernel<F, DP, 32, 1, 2, false><<<blocks, kThreads, 0, stream>>>(a);
         else if constexpr (DP > 128) {
             if (direct) attention_kernel<F, DP, 32, 1, 1, true><<<blocks, kThreads, 0, stream>>>(a);
             else attention_kernel<F, DP, 32, 1, 1, false><<<blocks, kThreads, 0, stream>>>(a);

@@ -25,54 +25,28 @@ struct Range {
     int32_t lo, hi;                      // smallest and largest `first` of the queries that hold a token; lo = INT32_MAX: none does
 };
 
-// delta of a row's heads by 16 lanes each, 4 rows and heads a wave; the ranges by the blocks behind them.
-template <int DT>
-__global__ __launch_bounds__(kThreads) void delta_kernel(AttentionGradArgs a, float *__restrict__ delta, Range *__restrict__ ranges, int64_t delta_blocks, int32_t rows)
+// The ranges, 16 lanes each.
+__global__ __launch_bounds__(kThreads) void ranges_kernel(AttentionGradArgs a, Range *__restrict__ ranges, int32_t rows)
 {
-    constexpr int ES = DT == 0 ? 4 : 2;
     const int lane = threadIdx.x & 15;
-    if (blockIdx.x >= delta_blocks) {
-        const int64_t stats = (a.T + rows - 1) / rows, n = (blockIdx.x - delta_blocks) * (kThreads / 16) + threadIdx.x / 16;
-        if (n >= a.N * stats) return;
-        const int64_t peer = n / stats;
-        const int32_t begin = static_cast<int32_t>(n % stats) * rows;
-        Range r{INT32_MAX, -1};
-        for (int k = lane; k < rows; k += 16) {
-            const int32_t i = begin + k, f = i < a.T ? a.first[peer * a.T + i] : -1;
-            if (f < 0 || f > i) continue;
-            r.lo = f < r.lo ? f : r.lo;
-            r.hi = f > r.hi ? f : r.hi;
-        }
-#pragma unroll
-        for (int off = 1; off < 16; off <<= 1) {
-            const int32_t lo = __shfl_xor(r.lo, off, 64), hi = __shfl_xor(r.hi, off, 64);
-            r.lo = lo < r.lo ? lo : r.lo;
-            r.hi = hi > r.hi ? hi : r.hi;
-        }
-        if (lane == 0) ranges[n] = r;
-        return;
-    }
-    const int64_t n = int64_t(blockIdx.x) * (kThreads / 16) + threadIdx.x / 16, row = n / a.heads, head = n % a.heads;
-    if (row >= a.N * a.T) return;
-    const char *out = a.out + (row * a.out_stride + head * a.depth) * ES, *dout = a.dout + (row * a.dout_stride + head * a.depth) * ES;
-    float sum = 0.f;
-    for (int at = lane * 8; at < a.depth; at += 128) {
-        float x[8], y[8];
-        if (at + 8 <= a.depth) {
-            load_elems<DT, 8>(out + at * ES, x);
-            load_elems<DT, 8>(dout + at * ES, y);
-        } else
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                x[k] = at + k < a.depth ? load_one<DT>(out + (at + k) * ES) : 0.f;
-                y[k] = at + k < a.depth ? load_one<DT>(dout + (at + k) * ES) : 0.f;
-            }
-#pragma unroll
-        for (int k = 0; k < 8; ++k) sum = fmaf(x[k], y[k], sum);
+    const int64_t stats = (a.T + rows - 1) / rows, n = int64_t(blockIdx.x) * (kThreads / 16) + threadIdx.x / 16;
+    if (n >= a.N * stats) return;
+    const int64_t peer = n / stats;
+    const int32_t begin = static_cast<int32_t>(n % stats) * rows;
+    Range r{INT32_MAX, -1};
+    for (int k = lane; k < rows; k += 16) {
+        const int32_t i = begin + k, f = i < a.T ? a.first[peer * a.T + i] : -1;
+        if (f < 0 || f > i) continue;
+        r.lo = f < r.lo ? f : r.lo;
+        r.hi = f > r.hi ? f : r.hi;
     }
 #pragma unroll
-    for (int off = 1; off < 16; off <<= 1) sum += __shfl_xor(sum, off, 64);
-    if (lane == 0) delta[(row / a.T * a.heads + head) * a.T + row % a.T] = sum;
+    for (int off = 1; off < 16; off <<= 1) {
+        const int32_t lo = __shfl_xor(r.lo, off, 64), hi = __shfl_xor(r.hi, off, 64);
+        r.lo = lo < r.lo ? lo : r.lo;
+        r.hi = hi > r.hi ? hi : r.hi;
+    }
+    if (lane == 0) ranges[n] = r;
 }
 
 // How a launch of the kernel for keys is cut: `parts` of the queries and heads that a block of keys meets, sums of a part apart, and
@@ -187,8 +161,8 @@ void keys_grad_kernel(AttentionGradArgs a, KeysPlan plan, const float *__restric
             d_next.store(d_into, threadIdx.x);
         }
         if (threadIdx.x < ROWS) {
-            lses[into][threadIdx.x] = first_next >= 0 ? lse_next : INFINITY;       // (a query without a token: weights of 0)
-            deltas[into][threadIdx.x] = first_next >= 0 ? delta_next : 0.f;
+            lses[into][threadIdx.x] = first_next >= 0 ? -lse_next : -INFINITY;     // (a query without a token: weights of 0)
+            deltas[into][threadIdx.x] = first_next >= 0 ? -delta_next : 0.f;
             firsts[into][threadIdx.x] = first_next;
         }
     };
@@ -202,15 +176,21 @@ void keys_grad_kernel(AttentionGradArgs a, KeysPlan plan, const float *__restric
             const int32_t i0 = it.tile * ROWS + 32 * n;
             if (it.lo > wave_begin + 31 || i0 + 32 <= wave_begin) continue;
             f32x16 p = rows_times<F, DP, ROWS>(queries, 32 * n, k), ds;
-            if constexpr (ASIDE) ds = rows_times<F, DP, ROWS>(douts, 32 * n, Aside<F, DP>{aside + 32 * wave * row_elems_of(DP)});
-            else ds = rows_times<F, DP, ROWS>(douts, 32 * n, v);
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {                              // (dp - delta: the sums begin with -delta)
+                const f32x4 d = *reinterpret_cast<const f32x4 *>(&deltas[now][32 * n + 8 * g + 4 * half]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) ds[4 * g + e] = d[e];
+            }
+            if constexpr (ASIDE) ds = rows_times<F, DP, ROWS>(douts, 32 * n, Aside<F, DP>{aside + 32 * wave * row_elems_of(DP)}, ds);
+            else ds = rows_times<F, DP, ROWS>(douts, 32 * n, v, ds);
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const f32x4 l = *reinterpret_cast<const f32x4 *>(&lses[now][32 * n + 8 * g + 4 * half]), d = *reinterpret_cast<const f32x4 *>(&deltas[now][32 * n + 8 * g + 4 * half]);
+                const f32x4 l = *reinterpret_cast<const f32x4 *>(&lses[now][32 * n + 8 * g + 4 * half]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    p[4 * g + e] = __builtin_amdgcn_exp2f(fmaf(p[4 * g + e], a.scale, -l[e]));
-                    ds[4 * g + e] = p[4 * g + e] * (ds[4 * g + e] - d[e]);
+                    p[4 * g + e] = __builtin_amdgcn_exp2f(fmaf(p[4 * g + e], a.scale, l[e]));
+                    ds[4 * g + e] *= p[4 * g + e];
                 }
             }
             if (i0 < wave_begin + 31 || it.hi > wave_begin) {
@@ -326,7 +306,9 @@ void queries_grad_kernel(AttentionGradArgs a, uint32_t tiles, float *__restrict_
     q.load(a.q + ((row0 + i) * a.q_stride + int64_t(head) * a.depth) * ES, there, a.depth);
     d.load(a.dout + ((row0 + i) * a.dout_stride + int64_t(head) * a.depth) * ES, there, a.depth);
     const int64_t n = (peer * a.heads + head) * a.T + i;
-    const float lse = there ? a.lse[n] * kLog2e : INFINITY, off = there ? delta[n] : 0.f;
+    const float lse = there ? a.lse[n] * kLog2e : INFINITY;
+    const float off = columns_dot<F, DP>(a.out + ((row0 + i) * a.out_stride + int64_t(head) * a.depth) * ES,
+                                         a.dout + ((row0 + i) * a.dout_stride + int64_t(head) * a.depth) * ES, there, a.depth);
     float drift = 0.f;
     f32x16 dq[BLOCKS] = {};
     const char *k_rows = a.k + (row0 * a.k_stride + int64_t(kv_head) * a.depth) * ES, *v_rows = a.v + (row0 * a.v_stride + int64_t(kv_head) * a.depth) * ES;
@@ -406,10 +388,8 @@ void queries_grad_kernel(AttentionGradArgs a, uint32_t tiles, float *__restrict_
             if (!step(k_odd, v_odd, k_even, v_even)) break;
         }
     }
-    if constexpr (F == kBf16) {
-        drift = halves_sum(drift);
-        if (there && half == 0) delta[n] = off + drift;
-    }
+    if constexpr (F == kBf16) drift = halves_sum(drift);
+    if (there && half == 0) delta[n] = off + drift;
     if (i >= T) return;
     char *to_row = a.dq + ((row0 + i) * a.dq_stride + int64_t(head) * a.depth) * ES;
 #pragma unroll
@@ -449,8 +429,7 @@ int64_t round_up(int64_t n) { return (n + 255) / 256 * 256; }
 
 bool attention_grad_fits(const AttentionGradArgs &a, int dtype)
 {
-    const int64_t delta_blocks = (a.N * a.T * a.heads + 15) / 16 + (a.N * stats_of(a, dtype) + 15) / 16;
-    return launchable(delta_blocks, kThreads) && launchable(a.N * a.heads * tiles_of(a) * slices_of(dtype, a.depth), kThreads);
+    return launchable((a.N * stats_of(a, dtype) + 15) / 16, kThreads) && launchable(a.N * a.heads * tiles_of(a) * slices_of(dtype, a.depth), kThreads);
 }
 
 int64_t attention_grad_work_bytes(const AttentionGradArgs &a, int dtype, int compute_units)
@@ -469,8 +448,7 @@ hipError_t launch_attention_grad(const AttentionGradArgs &given, int dtype, void
     float *delta = static_cast<float *>(work);
     Range *ranges = reinterpret_cast<Range *>(static_cast<char *>(work) + round_up(4 * a.N * a.heads * a.T));
     float *partials = reinterpret_cast<float *>(reinterpret_cast<char *>(ranges) + round_up(int64_t(sizeof(Range)) * a.N * stats_of(a, dtype)));
-    const int64_t delta_blocks = (a.N * a.T * a.heads + 15) / 16, range_blocks = (a.N * stats_of(a, dtype) + 15) / 16;
-    (dtype == 0 ? delta_kernel<0> : delta_kernel<1>)<<<static_cast<uint32_t>(delta_blocks + range_blocks), kThreads, 0, stream>>>(a, delta, ranges, delta_blocks, query_rows_of(dtype, a.depth));
+    ranges_kernel<<<static_cast<uint32_t>((a.N * stats_of(a, dtype) + 15) / 16), kThreads, 0, stream>>>(a, ranges, query_rows_of(dtype, a.depth));
     const bool q_direct = direct_rows(a.q, a.q_stride, a.depth, dtype) && direct_rows(a.dout, a.dout_stride, a.depth, dtype);
     const bool k_direct = direct_rows(a.k, a.k_stride, a.depth, dtype) && direct_rows(a.v, a.v_stride, a.depth, dtype);
     auto of = [&](auto form, auto dp) {

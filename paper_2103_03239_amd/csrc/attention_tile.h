@@ -145,7 +145,33 @@ template <Form F, int DP> struct Held {
     }
 };
 
-// The same out of LDS: the columns are rows 0 .. 31 of a tile.
+// The sum of products of two columns' elements (both halves' of the wave), in binary32.
+template <Form F, int DP> __device__ __forceinline__ float columns_dot(const char *a, const char *b, bool there, int depth)
+{
+    constexpr int CE = Num<F>::CE, ES = Num<F>::ES, DT = Num<F>::DT;
+    const int half = threadIdx.x >> 5 & 1;
+    float sum = 0.f;
+#pragma unroll
+    for (int s = 0; s < DP / (2 * CE); ++s) {
+        const int at = (2 * s + half) * CE;
+        if (!there || at >= depth) continue;
+        Unit<F> x, y;
+        x.load(a + at * ES, depth - at);
+        y.load(b + at * ES, depth - at);
+#pragma unroll
+        for (int q = 0; q < Unit<F>::WORDS; ++q)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t u = x.v[q][k], w = y.v[q][k];
+                if constexpr (DT == 0) sum = fmaf(__uint_as_float(u), __uint_as_float(w), sum);
+                else sum = fmaf(__uint_as_float(u & 0xffff0000u), __uint_as_float(w & 0xffff0000u), fmaf(__uint_as_float(u << 16), __uint_as_float(w << 16), sum));
+            }
+    }
+    const LanePair p = swap32(sum, sum);
+    return p.first + p.second;
+}
+
+// Held columns out of LDS: they are rows 0 .. 31 of a tile.
 template <Form F, int DP> struct Aside {
     const uint16_t *tile;                // (of one part: bfloat16)
 
@@ -180,13 +206,12 @@ template <Form F, int DP> __device__ __forceinline__ uint32_t lane_row()
     return afresh(static_cast<uint32_t>(chunk_at<F, row_elems_of(DP)>(row, half) * Num<F>::LS));
 }
 
-// Rows row0 .. row0 + 31 of the tile (ROWS rows a part) times the columns.
+// sum + rows row0 .. row0 + 31 of the tile (ROWS rows a part) times the columns.
 template <Form F, int DP, int ROWS>
-__device__ __forceinline__ f32x16 rows_times(const typename Num<F>::lds_t *tile, int row0, const Held<F, DP> &held)
+__device__ __forceinline__ f32x16 rows_times(const typename Num<F>::lds_t *tile, int row0, const Held<F, DP> &held, f32x16 sum = f32x16{})
 {
     constexpr int PARTS = Num<F>::PARTS, ROW_BYTES = row_elems_of(DP) * Num<F>::LS;
     const uint32_t at = lane_row<F, DP>();
-    f32x16 sum = {};
 #pragma unroll
     for (int s = 0; s < Held<F, DP>::COUNT; ++s) {
         u32x4 a[PARTS];
@@ -203,11 +228,10 @@ __device__ __forceinline__ f32x16 rows_times(const typename Num<F>::lds_t *tile,
     return sum;
 }
 template <Form F, int DP, int ROWS>
-__device__ __forceinline__ f32x16 rows_times(const uint16_t *tile, int row0, const Aside<F, DP> &aside)
+__device__ __forceinline__ f32x16 rows_times(const uint16_t *tile, int row0, const Aside<F, DP> &aside, f32x16 sum = f32x16{})
 {
     constexpr int ROW_BYTES = row_elems_of(DP) * 2;
     const uint32_t at = lane_row<F, DP>();
-    f32x16 sum = {};
 #pragma unroll
     for (int s = 0; s < DP / 16; ++s) sum = mfma_bf16(from_lds<u32x4>(tile, (at ^ (32 * s)) + row0 * ROW_BYTES), from_lds<u32x4>(aside.tile, at ^ (32 * s)), sum);
     return sum;
