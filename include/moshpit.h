@@ -428,7 +428,7 @@ int moshpit_dropout(moshpit_ctx *h, const void *x_dev, int32_t dtype, int64_t x_
  * kv_heads of them; query head a goes with key head floor(a / (heads / kv_heads)).  Row i * n_tokens + t is token t of peer i, whose n_tokens
  * places hold sequences one behind the other: first_dev, [N][n_tokens] int32, says for every token the first one that it
  * sees, as a rule the one its sequence begins with (a later one makes a window).  A number outside 0 .. t: a place
- * without a token, whose rows are not read.  Token t sees the tokens s with first[t] <= s <= t:
+ * without a token, whose rows may hold anything.  Token t sees the tokens s with first[t] <= s <= t:
  *   out[t] = sum over s of exp(scale * q[t] . k[s] - lse[t]) v[s],   lse[t] = log of the sum over s of exp(scale * q[t] . k[s]);
  * 0 for out and lse where there is no token.  Infinities and NaN reach no token that does not see them.  lse_dev: NULL, or
  * [N][heads][n_tokens] floats, which the backward pass takes.  Weights are rounded to bfloat16 for their product with bfloat16 values; all else
@@ -438,8 +438,9 @@ int moshpit_attention(moshpit_ctx *h, const void *q_dev, int64_t q_row_stride, c
                       int32_t depth, float scale, void *out_dev, int64_t out_row_stride, float *lse_dev);
 
 /* Its backward pass: the gradients of queries, keys and values (summed over the query heads that share them) for the gradient
- * dout of out; out and lse as moshpit_attention left them.  Zeros where there is no token.  A product of an infinity or a NaN with
- * a weight of 0 counts here: a peer's gradients are numbers where its rows with tokens are. */
+ * dout of out; out and lse as moshpit_attention left them.  Zeros where there is no token, whose rows may hold anything here too; but an infinity or
+ * a NaN in a row with a token may make gradients of the same peer's other sequences NaN (its products with weights of 0 count).  The gradients must not
+ * overlap each other or what is read. */
 int moshpit_attention_grad(moshpit_ctx *h, const void *dout_dev, int64_t dout_row_stride, const void *q_dev, int64_t q_row_stride, const void *k_dev,
                            int64_t k_row_stride, const void *v_dev, int64_t v_row_stride, const void *out_dev, int64_t out_row_stride, int32_t dtype,
                            const float *lse_dev, const int32_t *first_dev, int64_t n_tokens, int32_t heads, int32_t kv_heads, int32_t depth, float scale,
@@ -449,7 +450,8 @@ int moshpit_attention_grad(moshpit_ctx *h, const void *dout_dev, int64_t dout_ro
  * new ones' included.  Queries and outputs: row (i * sequences + s) * n_new + b for new token b of sequence s of peer i.  Keys and
  * values: n_keys rows a peer; spans_dev, [N][sequences][2] int32: the sequence's rows are spans[..][0] .. spans[..][1] - 1 of them (cut to
  * 0 .. n_keys), the last n_new the new tokens' own, and new token b sees all but the last n_new - 1 - b.  A token that sees none, of
- * an empty span for instance, gets zeros.  Rows outside the spans are not read.  n_new <= 4096. */
+ * an empty span for instance, gets zeros.  Rows outside the spans are not read, spans may share rows, and infinities and NaN reach no token that does
+ * not see them.  n_new <= 4096. */
 int moshpit_attention_cached(moshpit_ctx *h, const void *q_dev, int64_t q_row_stride, const void *k_dev, int64_t k_row_stride, const void *v_dev,
                              int64_t v_row_stride, int32_t dtype, const int32_t *spans_dev, int64_t sequences, int64_t n_new, int64_t n_keys, int32_t heads,
                              int32_t kv_heads, int32_t depth, float scale, void *out_dev, int64_t out_row_stride);

@@ -1598,7 +1598,9 @@ int moshpit_attention(moshpit_ctx *h, const void *q_dev, int64_t q_row_stride, c
     const AttentionArgs a{static_cast<const char *>(q_dev), static_cast<const char *>(k_dev), static_cast<const char *>(v_dev), static_cast<char *>(out_dev), lse_dev,
                           first_dev, h->N, n_tokens, q_row_stride, k_row_stride, v_row_stride, out_row_stride, heads, kv_heads, depth, scale, 0};
     if (!attention_fits(a)) return fail(h, MOSHPIT_EINVAL, "%lld x %lld tokens of %d heads are too many for one call", (long long)h->N, (long long)n_tokens, heads);
-    HIP_TRY(h, launch_attention(a, dtype, h->stream));
+    int compute_units = 0;
+    HIP_TRY(h, current_compute_units(&compute_units));
+    HIP_TRY(h, launch_attention(a, dtype, compute_units, h->stream));
     return MOSHPIT_OK;
 }
 

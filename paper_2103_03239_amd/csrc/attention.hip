@@ -139,7 +139,7 @@ void attention_kernel(AttentionArgs a)
 {
     constexpr int ES = Num<F>::ES, DT = Num<F>::DT, BLOCKS = DP / 32, N = JOINT, ELEMS = tile_elems<F, DP>(ROWS);
     constexpr uint64_t ALL = ROWS == 64 ? ~uint64_t(0) : 0xffffffffull;
-    constexpr bool TWO = F != kParts || DP <= 64;                      // two buffers of a tile; one where two blocks a compute unit are worth more
+    constexpr bool TWO = F != kParts || DP <= 64 || SIMD == 1;         // two buffers of a tile, or one (the launch says where)
     typedef Direct<(DIRECT ? F : kBf16), (DIRECT ? DP : 128), (DIRECT ? ROWS : 64), kThreads> Straight;
     typedef typename Num<F>::lds_t lds_t;
     // (four variables: an access to one does not wait for what is on its way into another)
@@ -281,6 +281,13 @@ void attention_kernel(AttentionArgs a)
 // Tokens' queries against a span of keys.  A block has one sequence, one head of keys and a share of the span; its waves take tiles of 32 keys in turn,
 // for the same 32 columns: the queries of the heads that share the keys, of the new tokens one after the other.  Nobody waits for
 // anybody before the end.
+// How many rows the sequence has in the cache, and the first.
+__device__ __forceinline__ int32_t span_of(const CachedArgs &a, int64_t seq, int32_t &begin)
+{
+    const int32_t n_keys = static_cast<int32_t>(a.n_keys), first = a.spans[2 * seq], last = a.spans[2 * seq + 1], end = last > n_keys ? n_keys : last;
+    begin = first < 0 ? 0 : first > n_keys ? n_keys : first;
+    return end > begin ? end - begin : 0;
+}
 struct Share {
     int64_t peer, row;                   // row: of this lane's query
     int32_t split, kv_head, col_tile, seq, group, head, from, to, sees, all_see;      // keys of the share, by their number in the span
@@ -299,14 +306,12 @@ struct Share {
         peer = b % static_cast<uint32_t>(a.N);
         split = static_cast<int32_t>(b / static_cast<uint32_t>(a.N));
         group = a.heads / a.kv_heads;
-        const int32_t column = col_tile * 32 + (threadIdx.x & 31), token = column / group, n_keys = static_cast<int32_t>(a.n_keys);
+        const int32_t column = col_tile * 32 + (threadIdx.x & 31), token = column / group;
+        int32_t begin;
         head = kv_head * group + column - token * group;
         there = token < a.fresh;
         row = (peer * a.seqs + seq) * a.fresh + token;
-        int32_t begin = a.spans[2 * (peer * a.seqs + seq)], end = a.spans[2 * (peer * a.seqs + seq) + 1];
-        begin = begin < 0 ? 0 : begin > n_keys ? n_keys : begin;
-        end = end > n_keys ? n_keys : end;
-        const int32_t count = end > begin ? end - begin : 0;
+        const int32_t count = span_of(a, peer * a.seqs + seq, begin);
         const int32_t each = static_cast<int32_t>((count + 32u * kWaves * a.splits - 1) / (32u * kWaves * a.splits)) * (32 * kWaves);
         from = split * each;
         to = int64_t(split + 1) * each < count ? (split + 1) * each : count;
@@ -325,6 +330,32 @@ struct Share {
     }
 };
 
+// This lane's elements of a query's sums by a wave again, key by key over those that the query sees, where values that are no numbers have come into them.
+template <int DT, int BLOCKS>
+__device__ __forceinline__ void attend_again(const CachedArgs &a, const Share &share, int32_t wave, int32_t half, float top, f32x16 (&sum)[BLOCKS])
+{
+    constexpr int ES = DT == 0 ? 4 : 2;
+    const char *q = a.q + (share.row * a.q_stride + int64_t(share.head) * a.depth) * ES;
+#pragma unroll
+    for (int m = 0; m < BLOCKS; ++m) sum[m] = f32x16{};
+    const int32_t end = share.sees < share.to ? share.sees : share.to;
+    for (int32_t at = share.from + 32 * wave; at < end; at += 32 * kWaves)
+        for (int32_t j = at; j < end && j < at + 32; ++j) {
+            const char *k = share.k_rows + j * a.k_stride * ES, *v = share.v_rows + j * a.v_stride * ES;
+            float s = 0.f;
+            for (int32_t d = 0; d < a.depth; ++d) s = fmaf(load_one<DT>(q + d * ES), load_one<DT>(k + d * ES), s);
+            const float w = __builtin_amdgcn_exp2f(fmaf(s, a.scale, -top));
+            if (w == 0.f) continue;
+#pragma unroll
+            for (int m = 0; m < BLOCKS; ++m)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    const int32_t d = 32 * m + 8 * (r >> 2) + 4 * half + (r & 3);
+                    if (d < a.depth) sum[m][r] = fmaf(w, load_one<DT>(v + d * ES), sum[m][r]);
+                }
+        }
+}
+
 // A wave has one tile in LDS, keys and values by turns, and the one after it on its way in registers.  (Four tiles a wave, straight into LDS, bring
 // nothing: 4 x 8 sequences of up to 16384, 4 heads of keys of 128 in bfloat16, in 155 us against 147.  Nor do equal shares of all sequences' keys, whatever
 // their lengths: 141 us, and 33 against 23 for two sequences of 16000 and one head of keys.)
@@ -335,7 +366,7 @@ void cached_kernel(CachedArgs a, float *__restrict__ partials)
     constexpr int ES = Num<F>::ES, DT = Num<F>::DT, BLOCKS = DP / 32, ELEMS = tile_elems<F, DP>(32);
     typedef typename Num<F>::lds_t lds_t;
     __shared__ __attribute__((aligned(16))) lds_t tiles[kWaves][ELEMS];
-    __shared__ float tops[kWaves][32], totals[kWaves][32], block_top[32], block_total[32];
+    __shared__ float tops[kWaves][32], totals[kWaves][32], block_total[32];
     const Share share(a, ES);
     const int32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), half = lane >> 5;
     const int64_t k_bytes = a.k_stride * ES, v_bytes = a.v_stride * ES;
@@ -371,6 +402,7 @@ void cached_kernel(CachedArgs a, float *__restrict__ partials)
 
     // the waves' sums, in order
     x.total = halves_sum(x.total);
+    if (share.there && fabsf(x.top) < INFINITY && fabsf(x.total) < INFINITY && !x.finite()) attend_again<DT>(a, share, wave, half, x.top, x.sum);
     if (half == 0) {
         tops[wave][lane] = x.top;
         totals[wave][lane] = x.total;
@@ -397,10 +429,7 @@ void cached_kernel(CachedArgs a, float *__restrict__ partials)
 #pragma unroll
                 for (int r = 0; r < 16; ++r)
                     joined[(wave * DP + 32 * m + 8 * (r >> 2) + 4 * half + (r & 3)) * PLACE + mine] = x.top == -INFINITY ? 0.f : x.sum[m][r] * factor;
-        if (c0 == 0 && wave == 0 && half == 0) {
-            block_top[lane] = top;
-            block_total[lane] = total;
-        }
+        if (c0 == 0 && wave == 0 && half == 0) block_total[lane] = total;
         __syncthreads();
         const int32_t some = columns - c0 < SOME ? columns - c0 : SOME;
         for (int32_t n = threadIdx.x; n < some * a.depth; n += kThreads) {
@@ -409,7 +438,7 @@ void cached_kernel(CachedArgs a, float *__restrict__ partials)
             float v = joined[d * PLACE + c];
 #pragma unroll
             for (int w = 1; w < kWaves; ++w) v += joined[(w * DP + d) * PLACE + c];
-            if (a.splits == 1) store_one<DT>(a.out + (r * a.out_stride + int64_t(h) * a.depth + d) * ES, block_top[c0 + c] == -INFINITY ? 0.f : v / block_total[c0 + c]);
+            if (a.splits == 1) store_one<DT>(a.out + (r * a.out_stride + int64_t(h) * a.depth + d) * ES, share.all_see + t > 0 ? v / block_total[c0 + c] : 0.f);
             else partials[((r * a.heads + h) * a.splits + share.split) * a.depth + d] = v;
         }
     }
@@ -459,10 +488,12 @@ __global__ __launch_bounds__(kThreads) void cached_join_kernel(CachedArgs a, con
             }
         }
     }
+    int32_t begin;
+    const bool some = span_of(a, row / a.fresh, begin) > a.fresh - 1 - row % a.fresh;
     char *out = a.out + (row * a.out_stride + head * a.depth) * ES;
 #pragma unroll
     for (int t = 0; t < MOST; ++t)
-        if (lane + 64 * t < a.depth) store_one<DT>(out + (lane + 64 * t) * ES, top == -INFINITY ? 0.f : sum[t] / total);
+        if (lane + 64 * t < a.depth) store_one<DT>(out + (lane + 64 * t) * ES, some ? sum[t] / total : 0.f);
 }
 
 int64_t attention_blocks(const AttentionArgs &a) { return a.N * a.heads * ((a.T + kQueries - 1) / kQueries); }
@@ -471,7 +502,7 @@ int64_t attention_blocks(const AttentionArgs &a) { return a.N * a.heads * ((a.T 
 
 bool attention_fits(const AttentionArgs &a) { return launchable(attention_blocks(a), kThreads); }
 
-hipError_t launch_attention(AttentionArgs a, int dtype, hipStream_t stream)
+hipError_t launch_attention(AttentionArgs a, int dtype, int compute_units, hipStream_t stream)
 {
     if (a.T == 0) return hipSuccess;
     a.scale *= kLog2e;
@@ -483,7 +514,17 @@ hipError_t launch_attention(AttentionArgs a, int dtype, hipStream_t stream)
         // bfloat16: two blocks of keys at a time (2 x 16 heads of 128, 8192 tokens: 430 us, one at a time 454), up to a depth of 64 one, with four waves a
         // SIMD (16 x 8 heads of 64, 4096 tokens: 138 us, two at a time with three waves 150)
         const bool direct = F != kParts && direct_rows(a.k, a.k_stride, a.depth, dtype) && direct_rows(a.v, a.v_stride, a.depth, dtype);
-        if constexpr (F == kParts) attention_kernel<F, DP, 32, 1, 2, false><<<blocks, kThreads, 0, stream>>>(a);
+        if constexpr (F == kParts) {
+            // binary32 deeper than 64: one buffer of a tile and two blocks a compute unit (4 x 8 heads, 4000 tokens, depth 80: 323 us, depth 128: 570; two
+            // buffers and one block 509, 631).  Deeper than 96 that spills, and two buffers pay for as long as there are not more than two blocks for
+            // each compute unit (4 x 4 heads of 128, 500 tokens: 56 us, one buffer 71; 4 x 16 heads, 1000 tokens: 132, 143; 4000 tokens: above)
+            if constexpr (DP > 96)
+                if (blocks <= 2 * static_cast<uint32_t>(compute_units)) {
+                    attention_kernel<F, DP, 32, 1, 1, false><<<blocks, kThreads, 0, stream>>>(a);
+                    return hipGetLastError();
+                }
+            attention_kernel<F, DP, 32, 1, 2, false><<<blocks, kThreads, 0, stream>>>(a);
+        }
         else if constexpr (DP > 128) {
             if (direct) attention_kernel<F, DP, 32, 1, 1, true><<<blocks, kThreads, 0, stream>>>(a);
             else attention_kernel<F, DP, 32, 1, 1, false><<<blocks, kThreads, 0, stream>>>(a);

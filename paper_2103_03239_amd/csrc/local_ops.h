@@ -106,7 +106,7 @@ struct AttentionArgs {
     uint32_t tiles;                      // (launch's own)
 };
 bool attention_fits(const AttentionArgs &a);
-hipError_t launch_attention(AttentionArgs a, int dtype, hipStream_t stream);
+hipError_t launch_attention(AttentionArgs a, int dtype, int compute_units, hipStream_t stream);
 
 // Its backward pass, into dq, dk and dv.
 struct AttentionGradArgs {

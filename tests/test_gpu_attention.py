@@ -455,3 +455,35 @@ def test_refusals():
                      lambda: m.attention_cached(q, k, v, spans.long(), 4, 2), lambda: m.attention_cached(q[:, :0].contiguous(), k, v, spans, 4, 2)):
             with pytest.raises(ValueError):
                 call()
+
+
+def test_attention_of_many_blocks():
+    """Deep binary32 heads with more blocks than run at once (another form of the kernel than few take)."""
+    test_attention("f32", "packed", 2, 3, 300, 32, 4, 128, 0)
+
+
+@pytest.mark.parametrize("act", ["f32", "bf16"])
+@pytest.mark.parametrize("D,keys", [(40, 90), (128, 2_500), (200, 300)])
+def test_spoilt_new_tokens(act, D, keys):
+    """Infinities and NaN in a new token's value reach it and later ones; queries that are no numbers, and scores of -inf alone, give NaN, not zeros."""
+    g, N, S, new, H, K = rng(D), 2, 3, 4, 4, 2
+    q, = make(N, S * new, H, K, D, act, g, 0, 1)
+    _, k, v = make(N, keys * S, H, K, D, act, g)
+    spans = torch.tensor([[keys * s, keys * (s + 1)] for s in range(S)], dtype=torch.int32, device=DEV).expand(N, S, 2).contiguous()
+    clean, _ = cached_want(q, k, v, spans, new, H, K, D ** -0.5, act)
+    q[0, 2 * new + 1] = math.nan                                      # sequence 2: one query
+    q[1, :new] = 1.0                                                  # sequence 0 of peer 1: scores of -inf
+    k[1, :keys] = -math.inf
+    v[0, keys - 2, 3], v[0, keys - 1, D + 4] = math.inf, math.nan     # sequence 0: the third new token's first head, the last one's second
+    v[0, keys + 5, 1] = -math.inf                                     # sequence 1: an old token
+    with peers(2, 1) as m:
+        out = m.attention_cached(q, k, v, spans, H, K)
+        m.sync()
+    heads = out.view(N, S, new, H, D)
+    assert torch.isnan(heads[0, 2, 1]).all() and torch.isnan(heads[1, 0]).all()
+    assert (heads[0, 0, 2:, :2, 3] == math.inf).all() and torch.isnan(heads[0, 0, 3, 2:, 4]).all() and (heads[0, 1, :, :2, 1] == -math.inf).all()
+    good = torch.ones_like(heads, dtype=torch.bool)
+    good[0, 2, 1] = good[1, 0] = False
+    good[0, 0, 2:, :2, 3] = good[0, 0, 3, 2:, 4] = good[0, 1, :, :2, 1] = False
+    good = good.view_as(out)
+    close(out[good], clean.out[good], clean.out_slack[good])
