@@ -4,7 +4,9 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <initializer_list>
 #include <new>
+#include <utility>
 #include <vector>
 
 #include "../../include/moshpit.h"
@@ -1328,6 +1330,23 @@ int check_matrix(moshpit_ctx *h, const char *what, const void *dev, int32_t dtyp
     return MOSHPIT_OK;
 }
 
+// A result that may take the place of what is read, row by row.
+int check_place(moshpit_ctx *h, const char *what, const void *out, int64_t out_stride, std::initializer_list<std::pair<const void *, int64_t>> read)
+{
+    for (const auto &in : read)
+        if (out && out == in.first && out_stride != in.second)
+            return fail(h, MOSHPIT_EINVAL, "%s: can take the place of what is read only with its row stride", what);
+    return MOSHPIT_OK;
+}
+
+// One that may not.
+int check_apart(moshpit_ctx *h, const char *what, const void *out, std::initializer_list<const void *> others)
+{
+    for (const void *other : others)
+        if (out && out == other) return fail(h, MOSHPIT_EINVAL, "%s: cannot take the place of another matrix", what);
+    return MOSHPIT_OK;
+}
+
 // An array of 4-byte values.
 int check_words(moshpit_ctx *h, const char *what, const void *dev, int64_t count)
 {
@@ -1512,6 +1531,9 @@ int moshpit_norm(moshpit_ctx *h, const void *x_dev, int32_t dtype, int64_t x_row
     if (residual_dev) CHECK(check_matrix(h, "residual", residual_dev, dtype, n_tokens, width, residual_row_stride));
     if (total_dev) CHECK(check_matrix(h, "total", total_dev, dtype, n_tokens, width, total_row_stride));
     CHECK(check_matrix(h, "output", out_dev, dtype, n_tokens, width, out_row_stride));
+    CHECK(check_place(h, "total", total_dev, total_row_stride, {{x_dev, x_row_stride}, {residual_dev, residual_row_stride}}));
+    CHECK(check_place(h, "output", out_dev, out_row_stride, {{x_dev, x_row_stride}, {residual_dev, residual_row_stride}}));
+    CHECK(check_apart(h, "output", out_dev, {total_dev}));
     if (n_tokens > 0 && !codes_dev != !scales_dev) return fail(h, MOSHPIT_EINVAL, "codes and scales: both or neither");
     if (!(eps >= 0.f) || !std::isfinite(eps)) return fail(h, MOSHPIT_EINVAL, "eps must be finite and >= 0");
     if (!norm_fits(h->N, n_tokens, width)) return fail(h, MOSHPIT_EINVAL, "%lld x %lld rows of %lld are too many for one call", (long long)h->N, (long long)n_tokens, (long long)width);
@@ -1535,6 +1557,7 @@ int moshpit_norm_grad(moshpit_ctx *h, const void *dy_dev, int32_t dtype, int64_t
     CHECK(check_matrix(h, "normed rows", x_dev, dtype, n_tokens, width, x_row_stride));
     if (dtotal_dev) CHECK(check_matrix(h, "total's gradient", dtotal_dev, dtype, n_tokens, width, dtotal_row_stride));
     CHECK(check_matrix(h, "input's gradient", dx_dev, dtype, n_tokens, width, dx_row_stride));
+    CHECK(check_place(h, "input's gradient", dx_dev, dx_row_stride, {{dy_dev, dy_row_stride}, {x_dev, x_row_stride}, {dtotal_dev, dtotal_row_stride}}));
     CHECK(check_grad(h, grad_dev, grad_row_stride_elems));
     if (!(eps >= 0.f) || !std::isfinite(eps)) return fail(h, MOSHPIT_EINVAL, "eps must be finite and >= 0");
     if (!norm_fits(h->N, n_tokens, width)) return fail(h, MOSHPIT_EINVAL, "%lld x %lld rows of %lld are too many for one call", (long long)h->N, (long long)n_tokens, (long long)width);
@@ -1559,6 +1582,7 @@ int moshpit_dropout(moshpit_ctx *h, const void *x_dev, int32_t dtype, int64_t x_
     CHECK(check_matrix(h, "input", x_dev, dtype, n_tokens, width, x_row_stride));
     if (residual_dev) CHECK(check_matrix(h, "residual", residual_dev, dtype, n_tokens, width, residual_row_stride));
     CHECK(check_matrix(h, "output", out_dev, dtype, n_tokens, width, out_row_stride));
+    CHECK(check_place(h, "output", out_dev, out_row_stride, {{x_dev, x_row_stride}, {residual_dev, residual_row_stride}}));
     if (!(p >= 0.0 && p < 1.0)) return fail(h, MOSHPIT_EINVAL, "the probability must be within [0, 1)");
     const uint32_t cut = static_cast<uint32_t>(p * 65536.0 + 0.5);
     if (cut > 65535) return fail(h, MOSHPIT_EINVAL, "a probability of %.9g drops everything (it is taken to the nearest multiple of 2^-16)", p);
@@ -1595,6 +1619,7 @@ int moshpit_attention(moshpit_ctx *h, const void *q_dev, int64_t q_row_stride, c
     CHECK(check_matrix(h, "keys", k_dev, dtype, n_tokens, kv_width, k_row_stride));
     CHECK(check_matrix(h, "values", v_dev, dtype, n_tokens, kv_width, v_row_stride));
     CHECK(check_matrix(h, "output", out_dev, dtype, n_tokens, width, out_row_stride));
+    CHECK(check_apart(h, "output", out_dev, {q_dev, k_dev, v_dev}));
     const AttentionArgs a{static_cast<const char *>(q_dev), static_cast<const char *>(k_dev), static_cast<const char *>(v_dev), static_cast<char *>(out_dev), lse_dev,
                           first_dev, h->N, n_tokens, q_row_stride, k_row_stride, v_row_stride, out_row_stride, heads, kv_heads, depth, scale, 0};
     if (!attention_fits(a)) return fail(h, MOSHPIT_EINVAL, "%lld x %lld tokens of %d heads are too many for one call", (long long)h->N, (long long)n_tokens, heads);
@@ -1623,6 +1648,9 @@ int moshpit_attention_grad(moshpit_ctx *h, const void *dout_dev, int64_t dout_ro
     CHECK(check_matrix(h, "queries' gradient", dq_dev, dtype, n_tokens, width, dq_row_stride));
     CHECK(check_matrix(h, "keys' gradient", dk_dev, dtype, n_tokens, kv_width, dk_row_stride));
     CHECK(check_matrix(h, "values' gradient", dv_dev, dtype, n_tokens, kv_width, dv_row_stride));
+    CHECK(check_apart(h, "queries' gradient", dq_dev, {dk_dev, dv_dev, q_dev, k_dev, v_dev, out_dev, dout_dev}));
+    CHECK(check_apart(h, "keys' gradient", dk_dev, {dv_dev, q_dev, k_dev, v_dev, out_dev, dout_dev}));
+    CHECK(check_apart(h, "values' gradient", dv_dev, {q_dev, k_dev, v_dev, out_dev, dout_dev}));
     const AttentionGradArgs a{static_cast<const char *>(q_dev), static_cast<const char *>(k_dev), static_cast<const char *>(v_dev), static_cast<const char *>(out_dev),
                               static_cast<const char *>(dout_dev), static_cast<char *>(dq_dev), static_cast<char *>(dk_dev), static_cast<char *>(dv_dev), lse_dev,
                               first_dev, h->N, n_tokens, q_row_stride, k_row_stride, v_row_stride, out_row_stride, dout_row_stride, dq_row_stride,
@@ -1651,6 +1679,7 @@ int moshpit_attention_cached(moshpit_ctx *h, const void *q_dev, int64_t q_row_st
     CHECK(check_matrix(h, "keys", k_dev, dtype, n_keys, kv_width, k_row_stride));
     CHECK(check_matrix(h, "values", v_dev, dtype, n_keys, kv_width, v_row_stride));
     CHECK(check_matrix(h, "output", out_dev, dtype, sequences, width, out_row_stride));
+    CHECK(check_apart(h, "output", out_dev, {q_dev, k_dev, v_dev}));
     int compute_units = 0;
     HIP_TRY(h, current_compute_units(&compute_units));
     const CachedArgs a{static_cast<const char *>(q_dev), static_cast<const char *>(k_dev), static_cast<const char *>(v_dev), static_cast<char *>(out_dev), spans_dev, h->N,

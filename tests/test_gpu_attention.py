@@ -487,3 +487,19 @@ def test_spoilt_new_tokens(act, D, keys):
     good[0, 0, 2:, :2, 3] = good[0, 0, 3, 2:, 4] = good[0, 1, :, :2, 1] = False
     good = good.view_as(out)
     close(out[good], clean.out[good], clean.out_slack[good])
+
+
+def test_results_apart():
+    """Results in the place of what is read, or of each other, are refused."""
+    g = rng(8)
+    q, k, v = make(2, 6, 2, 2, 16, "f32", g)
+    first, spans = firsts("one", 2, 6, g), torch.zeros((2, 6, 2), dtype=torch.int32, device=DEV)
+    with peers(2, 1) as m:
+        out, lse = m.attention(q, k, v, first, 2)
+        dout, dk = torch.ones_like(out), torch.empty_like(k)
+        for call in (lambda: m.attention(q, k, v, first, 2, out=q), lambda: m.attention(q, k, v, first, 2, out=v),
+                     lambda: m.attention_cached(q, k, v, spans, 2, out=k), lambda: m.attention_grad(dout, q, k, v, out, lse, first, 2, dq=dout),
+                     lambda: m.attention_grad(dout, q, k, v, out, lse, first, 2, dk=k), lambda: m.attention_grad(dout, q, k, v, out, lse, first, 2, dk=dk, dv=dk),
+                     lambda: m.attention_grad(dout, q, k, v, out, lse, first, 2, dv=out)):
+            with pytest.raises(binding.MoshpitError, match="cannot take the place"):
+                call()

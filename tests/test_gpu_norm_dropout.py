@@ -347,3 +347,20 @@ def test_refusals():
                      lambda: m.dropout(x, 0.1, 1, step=torch.zeros(1, device=DEV)), lambda: m.dropout(x, 0.1, 1, out=x.bfloat16())):
             with pytest.raises(ValueError):
                 call()
+
+
+def test_places_of_other_strides():
+    """A result that begins where an input does, by another stride, would be written over rows that are not yet read."""
+    g = rng(2)
+    X = gains(2, 4, 32, "f32", g, after=0)
+    G, flat = torch.zeros_like(X), normal((2 * 3 * 64,), torch.float32, g)
+    x, close_by = flat.as_strided((2, 3, 32), (3 * 64, 64, 1)), flat.as_strided((2, 3, 32), (3 * 32, 32, 1))
+    y = normal((2, 3, 32), torch.float32, g)
+    with handle(X, 2, 1) as m:
+        for call in (lambda: m.norm(x, 0, out=close_by), lambda: m.norm(y, 0, residual=x, out=close_by), lambda: m.norm(x, 0, residual=y, total=close_by),
+                     lambda: m.norm_grad(x, y, G, 0, out=close_by), lambda: m.norm_grad(y, x, G, 0, out=close_by), lambda: m.norm_grad(y, y, G, 0, dtotal=x, out=close_by),
+                     lambda: m.dropout(x, 0.1, 1, out=close_by), lambda: m.dropout(y, 0.1, 1, residual=x, out=close_by)):
+            with pytest.raises(binding.MoshpitError, match="only with its row stride"):
+                call()
+        with pytest.raises(binding.MoshpitError, match="cannot take the place"):
+            m.norm(x, 0, residual=y, out=x, total=x)
