@@ -19,6 +19,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "row_elems.h"
 #include "tile_math.h"
 
@@ -26,7 +28,6 @@ namespace moshpit {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.693147180559945309417f;
@@ -44,7 +45,6 @@ template <Form F> struct Num {
 // Elements of a tile's row in LDS, and of a tile of `rows` rows, all its parts.
 constexpr int row_elems_of(int DP) { return DP <= 32 ? 32 : DP <= 64 ? 64 : DP <= 128 ? 128 : 256; }
 template <Form F, int DP> constexpr int tile_elems(int rows) { return Num<F>::PARTS * rows * row_elems_of(DP); }
-template <Form F, int DP> constexpr int tile_bytes(int rows) { return tile_elems<F, DP>(rows) * Num<F>::LS; }
 
 // Where 16-byte chunk `chunk` of row `row` of a tile with LP elements a row lies, in elements.  Rows are a power of two long, so the chunks
 // of a row are stored with their numbers xor a number of the row: 16 consecutive rows' same chunks then lie in different banks (for
@@ -348,8 +348,7 @@ template <Form F, int DP, int ROWS, int THREADS> struct Staged {
 };
 
 // The same for rows that are whole 16-byte vectors (`chunks` of them), in the type that LDS has them in: from memory into LDS without passing through
-// registers, a wave 1 KiB at a time (THREADS = 64: a tile of a wave's own): lane l's 16 bytes to where the wave's begin + 16 * l, so the lane
-// reads the chunk that chunk_at() puts there.
+// registers, a wave 1 KiB at a time: lane l's 16 bytes to where the wave's begin + 16 * l, so the lane reads the chunk that chunk_at() puts there.
 template <Form F, int DP, int ROWS, int THREADS> struct Direct {
     static_assert(F != kParts);
     typedef typename Num<F>::lds_t lds_t;
@@ -360,7 +359,7 @@ template <Form F, int DP, int ROWS, int THREADS> struct Direct {
     __device__ __forceinline__ static void request(const char *rows, uint32_t row_bytes, int32_t last, int32_t chunks, lds_t *tile)
     {
         typedef __attribute__((address_space(3))) lds_t to_lds_t;
-        const int lane = threadIdx.x & 63, wave = WAVES == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
         const __amdgpu_buffer_rsrc_t from = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(rows), 0, 0xffffffffu, 0x00027000);
 #pragma unroll
         for (int n = 0; n < COUNT; ++n) {
@@ -373,7 +372,7 @@ template <Form F, int DP, int ROWS, int THREADS> struct Direct {
     __device__ __forceinline__ static void blank(int32_t chunks, lds_t *tile)
     {
         if (chunks == DP / CE) return;
-        const int lane = threadIdx.x & 63, wave = WAVES == 1 ? 0 : threadIdx.x >> 6;
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
         for (int n = 0; n < COUNT; ++n) {
             const int begin = (wave * COUNT + n) * EACH, chunk = (lane % CH) ^ chunk_shift<CH>(begin + lane / CH);
@@ -383,7 +382,7 @@ template <Form F, int DP, int ROWS, int THREADS> struct Direct {
     // And rows whose bit in `live` is not set.
     __device__ __forceinline__ static void trim(uint64_t live, lds_t *tile)
     {
-        const int lane = threadIdx.x & 63, wave = WAVES == 1 ? 0 : threadIdx.x >> 6;
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
         for (int n = 0; n < COUNT; ++n) {
             const int begin = (wave * COUNT + n) * EACH;
