@@ -4,13 +4,13 @@
 // with the sums over i also over the query heads that share the keys.
 //
 // Every sum has an order of its own that no other block takes part in, so there are no atomics and a call repeats to the bit; the price is
-// that p and dp are made twice, 14 multiplications a pair and depth instead of 10.  Three kernels:
+// that p and dp are made twice, 14 multiplications a pair and depth instead of 10 (in bfloat16 two more, see queries_grad_kernel).  Three kernels:
 //   ranges   of every tile of queries the range of `first` (which tiles a key is to be met with)
 //   queries  a wave holds 32 queries and their dout as columns and goes over the keys they see: blocks [key][query], dq [depth][query]; and delta_i, which
 //            the columns hold both factors of
 //   keys     a wave holds 32 keys and values as columns and goes over the queries that see them: blocks [query][key], dk and dv [depth][key]
 // Bound by registers: the columns and the sums leave two waves a SIMD, which the exponentials and roundings of one hide badly behind the
-// products of the other (matrix cores busy for a quarter of the time).  16 x 8 heads of 64, 4 heads of keys, 4096 tokens in bfloat16: queries 223 us, keys 263 us
+// products of the other (matrix cores busy for a quarter of the time).  16 x 8 heads of 64, 4 heads of keys, 4096 tokens in bfloat16: queries 270 us, keys 263 us
 // (forward 133 us).
 #include <hip/hip_runtime.h>
 
@@ -314,7 +314,10 @@ void queries_grad_kernel(AttentionGradArgs a, uint32_t tiles, float *__restrict_
     const float off = columns_dot<F, DP>(a.out + ((row0 + i) * a.out_stride + int64_t(head) * a.depth) * ES,
                                          a.dout + ((row0 + i) * a.dout_stride + int64_t(head) * a.depth) * ES, there, a.depth);
     float drift = 0.f;
-    f32x16 dq[BLOCKS] = {};
+    // delta from out as it was rounded (bfloat16) is off by 2^-9 of its terms, which would bring dq that much of the keys' mean, beside few keys more than
+    // all other roundings (windows of 4 tokens: dq off by 3.0e-3, so 2.3e-3).  sum ds over the keys, 0 in truth, is how much it is off: mean, the keys' sum
+    // by p, is taken from dq so many times.  (16 x 8 heads of 64, 4096 tokens: a training step in 665 us, without 614.)
+    f32x16 dq[BLOCKS] = {}, mean[F == kBf16 ? BLOCKS : 1] = {};
     const char *k_rows = a.k + (row0 * a.k_stride + int64_t(kv_head) * a.depth) * ES, *v_rows = a.v + (row0 * a.v_stride + int64_t(kv_head) * a.depth) * ES;
     const int64_t k_bytes = a.k_stride * ES, v_bytes = a.v_stride * ES;
     auto begins_at = [&](int32_t at) { return at <= to ? begin_of(at + lane) : -1; };
@@ -359,9 +362,12 @@ void queries_grad_kernel(AttentionGradArgs a, uint32_t tiles, float *__restrict_
                 const int32_t j0 = at + 32 * n;
                 if (j0 > wave_hi || j0 + 32 <= wave_lo) continue;
                 const f32x16 s = rows_times<F, DP, ROWS>(keys, 32 * n, q);
-                f32x16 ds = rows_times<F, DP, ROWS>(values, 32 * n, d);
+                f32x16 ds = rows_times<F, DP, ROWS>(values, 32 * n, d), p;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) ds[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale, -lse)) * (ds[r] - off);
+                for (int r = 0; r < 16; ++r) {
+                    p[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale, -lse));
+                    ds[r] = p[r] * (ds[r] - off);
+                }
                 const uint32_t seen = static_cast<uint32_t>(live >> (32 * n));
                 if (j0 < all_from || j0 + 31 > all_to || seen != 0xffffffffu) {
                     const int32_t low = there ? lo - j0 - 4 * half : INT32_MAX / 2;
@@ -369,17 +375,19 @@ void queries_grad_kernel(AttentionGradArgs a, uint32_t tiles, float *__restrict_
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         const int32_t j = 8 * (r >> 2) + (r & 3);
-                        ds[r] = static_cast<uint32_t>(j - low) <= span && (mine >> j & 1) != 0 ? ds[r] : 0.f;
+                        const bool sees = static_cast<uint32_t>(j - low) <= span && (mine >> j & 1) != 0;
+                        ds[r] = sees ? ds[r] : 0.f;
+                        if constexpr (F == kBf16) p[r] = sees ? p[r] : 0.f;
                     }
                 }
                 Weights<F> w;
                 w.take(ds);
                 columns_times<F, DP, ROWS>(keys, 32 * n, 0, w, dq);
-                if constexpr (F == kBf16) {                            // and what their rounding took off them
+                if constexpr (F == kBf16) {
 #pragma unroll
                     for (int r = 0; r < 16; ++r) drift += ds[r];
-                    w.rest(ds);
-                    columns_times<F, DP, ROWS>(keys, 32 * n, 0, w, dq);
+                    w.take(p);
+                    columns_times<F, DP, ROWS>(keys, 32 * n, 0, w, mean);
                 }
             }
             if (more) fill(live_next, k_into, v_into);
@@ -398,6 +406,9 @@ void queries_grad_kernel(AttentionGradArgs a, uint32_t tiles, float *__restrict_
     char *to_row = a.dq + ((row0 + i) * a.dq_stride + int64_t(head) * a.depth) * ES;
 #pragma unroll
     for (int m = 0; m < BLOCKS; ++m) {
+        if constexpr (F == kBf16)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) dq[m][r] = fmaf(-drift, mean[m][r], dq[m][r]);
         if (!there) dq[m] = f32x16{};
         store_column<DT>(to_row, 32 * m, a.depth, dq[m], a.scale * kLn2);
     }
@@ -458,11 +469,13 @@ hipError_t launch_attention_grad(const AttentionGradArgs &given, int dtype, void
     auto of = [&](auto form, auto dp) {
         constexpr Form F = decltype(form)::value;
         constexpr int DP = decltype(dp)::value, DT = Num<F>::DT, SIMD = DP > 128 || F == kParts ? 1 : 2;
+        // (bfloat16 heads of 128: with the keys' mean the sums of dq leave one wave a SIMD; two spill: 4 x 8 heads, 4096 tokens: 631 us, 654; of 96: 511, 448)
+        constexpr int Q_SIMD = DP > 96 ? 1 : SIMD;
         constexpr bool ASIDE = F == kBf16 && DP == 128, STRAIGHT = F != kParts && DP > 32;
         const uint32_t key_blocks = static_cast<uint32_t>(a.N * a.kv_heads * p.tiles * p.parts) * (DP / sum_depths<F, DP>()), query_blocks = static_cast<uint32_t>(a.N * a.heads * p.tiles);
         constexpr int ROWS = F == kBf16 && DP <= 128 ? 64 : 32;
-        if (STRAIGHT && k_direct) queries_grad_kernel<F, DP, ROWS, SIMD, STRAIGHT><<<query_blocks, kThreads, 0, stream>>>(a, p.tiles, delta);
-        else queries_grad_kernel<F, DP, ROWS, SIMD, false><<<query_blocks, kThreads, 0, stream>>>(a, p.tiles, delta);
+        if (STRAIGHT && k_direct) queries_grad_kernel<F, DP, ROWS, Q_SIMD, STRAIGHT><<<query_blocks, kThreads, 0, stream>>>(a, p.tiles, delta);
+        else queries_grad_kernel<F, DP, ROWS, Q_SIMD, false><<<query_blocks, kThreads, 0, stream>>>(a, p.tiles, delta);
         if (STRAIGHT && q_direct) keys_grad_kernel<F, DP, SIMD, ASIDE, STRAIGHT><<<key_blocks, kThreads, 0, stream>>>(a, p, delta, ranges, partials);
         else keys_grad_kernel<F, DP, SIMD, ASIDE, false><<<key_blocks, kThreads, 0, stream>>>(a, p, delta, ranges, partials);
         if (p.parts > 1) {

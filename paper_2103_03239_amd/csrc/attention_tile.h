@@ -255,17 +255,6 @@ template <Form F> struct Weights {
                 }
             }
     }
-    // What is left of p when w is taken off (bfloat16).
-    __device__ __forceinline__ void rest(const f32x16 &p)
-    {
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const uint32_t pair = w[0][t][k];
-                w[0][t][k] = bf16_pair(p[8 * t + 2 * k] - __uint_as_float(pair << 16), p[8 * t + 2 * k + 1] - __uint_as_float(pair & 0xffff0000u));
-            }
-    }
 };
 template <> struct Weights<kF32> {
     f32x16 w;

@@ -503,3 +503,21 @@ def test_results_apart():
                      lambda: m.attention_grad(dout, q, k, v, out, lse, first, 2, dv=out)):
             with pytest.raises(binding.MoshpitError, match="cannot take the place"):
                 call()
+
+
+@pytest.mark.parametrize("D", [64, 96, 128, 256])
+def test_queries_of_one_key(D):
+    """A token that sees itself alone: ds, and so dq, is 0.  delta is off by half a step of out's elements; what that brings, ds k, is taken off again as
+    ds p k.  There ds is rounded to bfloat16, and p, which is 1 but for binary32 roundings, at most as much: two half steps of it are left."""
+    g, N, T, H, K = rng(D), 2, 140, 4, 2
+    q, k, v = make(N, T, H, K, D, "bf16", g)
+    first = torch.arange(T, dtype=torch.int32, device=DEV).expand(N, T).contiguous()
+    dout = normal((N, T, H * D), torch.bfloat16, g)
+    with peers(2, 1) as m:
+        out, lse = m.attention(q, k, v, first, H, K)
+        dq, _, _ = m.attention_grad(dout, q, k, v, out, lse, first, H, K)
+        m.sync()
+    step = 2.0 ** -8
+    off = (step + (4 * D + 16) * U) * (split(dout, H) * split(out, H)).abs().sum(-1, keepdim=True)
+    bound = D ** -0.5 * merge(off * split(k, K).abs().repeat_interleave(H // K, 1)) * 2 * step * 1.05 + TINY
+    assert (dq.double().abs() <= bound).all()
