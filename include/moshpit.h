@@ -398,6 +398,8 @@ int moshpit_policy_loss(moshpit_ctx *h, const void *logits_dev, int32_t dtype, i
  *   y[i][t][c] = h[c] * (mean over the row of h^2 + eps)^(-1/2) * gain_i[c].
  * residual_dev NULL: h = x.  total_dev: NULL, or a matrix that gets h.  codes_dev, scales_dev: NULL, or what
  * moshpit_checkpoint makes of out, in the same pass.  All matrices are of type dtype; h is not rounded before the norm.
+ * Finite rows have their answer whatever their size, squares that binary32 does not hold included; eps is finite and >= 0 (with 0 a row of zeros has
+ * no answer: NaN, and NaN in its gradients).
  * total and out may take the place of x or of the residual (same row stride; not both the same one).  Matrices must not overlap in any other way, here
  * and below. */
 int moshpit_norm(moshpit_ctx *h, const void *x_dev, int32_t dtype, int64_t x_row_stride, const void *residual_dev, int64_t residual_row_stride,

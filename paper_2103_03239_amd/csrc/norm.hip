@@ -7,7 +7,8 @@
 // Bound by HBM.  A row lies in the registers of LANES threads, U units of 8 elements each, from its sums to its results, so it is
 // read once.  A block takes rows of one peer, whose gain it holds, and in the backward pass the sums of the gain's
 // gradient: a thread meets the same columns in every row.  The blocks' sums are joined by a second kernel, in order.
-// Rows of more than 16384 elements are read twice.  16 x 4096 rows of 4096 in bfloat16: forward with residual and 8-bit output 418 us, 5.8 TB/s;
+// Rows of more than 16384 elements are read twice, in the backward pass three times (sums, the gain's gradient by columns, results): 4 x 4000 rows of
+// 20000 in bfloat16 with a residual: 731 us and 1365 (of 16384: 415, 413).  16 x 4096 rows of 4096 in bfloat16: forward with residual and 8-bit output 418 us, 5.8 TB/s;
 // backward with a residual's gradient 407 us, 5.3 TB/s.
 #include <hip/hip_runtime.h>
 
@@ -82,12 +83,32 @@ __device__ __forceinline__ void save_unit(float (&f)[kUnit], int64_t at, int lef
             if (k < left) codes[at + k] = static_cast<int8_t>(w[k / 4] >> (8 * (k & 3)));
 }
 
-// 1 / root mean square and the factor that h is to be taken with first: 1, or 2^-64 where the squares pass binary32.
+// What a row's results are made with: x^ = (h factor) inverse, 1 / root mean square = (inverse root) root, root^2 = factor and
+//   inverse = (mean((h factor)^2) + eps factor^2)^(-1/2).
+// factor is 1 but where mean(h^2) + eps passes binary32, or is so small that squares lose bits below the normal numbers.  With 2^-96 the largest elements'
+// squares are 2^64 and the sum of 2^23 of them 2^87 (elements that it takes below the normal numbers are off by 2^-95 of the row's root mean square
+// and less); with 2^96 elements that were 2^-38 at most stay below 2^58, and the smallest, 2^-149, square to 2^-106.
 struct Size {
-    float factor, inverse;               // x^ = (h factor) inverse
+    float factor, inverse, root;
 };
-__device__ __forceinline__ Size size_of(float mean, float eps) { return Size{1.f, rsqrtf(mean + eps)}; }
-constexpr float kSmall = 0x1p-64f;
+constexpr float kTooSmall = 0x1p-100f;   // (squares' lost bits: 2^-150 each, 2^-50 of it)
+
+// Of a row that LANES threads share: sum(factor) is the sum over it of (h factor)^2, in every one of them.
+template <int LANES, typename Sum> __device__ __forceinline__ Size size_of(float share, float eps, Sum sum)
+{
+    float mean = fmaf(sum(1.f), share, eps), root = 1.f;
+    if (!(mean < INFINITY) || mean < kTooSmall) {                      // (the same in every thread of the row)
+        root = mean < kTooSmall ? 0x1p48f : 0x1p-48f;
+        const float factor = root * root;
+        mean = fmaf(sum(factor), share, eps * factor * factor);
+    }
+    float inverse = rsqrtf(mean);
+    if constexpr (LANES >= 64) {                                       // (the same in every lane: they take no vector registers)
+        root = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(root)));
+        inverse = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(inverse)));
+    }
+    return Size{root * root, inverse, root};
+}
 
 template <int DT, int ST, int LANES, int U>
 __global__ __launch_bounds__(threads_of<LANES>())
@@ -112,7 +133,7 @@ void norm_kernel(NormArgs a, int64_t rows_each, int64_t parts)
     int phase = 0;
     for (int64_t t = begin + slot; t < end; t += SLOTS) {              // (one slot, where the threads of a row wait for each other)
         const int64_t row = peer * a.T + t;
-        float h[U][kUnit], sum = 0.f;
+        float h[U][kUnit];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
 #pragma unroll
@@ -128,21 +149,14 @@ void norm_kernel(NormArgs a, int64_t rows_each, int64_t parts)
 #pragma unroll
                     for (int k = 0; k < kUnit; ++k) h[u][k] += r[k];
                 }
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int k = 0; k < kUnit; ++k) sum = fmaf(h[u][k], h[u][k], sum);
-        sum = group_sum<LANES>(sum, scratch[phase ^= 1]);
-        Size s = size_of(sum * share, a.eps);
-        if (!(sum < INFINITY)) {                                       // (the same in every thread of the row)
-            sum = 0.f;
+        const Size s = size_of<LANES>(share, a.eps, [&](float factor) {
+            float sum = 0.f;
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
-                for (int k = 0; k < kUnit; ++k) sum = fmaf(h[u][k] * kSmall, h[u][k] * kSmall, sum);
-            sum = group_sum<LANES>(sum, scratch[phase ^= 1]);
-            s = Size{kSmall, rsqrtf(sum * share)};
-        }
+                for (int k = 0; k < kUnit; ++k) sum = fmaf(h[u][k] * factor, h[u][k] * factor, sum);
+            return group_sum<LANES>(sum, scratch[phase ^= 1]);
+        });
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (left[u] > 0 && a.total) store_unit<DT>(a.total + (row * a.total_stride + at[u]) * ES, left[u], h[u]);
@@ -179,19 +193,16 @@ __global__ __launch_bounds__(1024) void wide_norm_kernel(NormArgs a)
             for (int k = 0; k < kUnit; ++k) h[k] += r[k];
         }
     };
-    auto squares = [&](float factor) {
+    int phase = 0;
+    const Size s = size_of<1024>(1.f / static_cast<float>(width), a.eps, [&](float factor) {
         float sum = 0.f, h[kUnit];
         for (int32_t at = threadIdx.x * kUnit; at < width; at += 1024 * kUnit) {
             load(at, h);
 #pragma unroll
             for (int k = 0; k < kUnit; ++k) sum = fmaf(h[k] * factor, h[k] * factor, sum);
         }
-        return sum;
-    };
-    const float share = 1.f / static_cast<float>(width);
-    float sum = group_sum<1024>(squares(1.f), scratch[0]);
-    Size s = size_of(sum * share, a.eps);
-    if (!(sum < INFINITY)) s = Size{kSmall, rsqrtf(group_sum<1024>(squares(kSmall), scratch[1]) * share)};
+        return group_sum<1024>(sum, scratch[phase ^= 1]);
+    });
     for (int32_t at = threadIdx.x * kUnit; at < last; at += 1024 * kUnit) {
         float h[kUnit] = {}, g[kUnit];
         const int32_t left = width - at;
@@ -210,8 +221,9 @@ __global__ __launch_bounds__(1024) void wide_norm_kernel(NormArgs a)
 
 // sums: [N][parts][width], the gain's gradient over the rows of a block, which takes every parts-th one, so that the blocks that run at the same time read
 // neighbouring rows (4 x 30000 rows of 1000 in bfloat16: 189 us, by pieces of consecutive rows 218).
+// Rows of 2048 to 4096 in bfloat16: four waves a SIMD (16 x 4096 rows of 4096: 407 us; as many registers as the compiler likes, three waves: 490).
 template <int DT, int ST, int LANES, int U>
-__global__ __launch_bounds__(threads_of<LANES>())
+__global__ __launch_bounds__(threads_of<LANES>(), (LANES == 256 && U == 2 ? 4 : 1))
 void norm_grad_kernel(NormGradArgs a, int64_t parts, float *__restrict__ sums)
 {
     constexpr int ES = DT == 0 ? 4 : 2, GS = ST == 0 ? 4 : 2, SLOTS = threads_of<LANES>() / LANES;
@@ -234,7 +246,7 @@ void norm_grad_kernel(NormGradArgs a, int64_t parts, float *__restrict__ sums)
     int phase = 0;
     for (int64_t t = part * SLOTS + slot; t < a.T; t += parts * SLOTS) {      // (SLOTS > 1: within a wave or less, no barrier in the loop)
         const int64_t row = peer * a.T + t;
-        float h[U][kUnit], dy[U][kUnit], square = 0.f, product = 0.f;
+        float h[U][kUnit], dy[U][kUnit], product = 0.f;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
 #pragma unroll
@@ -244,8 +256,9 @@ void norm_grad_kernel(NormGradArgs a, int64_t parts, float *__restrict__ sums)
                 load_unit<DT>(a.dy + (row * a.dy_stride + at[u]) * ES, left[u], dy[u]);
             }
         }
-        auto take = [&](float factor) {
-            square = product = 0.f;
+        const Size s = size_of<LANES>(share, a.eps, [&](float factor) {
+            float square = 0.f;
+            product = 0.f;
 #pragma unroll
             for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -255,14 +268,9 @@ void norm_grad_kernel(NormGradArgs a, int64_t parts, float *__restrict__ sums)
                     product = fmaf(dy[u][k] * g[u][k], v, product);
                 }
             group_sums<LANES>(square, product, scratch[phase ^= 1]);
-        };
-        take(1.f);
-        Size s = size_of(square * share, a.eps);
-        if (!(square < INFINITY)) {
-            take(kSmall);
-            s = Size{kSmall, rsqrtf(square * share)};
-        }
-        const float mean = product * share * s.inverse, outer = s.inverse * s.factor;
+            return square;
+        });
+        const float mean = product * share * s.inverse, outer = s.inverse * s.root;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (left[u] <= 0) continue;
@@ -272,7 +280,7 @@ void norm_grad_kernel(NormGradArgs a, int64_t parts, float *__restrict__ sums)
             for (int k = 0; k < kUnit; ++k) {
                 const float v = h[u][k] * s.factor * s.inverse;
                 dg[u][k] = fmaf(dy[u][k], v, dg[u][k]);
-                const float e = outer * (dy[u][k] * g[u][k] - v * mean);
+                const float e = outer * (dy[u][k] * g[u][k] - v * mean) * s.root;
                 d[k] = a.dtotal ? d[k] + e : e;
             }
             store_unit<DT>(a.dx + (row * a.dx_stride + at[u]) * ES, left[u], d);
@@ -299,7 +307,7 @@ void norm_grad_kernel(NormGradArgs a, int64_t parts, float *__restrict__ sums)
     }
 }
 
-// Rows that registers do not hold: 1 / root mean square (with its factor) and mean(u x^) of a row, by a block.
+// Rows that registers do not hold: factor, inverse, mean(u x^) and root of a row, by a block.
 template <int DT, int ST>
 __global__ __launch_bounds__(1024) void wide_norm_sums_kernel(NormGradArgs a, float4 *__restrict__ found)
 {
@@ -308,9 +316,12 @@ __global__ __launch_bounds__(1024) void wide_norm_sums_kernel(NormGradArgs a, fl
     const int64_t row = blockIdx.x;
     const char *gain = a.gain + row / a.T * a.gain_stride * GS, *x = a.x + row * a.x_stride * ES, *dy = a.dy + row * a.dy_stride * ES;
     const int32_t width = static_cast<int32_t>(a.width);
-    float square, product;
-    auto take = [&](float factor, float *lds) {
-        square = product = 0.f;
+    float product = 0.f;
+    int phase = 0;
+    const float share = 1.f / static_cast<float>(width);
+    const Size s = size_of<1024>(share, a.eps, [&](float factor) {
+        float square = 0.f;
+        product = 0.f;
         for (int32_t at = threadIdx.x * kUnit; at < width; at += 1024 * kUnit) {
             float h[kUnit], d[kUnit], g[kUnit];
             load_unit<DT>(x + int64_t(at) * ES, width - at, h);
@@ -323,16 +334,10 @@ __global__ __launch_bounds__(1024) void wide_norm_sums_kernel(NormGradArgs a, fl
                 product = fmaf(d[k] * g[k], v, product);
             }
         }
-        group_sums<1024>(square, product, lds);
-    };
-    const float share = 1.f / static_cast<float>(width);
-    take(1.f, scratch[0]);
-    Size s = size_of(square * share, a.eps);
-    if (!(square < INFINITY)) {
-        take(kSmall, scratch[1]);
-        s = Size{kSmall, rsqrtf(square * share)};
-    }
-    if (threadIdx.x == 0) found[row] = float4{s.factor, s.inverse, product * share * s.inverse, 0.f};
+        group_sums<1024>(square, product, scratch[phase ^= 1]);
+        return square;
+    });
+    if (threadIdx.x == 0) found[row] = float4{s.factor, s.inverse, product * share * s.inverse, s.root};
 }
 
 // Their gain's gradient: a thread has a column, and adds up the rows of a part.
@@ -370,7 +375,7 @@ __global__ __launch_bounds__(1024) void wide_norm_grad_kernel(NormGradArgs a, co
         if (a.dtotal) load_unit<DT>(a.dtotal + (row * a.dtotal_stride + at) * ES, width - at, more);
 #pragma unroll
         for (int k = 0; k < kUnit; ++k) {
-            const float e = s.y * s.x * (d[k] * g[k] - h[k] * s.x * s.y * s.z);
+            const float e = s.y * s.w * (d[k] * g[k] - h[k] * s.x * s.y * s.z) * s.w;
             d[k] = a.dtotal ? more[k] + e : e;
         }
         store_unit<DT>(a.dx + (row * a.dx_stride + at) * ES, width - at, d);
