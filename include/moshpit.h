@@ -454,7 +454,7 @@ int moshpit_attention_grad(moshpit_ctx *h, const void *dout_dev, int64_t dout_ro
  * values: n_keys rows a peer; spans_dev, [N][sequences][2] int32: the sequence's rows are spans[..][0] .. spans[..][1] - 1 of them (cut to
  * 0 .. n_keys), the last n_new the new tokens' own, and new token b sees all but the last n_new - 1 - b.  A token that sees none, of
  * an empty span for instance, gets zeros.  Rows outside the spans are not read, spans may share rows, and infinities and NaN reach no token that does
- * not see them.  n_new <= 4096. */
+ * not see them; finite values have finite outputs, the largest included.  n_new <= 4096. */
 int moshpit_attention_cached(moshpit_ctx *h, const void *q_dev, int64_t q_row_stride, const void *k_dev, int64_t k_row_stride, const void *v_dev,
                              int64_t v_row_stride, int32_t dtype, const int32_t *spans_dev, int64_t sequences, int64_t n_new, int64_t n_keys, int32_t heads,
                              int32_t kv_heads, int32_t depth, float scale, void *out_dev, int64_t out_row_stride);

@@ -336,15 +336,18 @@ struct Share {
     }
 };
 
-// This lane's elements of a query's sums by a wave again, key by key over those that the query sees, where values that are no numbers have come into them.
+// This lane's elements of a query's sums by a wave again, key by key over those that the query sees, where values that are no numbers have come into
+// them, or finite ones have passed binary32: weights are taken from the wave's log-sum, so that they add up to 1.  Both halves of a column take part.
 template <int DT, int BLOCKS>
-__device__ __forceinline__ void attend_again(const CachedArgs &a, const Share &share, int32_t wave, int32_t half, float top, f32x16 (&sum)[BLOCKS])
+__device__ __forceinline__ void attend_again(const CachedArgs &a, const Share &share, int32_t wave, int32_t half, float &top, float &total, f32x16 (&sum)[BLOCKS])
 {
     constexpr int ES = DT == 0 ? 4 : 2;
     const char *q = a.q + (share.row * a.q_stride + int64_t(share.head) * a.depth) * ES;
 #pragma unroll
     for (int m = 0; m < BLOCKS; ++m) sum[m] = f32x16{};
     const int32_t end = share.sees < share.to ? share.sees : share.to;
+    top += __builtin_amdgcn_logf(total);
+    total = 0.f;
     for (int32_t at = share.from + 32 * wave; at < end; at += 32 * kWaves)
         for (int32_t j = at; j < end && j < at + 32; ++j) {
             const char *k = share.k_rows + j * a.k_stride * ES, *v = share.v_rows + j * a.v_stride * ES;
@@ -352,6 +355,7 @@ __device__ __forceinline__ void attend_again(const CachedArgs &a, const Share &s
             for (int32_t d = 0; d < a.depth; ++d) s = fmaf(load_one<DT>(q + d * ES), load_one<DT>(k + d * ES), s);
             const float w = __builtin_amdgcn_exp2f(fmaf(s, a.scale, -top));
             if (w == 0.f) continue;
+            total += w;
 #pragma unroll
             for (int m = 0; m < BLOCKS; ++m)
 #pragma unroll
@@ -408,7 +412,8 @@ void cached_kernel(CachedArgs a, float *__restrict__ partials)
 
     // the waves' sums, in order
     x.total = halves_sum(x.total);
-    if (share.there && fabsf(x.top) < INFINITY && fabsf(x.total) < INFINITY && !x.finite()) attend_again<DT>(a, share, wave, half, x.top, x.sum);
+    const uint64_t halves = __ballot(share.there && fabsf(x.top) < INFINITY && fabsf(x.total) < INFINITY && !x.finite());
+    if (((halves | halves >> 32) >> (lane & 31) & 1) != 0) attend_again<DT>(a, share, wave, half, x.top, x.total, x.sum);
     if (half == 0) {
         tops[wave][lane] = x.top;
         totals[wave][lane] = x.total;
@@ -417,7 +422,8 @@ void cached_kernel(CachedArgs a, float *__restrict__ partials)
     float top = tops[0][lane & 31], total = 0.f;
 #pragma unroll
     for (int w = 1; w < kWaves; ++w) top = fmaxf(top, tops[w][lane & 31]);
-    auto factor_of = [&](float t) { return t == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(t - top); };
+    // (a quarter: four waves' sums together pass binary32 only where one of them does)
+    auto factor_of = [&](float t) { return t == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(t - top) * (1.f / kWaves); };
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) total += totals[w][lane & 31] * factor_of(tops[w][lane & 31]);
     const float factor = factor_of(x.top);
@@ -467,6 +473,7 @@ __global__ __launch_bounds__(kThreads) void cached_join_kernel(CachedArgs a, con
     const int lane = threadIdx.x & 63;
     const float *tops = partials + shares * a.depth + n * a.splits, *totals = tops + shares, *sums = partials + n * a.splits * a.depth;
     float top = -INFINITY, sum[MOST] = {}, total = 0.f;
+    const float less = __uint_as_float((127u - (32 - __clz(a.splits - 1))) << 23);     // 2^-n <= 1 / splits, as above
     for (int s = lane; s < a.splits; s += 64) top = fmaxf(top, tops[s]);
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor(top, off, 64));
@@ -477,7 +484,7 @@ __global__ __launch_bounds__(kThreads) void cached_join_kernel(CachedArgs a, con
             mine = tops[s0 + lane];
             part = totals[s0 + lane];
         }
-        const float factor = mine == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mine - top);
+        const float factor = mine == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mine - top) * less;
         for (int s = 0; s < left; s += 4) {                            // four shares requested at a time
             float v[4][MOST];
 #pragma unroll
