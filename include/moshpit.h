@@ -433,7 +433,9 @@ int moshpit_dropout(moshpit_ctx *h, const void *x_dev, int32_t dtype, int64_t x_
  * sees, as a rule the one its sequence begins with (a later one makes a window).  A number outside 0 .. t: a place
  * without a token, whose rows may hold anything.  Token t sees the tokens s with first[t] <= s <= t:
  *   out[t] = sum over s of exp(scale * q[t] . k[s] - lse[t]) v[s],   lse[t] = log of the sum over s of exp(scale * q[t] . k[s]);
- * 0 for out and lse where there is no token.  Infinities and NaN reach no token that does not see them.  lse_dev: NULL, or
+ * 0 for out and lse where there is no token.  Infinities and NaN reach no token that does not see them.  Of those that do, a score of -inf is a weight of 0;
+ * with one of +inf or NaN, or -inf alone, out is NaN.  Tokens that see an infinity or a NaN in a value, or of binary32 ones an infinite score, are taken
+ * anew one by one, which is slow: 8192 tokens of 4 heads of 128 that all see one in 103 ms, the call without it in 0.4.  lse_dev: NULL, or
  * [N][heads][n_tokens] floats, which the backward pass takes.  Weights are rounded to bfloat16 for their product with bfloat16 values; all else
  * is binary32.  scale > 0, 1 <= depth <= 256, heads <= 2^16.  out may take the place of nothing that is read. */
 int moshpit_attention(moshpit_ctx *h, const void *q_dev, int64_t q_row_stride, const void *k_dev, int64_t k_row_stride, const void *v_dev,

@@ -9,7 +9,8 @@
 //
 // A weight of 0 times a value that is no number is no number, so a sequence's infinities would reach others that share its tiles.  Rows
 // of places without a token are zeros in the tiles.  For the rest a wave looks at its results: a query whose weights are numbers and whose sums are
-// not is taken again, key by key over those that it sees.
+// not is taken again, key by key over those that it sees (and of binary32 ones in parts, one whose weights are not).  That is slow: 8192 tokens of 4 heads
+// of 128 in bfloat16 in 103 ms where the first value has an infinity; a NaN in the key in the middle of 4096 of 80 in binary32: 7 ms.
 //
 // Prompts are bound by the vector instructions beside the matrix ones: an exponential, a maximum and a rounding for each pair against 4 depth
 // multiplications (heads of 128 in bfloat16, the matrix cores are busy for 42 % of the time, vector instructions for about as much).  2 x 16 heads of 128, 4 heads of keys,
@@ -20,6 +21,7 @@
 
 #include "attention_tile.h"
 #include "local_ops.h"
+#include "row_sums.h"
 
 namespace moshpit {
 namespace {
@@ -106,24 +108,57 @@ template <Form F, int DP> struct Queries {
     }
 };
 
-// One query's result by a wave, key by key over those that it sees, where values that are no numbers have come into its sums.  lse: its log2-sum.
-template <int DT>
-__device__ __forceinline__ void attend_alone(const AttentionArgs &a, int64_t peer, int32_t head, int32_t i, int32_t lo, float lse, char *out)
+// The sum of products of `depth` elements, in order.
+template <int DT> __device__ __forceinline__ float dot(const char *x, const char *y, int32_t depth)
+{
+    constexpr int ES = DT == 0 ? 4 : 2;
+    float s = 0.f;
+    int32_t d = 0;
+    for (; d + 4 <= depth; d += 4) {
+        float f[4], g[4];
+        load_elems<DT, 4>(x + d * ES, f);
+        load_elems<DT, 4>(y + d * ES, g);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s = fmaf(f[e], g[e], s);
+    }
+    for (; d < depth; ++d) s = fmaf(load_one<DT>(x + d * ES), load_one<DT>(y + d * ES), s);
+    return s;
+}
+
+// One query's result by a wave, key by key over those that it sees, where values that are no numbers have come into its sums or finite ones have passed
+// binary32: with weights from its log-sum, which add up to 1.  lse: its log2-sum, or NaN where scores of three parts were no numbers (an infinity
+// times parts of 0 is none, also where the score is -inf, a weight of 0): then it is found first, and where it is no number either, nothing more is read.
+template <int DT> __device__ __forceinline__ void attend_alone(const AttentionArgs &a, int64_t peer, int32_t head, int32_t i, int32_t lo, float lse)
 {
     constexpr int ES = DT == 0 ? 4 : 2, MOST = 256 / 64;
     const int32_t lane = threadIdx.x & 63, kv_head = head / (a.heads / a.kv_heads);
     const int64_t row0 = peer * a.T;
     const char *q = a.q + ((row0 + i) * a.q_stride + int64_t(head) * a.depth) * ES;
-    float sum[MOST] = {};
-    for (int32_t j0 = lo; j0 <= i; j0 += 64) {
-        const int32_t j = j0 + lane, f = j <= i ? a.first[row0 + j] : -1;
-        float w = 0.f;
-        if (f >= 0 && f <= j) {
-            const char *k = a.k + ((row0 + j) * a.k_stride + int64_t(kv_head) * a.depth) * ES;
-            float s = 0.f;
-            for (int32_t d = 0; d < a.depth; ++d) s = fmaf(load_one<DT>(q + d * ES), load_one<DT>(k + d * ES), s);
-            w = __builtin_amdgcn_exp2f(fmaf(s, a.scale, -lse));
+    auto score = [&](int32_t j) {                                      // -inf: not seen
+        const int32_t f = j <= i ? a.first[row0 + j] : -1;
+        if (f < 0 || f > j) return -INFINITY;
+        const char *k = a.k + ((row0 + j) * a.k_stride + int64_t(kv_head) * a.depth) * ES;
+        return dot<DT>(q, k, a.depth) * a.scale;
+    };
+    if (lse != lse) {
+        float top = -INFINITY, total = 0.f;
+        for (int32_t j0 = lo; j0 <= i; j0 += 64) {
+            const float s = score(j0 + lane);
+            if (!__all(s < INFINITY)) {                                // NaN or +inf: no weight is a number
+                total = NAN;
+                break;
+            }
+            const float now = lanes_max(fmaxf(top, s));
+            if (now == -INFINITY) continue;
+            total = fmaf(total, __builtin_amdgcn_exp2f(top - now), lanes_sum<64>(__builtin_amdgcn_exp2f(s - now)));
+            top = now;
         }
+        lse = top + __builtin_amdgcn_logf(total);
+    }
+    const bool numbers = fabsf(lse) < INFINITY;
+    float sum[MOST] = {};
+    for (int32_t j0 = lo; j0 <= i && numbers; j0 += 64) {
+        const float w = __builtin_amdgcn_exp2f(score(j0 + lane) - lse);
         for (uint64_t left = __ballot(w != 0.f); left; left &= left - 1) {
             const int32_t n = __builtin_ctzll(left);
             const float one = __shfl(w, n, 64);
@@ -133,9 +168,11 @@ __device__ __forceinline__ void attend_alone(const AttentionArgs &a, int64_t pee
                 if (lane + 64 * t < a.depth) sum[t] = fmaf(one, load_one<DT>(v + (lane + 64 * t) * ES), sum[t]);
         }
     }
+    char *out = a.out + ((row0 + i) * a.out_stride + int64_t(head) * a.depth) * ES;
 #pragma unroll
     for (int t = 0; t < MOST; ++t)
-        if (lane + 64 * t < a.depth) store_one<DT>(out + (lane + 64 * t) * ES, sum[t]);
+        if (lane + 64 * t < a.depth) store_one<DT>(out + (lane + 64 * t) * ES, numbers ? sum[t] : NAN);
+    if (lane == 0 && a.lse) a.lse[(peer * a.heads + head) * a.T + i] = lse * kLn2;
 }
 
 // ROWS keys a tile, JOINT blocks of 32 keys at a time, SIMD waves a SIMD, DIRECT: rows go straight into LDS.
@@ -266,21 +303,20 @@ void attention_kernel(AttentionArgs a)
 
     const float total = halves_sum(x.total), share = 1.f / total, lse = x.top + __builtin_amdgcn_logf(total);
     char *out = a.out + ((row0 + i) * a.out_stride + int64_t(head) * a.depth) * ES;
-    // weights that are numbers, but sums that are not
-    const uint64_t halves = __ballot(there && fabsf(lse) < INFINITY && !x.finite());
+    // weights that are numbers, but sums that are not, or scores of parts that are not
+    const uint64_t halves = __ballot(there && (F == kParts && lse != lse ? true : fabsf(lse) < INFINITY && !x.finite()));
     const uint32_t spoilt = static_cast<uint32_t>(halves) | static_cast<uint32_t>(halves >> 32);
-    if (i < T) {
+    if (i < T && (spoilt >> (lane & 31) & 1) == 0) {
         if (half == 0 && a.lse) a.lse[(peer * a.heads + head) * a.T + i] = there ? lse * kLn2 : 0.f;
-        if ((spoilt >> (lane & 31) & 1) == 0)
 #pragma unroll
-            for (int m = 0; m < BLOCKS; ++m) {
-                if (!there) x.sum[m] = f32x16{};
-                store_column<DT>(out, 32 * m, a.depth, x.sum[m], there ? share : 0.f);
-            }
+        for (int m = 0; m < BLOCKS; ++m) {
+            if (!there) x.sum[m] = f32x16{};
+            store_column<DT>(out, 32 * m, a.depth, x.sum[m], there ? share : 0.f);
+        }
     }
     for (uint32_t left = spoilt; left; left &= left - 1) {
-        const int32_t n = __builtin_ctz(left), row = wave_first + n;
-        attend_alone<DT>(a, peer, head, row, __shfl(lo, n, 64), __shfl(lse, n, 64), a.out + ((row0 + row) * a.out_stride + int64_t(head) * a.depth) * ES);
+        const int32_t n = __builtin_ctz(left);
+        attend_alone<DT>(a, peer, head, wave_first + n, __shfl(lo, n, 64), __shfl(lse, n, 64));
     }
 }
 
@@ -336,34 +372,55 @@ struct Share {
     }
 };
 
-// This lane's elements of a query's sums by a wave again, key by key over those that the query sees, where values that are no numbers have come into
-// them, or finite ones have passed binary32: weights are taken from the wave's log-sum, so that they add up to 1.  Both halves of a column take part.
+// This lane's elements of a query's sums by a wave again, for the same reasons and in the same manner as attend_alone, key by key over those that the query
+// sees.  Both halves of a column take part.
 template <int DT, int BLOCKS>
 __device__ __forceinline__ void attend_again(const CachedArgs &a, const Share &share, int32_t wave, int32_t half, float &top, float &total, f32x16 (&sum)[BLOCKS])
 {
     constexpr int ES = DT == 0 ? 4 : 2;
     const char *q = a.q + (share.row * a.q_stride + int64_t(share.head) * a.depth) * ES;
+    const int32_t end = share.sees < share.to ? share.sees : share.to;
+    auto each = [&](auto go) {                                         // go(key, score), for as long as it is true
+        for (int32_t at = share.from + 32 * wave; at < end; at += 32 * kWaves)
+            for (int32_t j = at; j < end && j < at + 32; ++j) {
+                const char *k = share.k_rows + j * a.k_stride * ES;
+                if (!go(j, dot<DT>(q, k, a.depth) * a.scale)) return;
+            }
+    };
 #pragma unroll
     for (int m = 0; m < BLOCKS; ++m) sum[m] = f32x16{};
-    const int32_t end = share.sees < share.to ? share.sees : share.to;
+    if (total != total) {
+        top = -INFINITY;
+        total = 0.f;
+        each([&](int32_t, float s) {
+            if (!(s < INFINITY)) {                                     // NaN or +inf: no weight is a number
+                top = -INFINITY;
+                total = NAN;
+                return false;
+            }
+            if (s == -INFINITY) return true;
+            const float now = fmaxf(top, s);
+            total = fmaf(total, __builtin_amdgcn_exp2f(top - now), __builtin_amdgcn_exp2f(s - now));
+            top = now;
+            return true;
+        });
+        if (top == -INFINITY) return;
+    }
     top += __builtin_amdgcn_logf(total);
     total = 0.f;
-    for (int32_t at = share.from + 32 * wave; at < end; at += 32 * kWaves)
-        for (int32_t j = at; j < end && j < at + 32; ++j) {
-            const char *k = share.k_rows + j * a.k_stride * ES, *v = share.v_rows + j * a.v_stride * ES;
-            float s = 0.f;
-            for (int32_t d = 0; d < a.depth; ++d) s = fmaf(load_one<DT>(q + d * ES), load_one<DT>(k + d * ES), s);
-            const float w = __builtin_amdgcn_exp2f(fmaf(s, a.scale, -top));
-            if (w == 0.f) continue;
-            total += w;
+    each([&](int32_t j, float s) {
+        const float w = __builtin_amdgcn_exp2f(s - top);
+        if (w == 0.f) return true;
+        total += w;
 #pragma unroll
-            for (int m = 0; m < BLOCKS; ++m)
+        for (int m = 0; m < BLOCKS; ++m)
 #pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int32_t d = 32 * m + 8 * (r >> 2) + 4 * half + (r & 3);
-                    if (d < a.depth) sum[m][r] = fmaf(w, load_one<DT>(v + d * ES), sum[m][r]);
-                }
-        }
+            for (int r = 0; r < 16; ++r) {
+                const int32_t d = 32 * m + 8 * (r >> 2) + 4 * half + (r & 3);
+                if (d < a.depth) sum[m][r] = fmaf(w, load_one<DT>(share.v_rows + (j * a.v_stride + d) * ES), sum[m][r]);
+            }
+        return true;
+    });
 }
 
 // A wave has one tile in LDS, keys and values by turns, and the one after it on its way in registers.  (Four tiles a wave, straight into LDS, bring
@@ -412,7 +469,7 @@ void cached_kernel(CachedArgs a, float *__restrict__ partials)
 
     // the waves' sums, in order
     x.total = halves_sum(x.total);
-    const uint64_t halves = __ballot(share.there && fabsf(x.top) < INFINITY && fabsf(x.total) < INFINITY && !x.finite());
+    const uint64_t halves = __ballot(share.there && (F == kParts && x.total != x.total ? true : fabsf(x.top) < INFINITY && fabsf(x.total) < INFINITY && !x.finite()));
     if (((halves | halves >> 32) >> (lane & 31) & 1) != 0) attend_again<DT>(a, share, wave, half, x.top, x.total, x.sum);
     if (half == 0) {
         tops[wave][lane] = x.top;

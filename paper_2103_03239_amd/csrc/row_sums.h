@@ -32,6 +32,19 @@ template <int LANES> __device__ __forceinline__ float lanes_sum(float v)
     return v;
 }
 
+// The largest of a wave's 64 lanes.
+__device__ __forceinline__ float lanes_max(float v)
+{
+    v = fmaxf(v, lane_from<0xB1>(v));
+    v = fmaxf(v, lane_from<0x4E>(v));
+    v = fmaxf(v, lane_from<0x141>(v));
+    v = fmaxf(v, lane_from<0x140>(v));
+    const LanePair a = swap16(v, v);
+    v = fmaxf(a.first, a.second);
+    const LanePair b = swap32(v, v);
+    return fmaxf(b.first, b.second);
+}
+
 // lds: 16 floats that no thread still reads from the call before the last; a block's threads call it together.
 template <int LANES> __device__ __forceinline__ float group_sum(float v, float *lds)
 {
