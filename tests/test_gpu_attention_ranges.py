@@ -132,3 +132,88 @@ def test_cached_scores_of_infinities(act, S, new, keys, H, K, D):
         m.sync()
     close(out[:2], want.out[:2], want.out_slack[:2])
     assert torch.isnan(out[2:]).all()
+
+
+# ---- the backward pass ------------------------------------------------------------
+
+def check_gradients(act, N, M, d, T, H, K, D, first, want=None):
+    g = rng(T + D)
+    q, k, v = make(N, T, H, K, D, act, g)
+    dout = normal((N, T, H * D), TYPES[act][0], g, 0.1)
+    want = Want(q, k, v, seen_of(first), H, K, D ** -0.5, act, dout) if want is None else want(q, k, v, dout)
+    with peers(M, d) as m:
+        print("attention_grad", act, N, T, H, K, D, flush=True)
+        out, lse = m.attention(q, k, v, first, H, K)
+        got = m.attention_grad(dout, q, k, v, out, lse, first, H, K)
+        again = m.attention_grad(dout, q, k, v, out, lse, first, H, K)
+        m.sync()
+    for x, y, name in zip(got, again, ("dq", "dk", "dv")):
+        assert torch.equal(x, y)
+        close(x, getattr(want, name), getattr(want, name + "_slack"))
+
+
+@pytest.mark.parametrize("act,T,D", [("f32", 2_200, 32), ("bf16", 2_200, 96), ("bf16", 4_200, 64), ("bf16", 2_100, 200)])
+@pytest.mark.parametrize("kind", ["one", "padded", "far"])
+def test_gradients_of_many_tiles(act, T, D, kind):
+    """More than 64 tiles of queries, whose ranges a block of keys looks at 64 at a time: all of them see the first keys, or hardly any, or the last."""
+    g, N = rng(T), 2
+    if kind == "far":                                                 # tokens see themselves, the last 150 see everything
+        first = torch.arange(T, dtype=torch.int32, device=DEV).expand(N, T).contiguous()
+        first[:, T - 150:] = 0
+    else:
+        first = firsts(kind, N, T, g)
+    check_gradients(act, N, 2, 1, T, 1, 1, D, first)
+
+
+@pytest.mark.parametrize("act,M,T,H,K,D", [("f32", 4, 400, 16, 8, 20), ("f32", 4, 390, 16, 8, 96), ("f32", 4, 200, 8, 4, 200), ("bf16", 4, 500, 32, 16, 64),
+                                           ("bf16", 4, 390, 32, 16, 100), ("bf16", 4, 500, 8, 4, 200)])
+@pytest.mark.parametrize("kind", ["packed", "holes"])
+def test_gradients_of_many_blocks(act, M, T, H, K, D, kind):
+    """More blocks of keys than run at once, so that each goes over all queries and heads that see its keys and writes its sums itself: several tiles of
+    queries for two heads, and depths that are cut into slices.  (A compute unit of 256 runs one of these blocks, or two of bfloat16 heads up to 128.)"""
+    N, slices = M * M, 1 if D <= 128 else 2 if act == "bf16" else 4
+    assert N * K * ((T + 127) // 128) * slices >= 2 * 256 * (2 if act == "bf16" and D <= 128 else 1)
+    check_gradients(act, N, M, 2, T, H, K, D, firsts(kind, N, T, rng(T)))
+
+
+class Corrected:
+    """Gradients in 64 bits, with bounds for a delta that bfloat16 outputs put off and sum ds over the keys puts right.  With weights off by a share P of
+    them, dp by e, out's inner product with dout by O: delta + drift is off by sum p P (|dp - delta| + O + e) + sum p e and its sums' roundings, which
+    is what dk meets.  dq: ds, which O is still in, and p, which is taken from it drift times, are rounded to half a step b."""
+
+    def __init__(self, q, k, v, dout, seen, H, K, scale):
+        b, group = TYPES["bf16"][2], H // K
+        plain = Want(q, k, v, seen, H, K, scale, "bf16", dout)
+        self.dv, self.dv_slack, self.dk, self.dq = plain.dv, plain.dv_slack, plain.dk, plain.dq
+        out, out_slack, lse, lse_slack = split(plain.out, H), split(plain.out_slack, H), plain.lse[..., None], plain.lse_slack[..., None]
+        q, do = split(q, H), split(dout, H)
+        k, v = (split(x, K).repeat_interleave(group, 1) for x in (k, v))
+        D, n = q.shape[3], seen.sum(2)[:, None, :, None].double()
+        kt, vt = k.transpose(2, 3).contiguous(), v.transpose(2, 3).contiguous()
+        p = torch.where(seen[:, None], (scale * q @ kt - lse).exp(), 0.0)
+        E = (2 * D + 16) * U * torch.where(seen[:, None], scale * q.abs() @ kt.abs(), 0.0).amax(-1, keepdim=True)
+        P, dp, e = E + lse_slack + 8 * U, do @ vt, (2 * D + 8) * U * (do.abs() @ vt.abs())
+        delta = (do * out).sum(-1, keepdim=True)
+        O = (do.abs() * out_slack).sum(-1, keepdim=True) + (2 * D + 4) * U * (do * out).abs().sum(-1, keepdim=True)  # noqa: E741
+        S, pe = (p * ((dp - delta).abs() + O + e)).sum(-1, keepdim=True), (p * e).sum(-1, keepdim=True)
+        off = (P + (n + 8) * U) * S + pe * 1.01 + 2 * U * delta.abs()
+        ds, m = p * (dp - delta), float(q.shape[2] * group)
+        slack = p * ((dp - delta).abs() * (P + 3 * U) + e + off + 2 * U * delta.abs()) * 1.01
+        mine = slack + b * ds.abs() * 1.01
+        shared = lambda x: merge(x.unflatten(1, (-1, group)).sum(2))  # noqa: E731
+        t = lambda x: x.transpose(2, 3).contiguous()  # noqa: E731
+        self.dk_slack = scale * (shared(t(mine) @ q.abs()) + 2 * m * U * shared(t(ds.abs() + slack) @ q.abs()))
+        both = ds.abs() + 2 * p * (O + off)
+        self.dq_slack = scale * merge((mine + 2.02 * b * p * (O + off)) @ k.abs() + 2 * (n + 6) * U * (both @ k.abs()))
+        for name in ("dk", "dq"):
+            setattr(self, name + "_slack", (getattr(self, name + "_slack") + (4 * U + b) * getattr(self, name).abs()) * 1.01 + TINY)
+
+
+@pytest.mark.parametrize("T,H,K,D", [(300, 4, 2, 64), (260, 4, 2, 96), (260, 2, 1, 128), (150, 4, 2, 20), (150, 2, 1, 200), (140, 2, 1, 256)])
+@pytest.mark.parametrize("window", [1, 2, 4, 30, 1_000])
+def test_delta_is_put_right(T, H, K, D, window):
+    """What rounding a bfloat16 output puts delta off by reaches neither dk nor dq (left as it is, it would be up to 5 to 25 times dk's bound and 3 to 19
+    times dq's in windows of 2 tokens)."""
+    t = torch.arange(T, device=DEV)
+    first = (t - window + 1).clamp(min=0).int().expand(4, T).contiguous()
+    check_gradients("bf16", 4, 2, 2, T, H, K, D, first, lambda q, k, v, dout: Corrected(q, k, v, dout, seen_of(first), H, K, D ** -0.5))
