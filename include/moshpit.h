@@ -437,7 +437,7 @@ int moshpit_dropout(moshpit_ctx *h, const void *x_dev, int32_t dtype, int64_t x_
  * with one of +inf or NaN, or -inf alone, out is NaN.  Tokens that see an infinity or a NaN in a value, or of binary32 ones an infinite score, are taken
  * anew one by one, which is slow: 8192 tokens of 4 heads of 128 that all see one in 103 ms, the call without it in 0.4.  lse_dev: NULL, or
  * [N][heads][n_tokens] floats, which the backward pass takes.  Weights are rounded to bfloat16 for their product with bfloat16 values; all else
- * is binary32.  scale > 0, 1 <= depth <= 256, heads <= 2^16.  out may take the place of nothing that is read. */
+ * is binary32.  0 < scale <= 2^127, 1 <= depth <= 256, heads <= 2^16.  out may take the place of nothing that is read. */
 int moshpit_attention(moshpit_ctx *h, const void *q_dev, int64_t q_row_stride, const void *k_dev, int64_t k_row_stride, const void *v_dev,
                       int64_t v_row_stride, int32_t dtype, const int32_t *first_dev, int64_t n_tokens, int32_t heads, int32_t kv_heads,
                       int32_t depth, float scale, void *out_dev, int64_t out_row_stride, float *lse_dev);

@@ -1600,7 +1600,8 @@ int check_heads(moshpit_ctx *h, int32_t heads, int32_t kv_heads, int32_t depth, 
     if (heads < 1 || kv_heads < 1 || heads % kv_heads != 0 || heads > 65536)
         return fail(h, MOSHPIT_EINVAL, "%d heads over %d heads of keys: a multiple, at most 2^16", heads, kv_heads);
     if (depth < 1 || depth > 256) return fail(h, MOSHPIT_EINVAL, "a head of %d: 1 .. 256", depth);
-    if (!(scale > 0.f) || !std::isfinite(scale)) return fail(h, MOSHPIT_EINVAL, "the scale must be finite and > 0");
+    // (at most 2^127: the kernels take it times log2 e)
+    if (!(scale > 0.f) || !(scale <= 0x1p127f)) return fail(h, MOSHPIT_EINVAL, "the scale must be > 0 and at most 2^127");
     return MOSHPIT_OK;
 }
 }  // namespace

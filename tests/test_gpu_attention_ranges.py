@@ -5,6 +5,7 @@ import math
 import pytest
 import torch
 
+from paper_2103_03239_amd import binding
 from test_gpu_attention import Want, cached_want, firsts, make, merge, peers, seen_of, split
 from test_gpu_local_ops import DEV, TINY, TYPES, U, close, normal, rng
 
@@ -217,3 +218,23 @@ def test_delta_is_put_right(T, H, K, D, window):
     t = torch.arange(T, device=DEV)
     first = (t - window + 1).clamp(min=0).int().expand(4, T).contiguous()
     check_gradients("bf16", 4, 2, 2, T, H, K, D, first, lambda q, k, v, dout: Corrected(q, k, v, dout, seen_of(first), H, K, D ** -0.5))
+
+
+@pytest.mark.parametrize("act", ["f32", "bf16"])
+def test_the_largest_scale(act):
+    """Scores of 0 by whatever scale are 0; one that is infinite times log2 e is refused."""
+    g, N, T, H, D = rng(4), 2, 70, 2, 16
+    q, k, v = make(N, T, H, H, D, act, g)
+    k.zero_()
+    first, spans = torch.zeros((N, T), dtype=torch.int32, device=DEV), torch.tensor([0, T], dtype=torch.int32, device=DEV).expand(N, T, 2).contiguous()
+    want = Want(q, k, v, seen_of(first), H, H, 1.0, act)
+    with peers(2, 1) as m:
+        out, lse = m.attention(q, k, v, first, H, scale=2.0 ** 127)
+        for scale in (2.5e38, 3.4e38):
+            for call in (lambda: m.attention(q, k, v, first, H, scale=scale), lambda: m.attention_cached(q, k, v, spans, H, scale=scale),
+                         lambda: m.attention_grad(out, q, k, v, out, lse, first, H, scale=scale)):
+                with pytest.raises(binding.MoshpitError, match="scale"):
+                    call()
+        m.sync()
+    close(out, want.out, want.out_slack)
+    close(lse, want.lse, want.lse_slack)
