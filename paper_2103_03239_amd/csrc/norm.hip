@@ -96,18 +96,16 @@ constexpr float kTooSmall = 0x1p-100f;   // (squares' lost bits: 2^-150 each, 2^
 // Of a row that LANES threads share: sum(factor) is the sum over it of (h factor)^2, in every one of them.
 template <int LANES, typename Sum> __device__ __forceinline__ Size size_of(float share, float eps, Sum sum)
 {
-    float mean = fmaf(sum(1.f), share, eps), root = 1.f;
-    if (!(mean < INFINITY) || mean < kTooSmall) {                      // (the same in every thread of the row)
-        root = mean < kTooSmall ? 0x1p48f : 0x1p-48f;
-        const float factor = root * root;
-        mean = fmaf(sum(factor), share, eps * factor * factor);
+    const float mean = fmaf(sum(1.f), share, eps);
+    Size s{1.f, rsqrtf(mean), 1.f};
+    if (__builtin_expect(!(mean < INFINITY) || mean < kTooSmall, 0)) { // (the same in every thread of the row)
+        s.root = mean < kTooSmall ? 0x1p48f : 0x1p-48f;
+        s.factor = s.root * s.root;
+        s.inverse = rsqrtf(fmaf(sum(s.factor), share, eps * s.factor * s.factor));
     }
-    float inverse = rsqrtf(mean);
-    if constexpr (LANES >= 64) {                                       // (the same in every lane: they take no vector registers)
-        root = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(root)));
-        inverse = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(inverse)));
-    }
-    return Size{root * root, inverse, root};
+    if constexpr (LANES >= 64)                                         // (they take no vector registers: 16 x 4096 rows of 4096 in bfloat16, backward: 407 us, 490 with them)
+        for (float *v : {&s.factor, &s.inverse, &s.root}) *v = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(*v)));
+    return s;
 }
 
 template <int DT, int ST, int LANES, int U>
@@ -221,9 +219,8 @@ __global__ __launch_bounds__(1024) void wide_norm_kernel(NormArgs a)
 
 // sums: [N][parts][width], the gain's gradient over the rows of a block, which takes every parts-th one, so that the blocks that run at the same time read
 // neighbouring rows (4 x 30000 rows of 1000 in bfloat16: 189 us, by pieces of consecutive rows 218).
-// Rows of 2048 to 4096 in bfloat16: four waves a SIMD (16 x 4096 rows of 4096: 407 us; as many registers as the compiler likes, three waves: 490).
 template <int DT, int ST, int LANES, int U>
-__global__ __launch_bounds__(threads_of<LANES>(), (LANES == 256 && U == 2 ? 4 : 1))
+__global__ __launch_bounds__(threads_of<LANES>())
 void norm_grad_kernel(NormGradArgs a, int64_t parts, float *__restrict__ sums)
 {
     constexpr int ES = DT == 0 ? 4 : 2, GS = ST == 0 ? 4 : 2, SLOTS = threads_of<LANES>() / LANES;
