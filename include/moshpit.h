@@ -435,7 +435,8 @@ int moshpit_dropout(moshpit_ctx *h, const void *x_dev, int32_t dtype, int64_t x_
  *   out[t] = sum over s of exp(scale * q[t] . k[s] - lse[t]) v[s],   lse[t] = log of the sum over s of exp(scale * q[t] . k[s]);
  * 0 for out and lse where there is no token.  Infinities and NaN reach no token that does not see them.  Of those that do, a score of -inf is a weight of 0;
  * with one of +inf or NaN, or -inf alone, out is NaN.  Tokens that see an infinity or a NaN in a value, or of binary32 ones an infinite score, are taken
- * anew one by one, which is slow: 8192 tokens of 4 heads of 128 that all see one in 103 ms, the call without it in 0.4.  lse_dev: NULL, or
+ * anew one by one, which is slow: 8192 tokens of 4 heads of 128 that all see one in 103 ms, the call without it in 0.4.  Values of up to 2^127 in
+ * size have finite outputs.  lse_dev: NULL, or
  * [N][heads][n_tokens] floats, which the backward pass takes.  Weights are rounded to bfloat16 for their product with bfloat16 values; all else
  * is binary32.  0 < scale <= 2^127, 1 <= depth <= 256, heads <= 2^16.  out may take the place of nothing that is read. */
 int moshpit_attention(moshpit_ctx *h, const void *q_dev, int64_t q_row_stride, const void *k_dev, int64_t k_row_stride, const void *v_dev,
@@ -444,8 +445,9 @@ int moshpit_attention(moshpit_ctx *h, const void *q_dev, int64_t q_row_stride, c
 
 /* Its backward pass: the gradients of queries, keys and values (summed over the query heads that share them) for the gradient
  * dout of out; out and lse as moshpit_attention left them.  Zeros where there is no token, whose rows may hold anything here too; but an infinity or
- * a NaN in a row with a token may make gradients of the same peer's other sequences NaN (its products with weights of 0 count).  The gradients must not
- * overlap each other or what is read. */
+ * a NaN in a row with a token may make gradients of the same peer's other sequences NaN (its products with weights of 0 count).  With bfloat16 matrices
+ * the weights and the gradients of the scores are rounded to bfloat16 for their products; what the rounding of out does to dq and dk is taken off
+ * again.  The gradients must not overlap each other or what is read. */
 int moshpit_attention_grad(moshpit_ctx *h, const void *dout_dev, int64_t dout_row_stride, const void *q_dev, int64_t q_row_stride, const void *k_dev,
                            int64_t k_row_stride, const void *v_dev, int64_t v_row_stride, const void *out_dev, int64_t out_row_stride, int32_t dtype,
                            const float *lse_dev, const int32_t *first_dev, int64_t n_tokens, int32_t heads, int32_t kv_heads, int32_t depth, float scale,
@@ -456,7 +458,7 @@ int moshpit_attention_grad(moshpit_ctx *h, const void *dout_dev, int64_t dout_ro
  * values: n_keys rows a peer; spans_dev, [N][sequences][2] int32: the sequence's rows are spans[..][0] .. spans[..][1] - 1 of them (cut to
  * 0 .. n_keys), the last n_new the new tokens' own, and new token b sees all but the last n_new - 1 - b.  A token that sees none, of
  * an empty span for instance, gets zeros.  Rows outside the spans are not read, spans may share rows, and infinities and NaN reach no token that does
- * not see them; finite values have finite outputs, the largest included.  n_new <= 4096. */
+ * not see them; of infinities, NaN and large values that tokens see, as for moshpit_attention.  n_new <= 4096. */
 int moshpit_attention_cached(moshpit_ctx *h, const void *q_dev, int64_t q_row_stride, const void *k_dev, int64_t k_row_stride, const void *v_dev,
                              int64_t v_row_stride, int32_t dtype, const int32_t *spans_dev, int64_t sequences, int64_t n_new, int64_t n_keys, int32_t heads,
                              int32_t kv_heads, int32_t depth, float scale, void *out_dev, int64_t out_row_stride);

@@ -2,8 +2,9 @@
 //   s_ij = scale q_i . k_j,   out_i = sum_j exp(s_ij - lse_i) v_j,   lse_i = log sum_j exp s_ij
 // over the keys first_i <= j <= i of places that hold a token (cached: over a span's rows up to the query's own).
 //
-// One pass over the keys with running largest and sum.  A wave holds 32 queries as columns; tiles of keys and values lie in LDS, two of each, the
-// next ones on their way through registers.  Scores come as blocks [key][query] (attention_tile.h), so a query's largest and sum are
+// One pass over the keys with running largest and sum.  A wave holds 32 queries as columns; tiles of keys and values lie in LDS, two of each (binary32 heads
+// deeper than 64: one, where two blocks are to run beside each other).  The next ones go straight into LDS where heads are whole vectors of the type that it
+// has them in, else through registers.  Scores come as blocks [key][query] (attention_tile.h), so a query's largest and sum are
 // taken within a lane and once between the two halves of the wave, and the weights go into the second product where they lie.
 // Sums are rescaled only where a query's largest score has grown by more than 2^8 (weights stay below 2^8, in binary32).
 //
@@ -12,11 +13,13 @@
 // not is taken again, key by key over those that it sees (and of binary32 ones in parts, one whose weights are not).  That is slow: 8192 tokens of 4 heads
 // of 128 in bfloat16 in 103 ms where the first value has an infinity; a NaN in the key in the middle of 4096 of 80 in binary32: 7 ms.
 //
-// Prompts are bound by the vector instructions beside the matrix ones: an exponential, a maximum and a rounding for each pair against 4 depth
-// multiplications (heads of 128 in bfloat16, the matrix cores are busy for 42 % of the time, vector instructions for about as much).  2 x 16 heads of 128, 4 heads of keys,
-// 8192 tokens in two sequences a peer: 372 us, 0.87 PFLOP/s over the pairs that are seen.  One new token is bound by the reads of the cache: 4 x 8
-// sequences of up to 16384, 4 heads of keys of 128 in bfloat16, in 144 us, 4.9 TB/s, of which about 20 us are the start, the longest span's end and
-// the join.
+// Prompts are bound by what follows on what: an exponential, a maximum and a rounding for each pair beside its 4 depth multiplications, which a wave
+// makes one after the other, and two waves a SIMD (heads of 128) that nothing keeps half a step apart.  Heads of 128 in bfloat16: matrix cores busy for 42 % of
+// the time, vector instructions for 46, neither full; of 64, four waves a SIMD: 21 and 54.  2 x 16 heads of 128, 4 heads of keys,
+// 8192 tokens in two sequences a peer: 367 us, 0.88 PFLOP/s over the pairs that are seen; 16 x 8 heads of 64, 4 of keys, 4096 tokens in 8 sequences: 139 us.
+// One new token is bound by the reads of the cache: 4 x 8
+// sequences of up to 16384, 4 heads of keys of 128 in bfloat16, in 145 us, 4.9 TB/s, of which about 20 us are the start, the longest span's end and
+// the join; 5 new tokens of each: 160 us.
 #include <hip/hip_runtime.h>
 
 #include "attention_tile.h"
@@ -608,7 +611,9 @@ hipError_t launch_attention(AttentionArgs a, int dtype, int compute_units, hipSt
     });
 }
 
-// Blocks of cached_kernel a compute unit, as its registers allow.
+// Blocks of cached_kernel a compute unit, as its registers allow.  The deepest heads hold a tile on its way, the queries and the sums in more than there are:
+// 84 of 256 in bfloat16 spill, 205 of 192 and 799 of 256 in binary32 (4 x 8 sequences, 4 heads of keys, caches of 8192 in bfloat16 and 4096 in binary32: of 192
+// 144 us and 242, of 256 374 and 410).
 constexpr int cached_waves(Form f, int dp) { return f == kBf16 && dp <= 128 ? 2 : 1; }
 
 // Shares of a span: twice the blocks that run at once, and 512 keys each and more where the keys of a peer are one sequence's.

@@ -10,8 +10,9 @@
 //            the columns hold both factors of
 //   keys     a wave holds 32 keys and values as columns and goes over the queries that see them: blocks [query][key], dk and dv [depth][key]
 // Bound by registers: the columns and the sums leave two waves a SIMD, which the exponentials and roundings of one hide badly behind the
-// products of the other (matrix cores busy for a quarter of the time).  16 x 8 heads of 64, 4 heads of keys, 4096 tokens in bfloat16: queries 270 us, keys 263 us
-// (forward 133 us).
+// products of the other (matrix cores busy for 22 % of the time in the one, 25 in the other; vector instructions 37 and 32).  16 x 8 heads of 64, 4 heads of
+// keys, 4096 tokens in bfloat16: queries 273 us, keys 258 us (forward 139 us).  What spills: keys' kernel for bfloat16 heads of 128 (7 registers; 122 where
+// heads are not whole vectors), queries' kernel for such heads of 96 (44) and 256 (244), both for binary32 heads of 256 and, not whole vectors, of 192.
 #include <hip/hip_runtime.h>
 
 #include "attention_tile.h"

@@ -10,8 +10,8 @@
 //
 // Forms:
 //   kBf16   bfloat16 matrices; weights are rounded to bfloat16 for their product, the rest is exact before the binary32 sums
-//   kParts  binary32 matrices as three bfloat16 parts of 8 significant bits each, six products in place of one: what is left out is 2^-24 of
-//           a product and less.  At sixteen times the rate of the binary32 matrix instructions, so 2.7 times as fast
+//   kParts  binary32 matrices as three bfloat16 parts of 8 significant bits each, six products in place of one: what is left out is below 2^-21 of
+//           a product and of its sign, 2^-24.5 of it on average.  At sixteen times the rate of the binary32 matrix instructions, so 2.7 times as fast
 //   kF32    binary32 matrices by the binary32 matrix instructions, where the parts of deep heads do not fit the registers
 // DP: the depth, rounded up to a multiple of 32 (zeros behind it).
 #pragma once
@@ -187,7 +187,9 @@ __device__ __forceinline__ f32x16 mfma_bf16(const u32x4 &a, const u32x4 &b, cons
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-// Products of parts, the smallest first; 2^-24 of a product and less is left out.
+// Products of parts, the smallest first.  Parts are cut off, so the second is below 2^-7 of its number and the third below 2^-15: the three products that
+// are left out come to less than 2 * 2^-22 + 2^-30 of the whole.  (Numbers rounded to their parts would leave out 2^-24 and less, but the largest
+// ones then round to infinity.)
 constexpr int kTileParts[6] = {2, 1, 0, 1, 0, 0}, kHeldParts[6] = {0, 1, 2, 0, 1, 0};
 
 // v, as a number that the compiler knows nothing of: addresses made of it are made anew where they are used, in an instruction or none, and do not
