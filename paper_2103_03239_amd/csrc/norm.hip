@@ -83,7 +83,7 @@ __device__ __forceinline__ void save_unit(float (&f)[kUnit], int64_t at, int lef
             if (k < left) codes[at + k] = static_cast<int8_t>(w[k / 4] >> (8 * (k & 3)));
 }
 
-// What a row's results are made with: x^ = (h factor) inverse, 1 / root mean square = (inverse root) root, root^2 = factor and
+// What a row's results are made with: x^ = (h factor) inverse, 1 / root mean square = (inverse root) root (each a factor of its own), root^2 = factor and
 //   inverse = (mean((h factor)^2) + eps factor^2)^(-1/2).
 // factor is 1 but where mean(h^2) + eps passes binary32, or is so small that squares lose bits below the normal numbers.  With 2^-96 the largest elements'
 // squares are 2^64 and the sum of 2^23 of them 2^87 (elements that it takes below the normal numbers are off by 2^-95 of the row's root mean square
@@ -277,7 +277,7 @@ void norm_grad_kernel(NormGradArgs a, int64_t parts, float *__restrict__ sums)
             for (int k = 0; k < kUnit; ++k) {
                 const float v = h[u][k] * s.factor * s.inverse;
                 dg[u][k] = fmaf(dy[u][k], v, dg[u][k]);
-                const float e = outer * (dy[u][k] * g[u][k] - v * mean) * s.root;
+                const float e = outer * ((dy[u][k] * g[u][k] - v * mean) * s.root);
                 d[k] = a.dtotal ? d[k] + e : e;
             }
             store_unit<DT>(a.dx + (row * a.dx_stride + at[u]) * ES, left[u], d);
@@ -372,7 +372,7 @@ __global__ __launch_bounds__(1024) void wide_norm_grad_kernel(NormGradArgs a, co
         if (a.dtotal) load_unit<DT>(a.dtotal + (row * a.dtotal_stride + at) * ES, width - at, more);
 #pragma unroll
         for (int k = 0; k < kUnit; ++k) {
-            const float e = s.y * s.w * (d[k] * g[k] - h[k] * s.x * s.y * s.z) * s.w;
+            const float e = s.y * s.w * ((d[k] * g[k] - h[k] * s.x * s.y * s.z) * s.w);
             d[k] = a.dtotal ? more[k] + e : e;
         }
         store_unit<DT>(a.dx + (row * a.dx_stride + at) * ES, width - at, d);
